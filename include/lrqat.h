@@ -59,7 +59,9 @@ typedef enum {
   LRQAT_ERR_ALIGNMENT = -3,   /* a pointer is not 16-byte aligned                     */
   LRQAT_ERR_WORKSPACE = -4,   /* workspace missing or smaller than required           */
   LRQAT_ERR_CUDA = -5,        /* a CUDA runtime/driver call or launch failed          */
-  LRQAT_ERR_TIMEOUT = -6      /* a kernel's bounded wait gave up (device status)      */
+  LRQAT_ERR_TIMEOUT = -6,     /* a kernel's bounded wait gave up (device status)      */
+  LRQAT_ERR_RANGE = -7        /* device arrays of a batch contradict its bounds (device
+                                 status; lrqat_kv_write, _read and _attn)             */
 } lrqat_status;
 
 /* Storage format of the frozen base Phi0 (Sec. 3, "Downcasting operator"). */
@@ -260,6 +262,121 @@ int lrqat_linear_bwd_quantized(const lrqat_layer* layer, int64_t T, const uint16
 int lrqat_merge(const lrqat_layer* layer, const void* Phi0, const uint16_t* A, const uint16_t* B,
                 int8_t* W_Z, lrqat_stream_t stream);
 
+/* ---- Norm in front of a quantized linear layer ----------------------------------
+ * Residual addition, root-mean-square norm and the per-token 8-bit quantizer of the
+ * weight-activation runs (act_per_token of lrqat_layer) in one pass, for rows of k:
+ *   h = x + r,  y = gamma h / sqrt(mean(h^2) + eps),
+ *   s = max|y| / 127 (1 for a row of zeros),  c = round(y / s),  y_hat = s c.
+ * Everything between the inputs and the rounded outputs is fp32 (y is not rounded to
+ * bf16 before the quantizer, as it is where lrqat_act_quant reads a stored y).  A row
+ * that holds a NaN or an infinity, or whose sum of squares overflows fp32, gets a NaN
+ * scale.  k: a multiple of 8, at most 16384. */
+typedef struct {
+  int64_t k;
+  float eps;        /* >= 0                                              */
+  int32_t act_bits; /* 0: y itself; 8: quantized per token               */
+} lrqat_norm;
+
+/* X, R: bf16 [T, k] (R NULL: h = x); gamma: bf16 [k].  Outputs: H = bf16(h) [T, k], the
+ * residual stream (required with R, else NULL allowed; may be X or R itself);
+ * act_bits 0: Y = bf16(y) [T, k], Y_q and s_y NULL;
+ * act_bits 8: Y = bf16(y_hat), the X_q that lrqat_linear_fwd_quantized and
+ * lrqat_linear_bwd_quantized take with act_per_token = 1, and / or Y_q = c, int8 [T, k],
+ * with s_y = s, fp32 [T] (required with Y_q, else nullable).  One of Y and Y_q may be NULL. */
+int lrqat_add_rmsnorm_fwd(const lrqat_norm* norm, int64_t T, const uint16_t* X, const uint16_t* R,
+                          const uint16_t* gamma, uint16_t* H, uint16_t* Y, int8_t* Y_q, float* s_y,
+                          lrqat_stream_t stream);
+
+/* Bytes of workspace lrqat_add_rmsnorm_bwd needs for T rows when it writes dgamma (none
+ * without). */
+size_t lrqat_add_rmsnorm_bwd_workspace_bytes(const lrqat_norm* norm, int64_t T);
+
+/* Gradient of the norm at the stored residual stream H (the X of a forward without R), the
+ * quantizer passed straight through and its scale not differentiated: with
+ * q = 1 / sqrt(mean(h^2) + eps) and g = dy gamma,
+ *   dX = q (g - h q^2 mean(g h)) + dH,  the gradient of x and of r alike;
+ *   dgamma = sum over the rows of dy h q.
+ * dY, dH (nullable: the gradient of H from the rest of the network), H, dX (output; may be dY
+ * or dH itself): bf16 [T, k].  dgamma: fp32 [k] or NULL (a frozen norm: then no workspace);
+ * accumulate = 1 adds to it.  Sums run in a fixed order. */
+int lrqat_add_rmsnorm_bwd(const lrqat_norm* norm, int64_t T, const uint16_t* dY, const uint16_t* dH,
+                          const uint16_t* H, const uint16_t* gamma, uint16_t* dX, float* dgamma, int accumulate,
+                          void* workspace, size_t workspace_bytes, lrqat_stream_t stream);
+
+/* The values of stored 8-bit activations: X_hat = bf16(s c), bf16 [T, k], from codes int8
+ * [T, k] and scales fp32 [T] (lrqat_add_rmsnorm_fwd's Y_q and s_y): a backward that keeps a byte
+ * per activation rebuilds the X_q of lrqat_linear_bwd_quantized with it, bit for bit. */
+int lrqat_act_dequant(const lrqat_norm* norm, int64_t T, const int8_t* codes, const float* s, uint16_t* X_hat,
+                      lrqat_stream_t stream);
+
+/* ---- 8-bit key / value cache (the KV8 of the W4A8KV8 runs, Sec. 4) ----------------
+ * A pool of blocks of `block` tokens.  Codes are int8 [n_blocks, n_kv_heads, block,
+ * head_dim], with one fp32 scale per block and head, [n_blocks, n_kv_heads]:
+ * value = scale * code.  A block belongs to one sequence while it is written (several
+ * sequences may read it); nothing has to be cleared before its first use. */
+typedef struct {
+  int64_t n_blocks;
+  int32_t n_kv_heads;
+  int32_t head_dim;   /* 64 or 128                          */
+  int32_t block;      /* 16, 32, 64 or 128                  */
+  int8_t* k_codes;
+  int8_t* v_codes;
+  float* k_scale;
+  float* v_scale;
+} lrqat_kv_cache;
+
+/* A ragged batch: rows row_start[b] .. row_start[b + 1] - 1 of the call's row arrays are
+ * sequence b's newest tokens, at positions len[b] - n .. len[b] - 1 for its n rows; position
+ * p lies in cache block block_table[b, p / block].  Rows at negative positions (n > len[b], such
+ * as the row of an idle slot with len 0) are padding: they are not written, not read back,
+ * and attend to nothing.  The arrays live on the device; the bounds are the host's, and may be
+ * larger than what the arrays hold (a captured graph keeps them).  A sequence that exceeds them,
+ * or a block id outside the pool, is skipped, and lrqat_get_device_status reports
+ * LRQAT_ERR_RANGE. */
+typedef struct {
+  int32_t n_seqs;             /* 1 .. 65535                                           */
+  int32_t max_blocks;         /* columns of block_table                               */
+  const int32_t* len;         /* [n_seqs] tokens of the sequence, the call's included */
+  const int32_t* row_start;   /* [n_seqs + 1]                                         */
+  const int32_t* block_table; /* [n_seqs, max_blocks]                                 */
+  int64_t rows;               /* rows of the call's row arrays                        */
+  int32_t max_rows;           /* bound on the rows of one sequence                    */
+  int32_t max_len;            /* bound on len, at most max_blocks * block             */
+} lrqat_kv_batch;
+
+/* Quantizes the batch's new keys and values into the cache.  For each block and head, with a the
+ * largest magnitude among the block's new tokens:
+ *   a block that starts with a new token takes scale s = a / 127 (1 if a = 0);
+ *   one that holds older tokens takes s = max(its scale, a / 127), and where that grew the older
+ *   codes become round(c * (old scale / s));
+ *   new codes are round(x / s).
+ * Divisions are fp32; a block that takes a NaN or an infinity gets a NaN scale.  Writing the same
+ * rows again changes nothing.
+ * K, V: bf16 [rows, n_kv_heads, head_dim], consecutive rows ldk / ldv elements apart (multiples of
+ * 8), so that they may be parts of one projection's output. */
+int lrqat_kv_write(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, const uint16_t* K, int64_t ldk,
+                   const uint16_t* V, int64_t ldv, lrqat_stream_t stream);
+
+/* Reads the batch's rows back: K, V = bf16(scale * code), laid out as in lrqat_kv_write. */
+int lrqat_kv_read(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, uint16_t* K, int64_t ldk, uint16_t* V,
+                  int64_t ldv, lrqat_stream_t stream);
+
+/* Bytes of workspace lrqat_kv_attn needs for this batch's bounds (0: none). */
+size_t lrqat_kv_attn_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                                     int32_t window);
+
+/* Causal attention of the batch's rows over the cache (after lrqat_kv_write of the same batch):
+ *   O[i, h] = sum_j softmax_j(softmax_scale q[i, h] . k_j) v_j
+ * over the keys j at positions p - window < j <= p for a row at position p (window 0: all j <= p);
+ * query head h reads key/value head h / (n_heads / n_kv_heads).  A row that sees no key is 0.
+ * n_heads: a multiple of n_kv_heads.  Q, O: bf16 [rows, n_heads, head_dim], consecutive rows
+ * ldq / ldo elements apart (multiples of 8).
+ * Scores, the softmax statistics and the sums are fp32; probabilities are rounded to 11
+ * significant bits.  The result of a row does not depend on the order of thread blocks. */
+int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
+                  int32_t window, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo, void* workspace,
+                  size_t workspace_bytes, lrqat_stream_t stream);
+
 /* ---- Optimizer step on A, B, s (App. B, Table B1) ------------------------------
  * AdamW with decoupled weight decay, bias-corrected moments, separate learning rates
  * for the adapters and the scales, after clipping the global L2 norm of all
@@ -351,7 +468,8 @@ int lrqat_get_lowrank_path(void);
 
 /* Synchronizes `stream`, then reads and clears the device status word of the
  * current device.  Returns LRQAT_OK, LRQAT_ERR_TIMEOUT (a kernel's bounded
- * wait gave up since the last call) or LRQAT_ERR_CUDA. */
+ * wait gave up since the last call), LRQAT_ERR_RANGE (a batch's device arrays
+ * contradicted its bounds) or LRQAT_ERR_CUDA. */
 int lrqat_get_device_status(lrqat_stream_t stream);
 
 /* ---------------------------------------------------------------------------

@@ -17,6 +17,7 @@
 
 #include "kernels.h"
 #include "merge.h"
+#include "serve.h"
 #include "lrqat.h"
 
 namespace lrqat {
@@ -585,6 +586,101 @@ int run_codes_pass(const lrqat_layer& L, const void* Phi0, const uint16_t* A, co
   LRQAT_LAUNCH("lowrank_codes", 1, stream,
                launch_merge_tc(L.phi_format, L.u_bf16, direct ? 0 : 1, tm_a, tm_b, tm_phi, a, stream),
                "low-rank code pass");
+  return LRQAT_OK;
+}
+
+// ------------------------------------------- norm, 8-bit cache, cache attention --
+constexpr int kMaxNormWidth = 16384;
+
+int validate_norm(const lrqat_norm* n, int64_t T) {
+  if (!n) return fail(LRQAT_ERR_INVALID_ARG, "norm is NULL");
+  if (n->k <= 0 || T < 1)
+    return fail(LRQAT_ERR_INVALID_ARG, "k and T must be positive (k=%lld T=%lld)", (long long)n->k, (long long)T);
+  if (n->k % 8 || n->k > kMaxNormWidth)
+    return fail(LRQAT_ERR_UNSUPPORTED, "k must be a multiple of 8 up to %d (k=%lld)", kMaxNormWidth, (long long)n->k);
+  if (T > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "T too large (T=%lld)", (long long)T);
+  if (!(n->eps >= 0.0f) || !std::isfinite(n->eps)) return fail(LRQAT_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (n->act_bits != 0 && n->act_bits != 8)
+    return fail(LRQAT_ERR_UNSUPPORTED, "act_bits must be 0 or 8 (got %d)", n->act_bits);
+  return LRQAT_OK;
+}
+
+// The SMs of the current device; 152 when there is none (workspace sizes on a host without a GPU).
+int sm_count() {
+  DeviceInfo* d = nullptr;
+  return device_info(&d) == LRQAT_OK ? d->sms : 152;
+}
+
+// Checks a cache and a batch and lowers them to kernel arguments (all but the status word).
+int kv_args(const lrqat_kv_cache* c, const lrqat_kv_batch* b, KvArgs* a) {
+  if (!c || !b) return fail(LRQAT_ERR_INVALID_ARG, "cache and batch must be non-NULL");
+  if (c->n_blocks < 1 || c->n_kv_heads < 1)
+    return fail(LRQAT_ERR_INVALID_ARG, "n_blocks and n_kv_heads must be positive");
+  if (c->n_blocks > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "n_blocks too large");
+  if (c->n_kv_heads > 16384) return fail(LRQAT_ERR_UNSUPPORTED, "n_kv_heads %d > 16384", c->n_kv_heads);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(LRQAT_ERR_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", c->head_dim);
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128)
+    return fail(LRQAT_ERR_UNSUPPORTED, "block must be 16, 32, 64 or 128 (got %d)", c->block);
+  LRQAT_CHECK_PTR(c->k_codes, "k_codes");
+  LRQAT_CHECK_PTR(c->v_codes, "v_codes");
+  LRQAT_CHECK_PTR(c->k_scale, "k_scale");
+  LRQAT_CHECK_PTR(c->v_scale, "v_scale");
+  if (b->n_seqs < 1 || b->max_blocks < 1 || b->rows < 0 || b->max_rows < 0 || b->max_len < 0)
+    return fail(LRQAT_ERR_INVALID_ARG, "n_seqs and max_blocks must be positive, rows, max_rows and max_len >= 0");
+  if (b->n_seqs > 65535) return fail(LRQAT_ERR_UNSUPPORTED, "n_seqs %d > 65535", b->n_seqs);
+  if (static_cast<int64_t>(b->max_blocks) * c->block > INT32_MAX - 1024)
+    return fail(LRQAT_ERR_UNSUPPORTED, "max_blocks * block does not fit 32 bits");
+  if (b->max_len > static_cast<int64_t>(b->max_blocks) * c->block)
+    return fail(LRQAT_ERR_INVALID_ARG, "max_len %d exceeds max_blocks * block", b->max_len);
+  if (b->rows > INT32_MAX || b->max_rows > (1 << 24))
+    return fail(LRQAT_ERR_UNSUPPORTED, "rows or max_rows too large");
+  if (!b->len || !b->row_start || !b->block_table)
+    return fail(LRQAT_ERR_INVALID_ARG, "len, row_start and block_table must be non-NULL");
+  if (((reinterpret_cast<uintptr_t>(b->len) | reinterpret_cast<uintptr_t>(b->row_start) |
+        reinterpret_cast<uintptr_t>(b->block_table)) & 3u) != 0)
+    return fail(LRQAT_ERR_ALIGNMENT, "len, row_start and block_table must be 4-byte aligned");
+  *a = KvArgs{};
+  a->codes[0] = c->k_codes;
+  a->codes[1] = c->v_codes;
+  a->scale[0] = c->k_scale;
+  a->scale[1] = c->v_scale;
+  a->n_blocks = c->n_blocks;
+  a->heads = c->n_kv_heads;
+  a->d = c->head_dim;
+  a->block_log2 = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
+  a->n_seqs = b->n_seqs;
+  a->len = b->len;
+  a->row_start = b->row_start;
+  a->table = b->block_table;
+  a->max_blocks = b->max_blocks;
+  a->rows = b->rows;
+  a->max_rows = b->max_rows;
+  a->max_len = b->max_len;
+  return LRQAT_OK;
+}
+
+int check_rows(const void* p, int64_t ld, int64_t width, const char* name) {
+  LRQAT_CHECK_PTR(p, name);
+  if (ld < width) return fail(LRQAT_ERR_INVALID_ARG, "%s: rows %lld elements apart are shorter than a row's %lld", name,
+                              (long long)ld, (long long)width);
+  if (ld % 8) return fail(LRQAT_ERR_ALIGNMENT, "%s: the row distance must be a multiple of 8 elements", name);
+  return LRQAT_OK;
+}
+
+int attn_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, int32_t window, AttnArgs* a) {
+  *a = AttnArgs{};
+  LRQAT_TRY(kv_args(cache, batch, &a->kv));
+  if (n_heads < 1 || n_heads % cache->n_kv_heads)
+    return fail(LRQAT_ERR_INVALID_ARG, "n_heads %d is not a positive multiple of n_kv_heads %d", n_heads,
+                cache->n_kv_heads);
+  if (window < 0) return fail(LRQAT_ERR_INVALID_ARG, "window must be >= 0");
+  a->group = n_heads / cache->n_kv_heads;
+  a->window = window;
+  plan_attn(*a, sm_count());
+  if (static_cast<int64_t>(a->kv.max_rows) * a->group > (1 << 24) ||
+      static_cast<int64_t>(a->kv.heads) * a->row_tiles > 65535)
+    return fail(LRQAT_ERR_UNSUPPORTED, "too many (token, head) rows in one sequence");
   return LRQAT_OK;
 }
 }  // namespace
@@ -1214,6 +1310,133 @@ int lrqat_adamw_step(const lrqat_layer* layer, const lrqat_adamw* opt, const flo
   return LRQAT_OK;
 }
 
+int lrqat_add_rmsnorm_fwd(const lrqat_norm* norm, int64_t T, const uint16_t* X, const uint16_t* R,
+                          const uint16_t* gamma, uint16_t* H, uint16_t* Y, int8_t* Y_q, float* s_y,
+                          lrqat_stream_t stream) {
+  LRQAT_TRY(validate_norm(norm, T));
+  LRQAT_CHECK_PTR(X, "X");
+  LRQAT_CHECK_PTR(gamma, "gamma");
+  if (R) {
+    LRQAT_CHECK_PTR(R, "R");
+    LRQAT_CHECK_PTR(H, "H (with R)");
+  }
+  if (H && !aligned16(H)) return fail(LRQAT_ERR_ALIGNMENT, "H is not 16-byte aligned");
+  if (!Y && !Y_q) return fail(LRQAT_ERR_INVALID_ARG, "one of Y and Y_q must be non-NULL");
+  if (norm->act_bits == 0 && (Y_q || s_y)) return fail(LRQAT_ERR_INVALID_ARG, "Y_q and s_y need act_bits == 8");
+  if (Y_q && !s_y) return fail(LRQAT_ERR_INVALID_ARG, "Y_q needs s_y");
+  if (!aligned16(Y) || !aligned16(Y_q) || !aligned16(s_y))
+    return fail(LRQAT_ERR_ALIGNMENT, "Y, Y_q and s_y must be 16-byte aligned");
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  const NormFwdArgs a{T, norm->k, norm->eps, X, R, gamma, H, Y, Y_q, s_y, norm->act_bits == 8};
+  LRQAT_LAUNCH("add_rmsnorm_fwd", 1, stream, launch_add_rmsnorm_fwd(a, dev->sms, stream), "norm launch");
+  return LRQAT_OK;
+}
+
+size_t lrqat_add_rmsnorm_bwd_workspace_bytes(const lrqat_norm* norm, int64_t T) {
+  if (validate_norm(norm, T) != LRQAT_OK) return 0;
+  return static_cast<size_t>(norm_bwd_parts(T, norm->k, sm_count())) * norm->k * sizeof(float);
+}
+
+int lrqat_add_rmsnorm_bwd(const lrqat_norm* norm, int64_t T, const uint16_t* dY, const uint16_t* dH,
+                          const uint16_t* H, const uint16_t* gamma, uint16_t* dX, float* dgamma, int accumulate,
+                          void* workspace, size_t workspace_bytes, lrqat_stream_t stream) {
+  LRQAT_TRY(validate_norm(norm, T));
+  LRQAT_CHECK_PTR(dY, "dY");
+  LRQAT_CHECK_PTR(H, "H");
+  LRQAT_CHECK_PTR(gamma, "gamma");
+  LRQAT_CHECK_PTR(dX, "dX");
+  if (!aligned16(dH) || !aligned16(dgamma))
+    return fail(LRQAT_ERR_ALIGNMENT, "dH and dgamma must be 16-byte aligned");
+  if (dgamma) {
+    const size_t need = lrqat_add_rmsnorm_bwd_workspace_bytes(norm, T);
+    if (!workspace || workspace_bytes < need)
+      return fail(LRQAT_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
+    if (!aligned16(workspace)) return fail(LRQAT_ERR_ALIGNMENT, "workspace is not 16-byte aligned");
+  }
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  const NormBwdArgs a{T, norm->k, norm->eps, dY, dH, H, gamma, dX, dgamma, static_cast<float*>(workspace), accumulate};
+  LRQAT_LAUNCH("add_rmsnorm_bwd", dgamma ? 2 : 1, stream, launch_add_rmsnorm_bwd(a, dev->sms, stream),
+               "norm backward launch");
+  return LRQAT_OK;
+}
+
+int lrqat_act_dequant(const lrqat_norm* norm, int64_t T, const int8_t* codes, const float* s, uint16_t* X_hat,
+                      lrqat_stream_t stream) {
+  LRQAT_TRY(validate_norm(norm, T));
+  LRQAT_CHECK_PTR(codes, "codes");
+  LRQAT_CHECK_PTR(s, "s");
+  LRQAT_CHECK_PTR(X_hat, "X_hat");
+  LRQAT_LAUNCH("act_dequant", 1, stream, launch_act_dequant(codes, s, T, norm->k, X_hat, stream), "dequantizer launch");
+  return LRQAT_OK;
+}
+
+int lrqat_kv_write(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, const uint16_t* K, int64_t ldk,
+                   const uint16_t* V, int64_t ldv, lrqat_stream_t stream) {
+  KvArgs a;
+  LRQAT_TRY(kv_args(cache, batch, &a));
+  if (a.rows == 0) return LRQAT_OK;
+  LRQAT_TRY(check_rows(K, ldk, static_cast<int64_t>(a.heads) * a.d, "K"));
+  LRQAT_TRY(check_rows(V, ldv, static_cast<int64_t>(a.heads) * a.d, "V"));
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  a.status = dev->status;
+  LRQAT_LAUNCH("kv_write", 1, stream, launch_kv_write(a, K, ldk, V, ldv, stream), "cache write launch");
+  return LRQAT_OK;
+}
+
+int lrqat_kv_read(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, uint16_t* K, int64_t ldk, uint16_t* V,
+                  int64_t ldv, lrqat_stream_t stream) {
+  KvArgs a;
+  LRQAT_TRY(kv_args(cache, batch, &a));
+  if (a.rows == 0) return LRQAT_OK;
+  LRQAT_TRY(check_rows(K, ldk, static_cast<int64_t>(a.heads) * a.d, "K"));
+  LRQAT_TRY(check_rows(V, ldv, static_cast<int64_t>(a.heads) * a.d, "V"));
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  a.status = dev->status;
+  LRQAT_LAUNCH("kv_read", 1, stream, launch_kv_read(a, K, ldk, V, ldv, stream), "cache read launch");
+  return LRQAT_OK;
+}
+
+size_t lrqat_kv_attn_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                                     int32_t window) {
+  AttnArgs a;
+  if (attn_args(cache, batch, n_heads, window, &a) != LRQAT_OK) return 0;
+  return static_cast<size_t>(attn_part_rows(a)) * (a.kv.d + 4) * sizeof(float);
+}
+
+int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
+                  int32_t window, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo, void* workspace,
+                  size_t workspace_bytes, lrqat_stream_t stream) {
+  AttnArgs a;
+  LRQAT_TRY(attn_args(cache, batch, n_heads, window, &a));
+  if (!std::isfinite(softmax_scale)) return fail(LRQAT_ERR_INVALID_ARG, "softmax_scale must be finite");
+  if (a.kv.rows == 0 || a.kv.max_rows == 0) return LRQAT_OK;
+  LRQAT_TRY(check_rows(Q, ldq, static_cast<int64_t>(n_heads) * a.kv.d, "Q"));
+  LRQAT_TRY(check_rows(O, ldo, static_cast<int64_t>(n_heads) * a.kv.d, "O"));
+  const int64_t part_rows = attn_part_rows(a);
+  const size_t need = static_cast<size_t>(part_rows) * (a.kv.d + 4) * sizeof(float);
+  if (need > 0) {
+    if (!workspace || workspace_bytes < need)
+      return fail(LRQAT_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
+    if (!aligned16(workspace)) return fail(LRQAT_ERR_ALIGNMENT, "workspace is not 16-byte aligned");
+  }
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  a.kv.status = dev->status;
+  a.Q = Q;
+  a.ldq = ldq;
+  a.O = O;
+  a.ldo = ldo;
+  a.scale_log2 = softmax_scale * 1.4426950408889634f;
+  a.part = static_cast<float*>(workspace);
+  a.part_stat = a.part + part_rows * a.kv.d;
+  LRQAT_LAUNCH("kv_attn", a.splits > 1 ? 2 : 1, stream, launch_kv_attn(a, stream), "cache attention launch");
+  return LRQAT_OK;
+}
+
 int lrqat_get_gemm_variant(void) { return g_gemm_variant.load(std::memory_order_relaxed); }
 int lrqat_get_lowrank_path(void) { return g_lowrank_path.load(std::memory_order_relaxed); }
 int lrqat_get_dw_schedule(void) { return g_dw_schedule.load(std::memory_order_relaxed); }
@@ -1245,6 +1468,8 @@ int lrqat_get_device_status(lrqat_stream_t stream) {
   LRQAT_CUDA(cudaMemcpy(&h, dev->status, sizeof(int), cudaMemcpyDeviceToHost), "read device status");
   if (h != 0) {
     LRQAT_CUDA(cudaMemset(dev->status, 0, sizeof(int)), "clear device status");
+    if ((h & ~kStatusRange) == 0)
+      return fail(LRQAT_ERR_RANGE, "a batch's rows, lengths or block table contradicted its bounds");
     return fail(LRQAT_ERR_TIMEOUT, "a kernel's bounded wait gave up (status word 0x%x)", h);
   }
   return LRQAT_OK;

@@ -1,0 +1,98 @@
+// Device helpers shared by the norm, 8-bit cache and cache attention kernels.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "serve.h"
+
+namespace lrqat {
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
+  x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
+  x[4] = bf16_lo(v.z), x[5] = bf16_hi(v.z), x[6] = bf16_lo(v.w), x[7] = bf16_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+  return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+// 1.5 * 2^23: adding it to |y| < 2^22 rounds y to the nearest integer (ties to even) and
+// leaves that integer, in two's complement, in the low bits of the sum.
+constexpr float kRoundMagic = 12582912.0f;
+
+// round(fl32(x / s)) of 8 values as floats (values and scales for which |x / s| < 2^10), and
+// as int8 codes.  y = x r with r = fl32(1 / s) and fl32(x / s) both lie within 2^-22 |y| of x / s,
+// below 2^-12: where y is more than 2^-11 away from a half-integer both round to the same
+// integer; otherwise, and where r is infinite or a value is not a number, the division decides.
+__device__ __forceinline__ void round_div8(const float (&x)[8], float s, float r, float (&q)[8]) {
+  bool far = true;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    q[e] = __fmaf_rn(x[e], r, kRoundMagic) - kRoundMagic;
+    far = far && fabsf(__fmaf_rn(x[e], r, -q[e])) < 0.49951171875f;
+  }
+  if (!far) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = rintf(__fdiv_rn(x[e], s));
+  }
+}
+// The low bytes of 8 whole numbers in [-128, 127] (of anything else, some byte).
+__device__ __forceinline__ uint2 pack_codes8(const float (&q)[8]) {
+  uint32_t b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(q[e] + kRoundMagic);
+  return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+}
+// Four int8 codes as floats: 2^23 + (c + 128) has the byte c + 128 as its low mantissa bits.
+__device__ __forceinline__ void codes4(uint32_t w, float (&c)[4]) {
+  const uint32_t u = w ^ 0x80808080u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    c[e] = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540 + e)) - 8388736.0f;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The rows of sequence b: `n` rows from row `row0` of the batch, at positions first .. len - 1.
+// Negative positions belong to padding rows.  False (and the range bit of the status word) where
+// the arrays contradict the batch's bounds.
+struct SeqRows {
+  int64_t row0;
+  int n, len, first;
+};
+__device__ __forceinline__ bool seq_rows(const KvArgs& a, int b, SeqRows& s) {
+  const int64_t r0 = a.row_start[b], r1 = a.row_start[b + 1];
+  const int len = a.len[b];
+  s.row0 = r0;
+  s.n = static_cast<int>(r1 - r0);
+  s.len = len;
+  s.first = len - s.n;
+  if (r0 < 0 || r1 < r0 || r1 > a.rows || r1 - r0 > a.max_rows || len < 0 || len > a.max_len) {
+    if (threadIdx.x == 0) atomicOr(a.status, kStatusRange);
+    return false;
+  }
+  return true;
+}
+// The cache block that holds position `pos` of sequence b, or -1 (and the range bit).
+__device__ __forceinline__ int seq_block(const KvArgs& a, int b, int pos) {
+  const int blk = __ldg(a.table + static_cast<int64_t>(b) * a.max_blocks + (pos >> a.block_log2));
+  if (static_cast<uint32_t>(blk) >= static_cast<uint64_t>(a.n_blocks)) {
+    atomicOr(a.status, kStatusRange);
+    return -1;
+  }
+  return blk;
+}
+
+}  // namespace lrqat

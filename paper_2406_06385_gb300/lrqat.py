@@ -22,7 +22,7 @@ PHI_FP8_E4M3 = 4
 PHI_FP8_E5M2 = 5
 
 STATUS = {0: "LRQAT_OK", -1: "LRQAT_ERR_INVALID_ARG", -2: "LRQAT_ERR_UNSUPPORTED", -3: "LRQAT_ERR_ALIGNMENT",
-          -4: "LRQAT_ERR_WORKSPACE", -5: "LRQAT_ERR_CUDA", -6: "LRQAT_ERR_TIMEOUT"}
+          -4: "LRQAT_ERR_WORKSPACE", -5: "LRQAT_ERR_CUDA", -6: "LRQAT_ERR_TIMEOUT", -7: "LRQAT_ERR_RANGE"}
 
 
 class LrqatError(RuntimeError):
@@ -62,6 +62,50 @@ class AdamWState(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("A32", "B32", "mA", "vA", "mB", "vB", "ms", "vs")]
 
 
+class Norm(ctypes.Structure):
+    """Mirror of lrqat_norm."""
+    _fields_ = [("k", ctypes.c_int64), ("eps", ctypes.c_float), ("act_bits", ctypes.c_int32)]
+
+
+class KVCache(ctypes.Structure):
+    """Mirror of lrqat_kv_cache."""
+    _fields_ = [("n_blocks", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+    @classmethod
+    def of(cls, k_codes, v_codes, k_scale, v_scale) -> "KVCache":
+        """`k_codes`, `v_codes`: int8 [n_blocks, n_kv_heads, block, head_dim]; `k_scale`, `v_scale`: fp32
+        [n_blocks, n_kv_heads]; all dense.  The cache keeps the tensors alive."""
+        for t, shape in ((k_codes, k_codes.shape), (v_codes, k_codes.shape), (k_scale, k_codes.shape[:2]),
+                         (v_scale, k_codes.shape[:2])):
+            if t.shape != shape or not t.is_contiguous():
+                raise LrqatError(-1, "cache tensors must be dense and of matching shapes")
+        n_blocks, heads, block, d = k_codes.shape
+        cache = cls(n_blocks, heads, d, block, _ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale))
+        cache.tensors = (k_codes, v_codes, k_scale, v_scale)
+        return cache
+
+
+class KVBatch(ctypes.Structure):
+    """Mirror of lrqat_kv_batch."""
+    _fields_ = [("n_seqs", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("len", ctypes.c_void_p),
+                ("row_start", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("max_rows", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+    @classmethod
+    def of(cls, lens, row_start, block_table, rows: int, max_rows: int, max_len: int) -> "KVBatch":
+        """`lens` int32 [n_seqs], `row_start` int32 [n_seqs + 1], `block_table` int32 [n_seqs, max_blocks], all
+        dense device tensors, which the batch keeps alive; `rows`, `max_rows`, `max_len`: the host's bounds."""
+        n_seqs, max_blocks = block_table.shape
+        if (lens.shape != (n_seqs,) or row_start.shape != (n_seqs + 1,)
+                or not (lens.is_contiguous() and row_start.is_contiguous() and block_table.is_contiguous())):
+            raise LrqatError(-1, "lens, row_start and block_table must be dense, of n_seqs, n_seqs + 1 and n_seqs rows")
+        batch = cls(n_seqs, max_blocks, _ptr(lens), _ptr(row_start), _ptr(block_table), rows, max_rows, max_len)
+        batch.tensors = (lens, row_start, block_table)
+        return batch
+
+
 _lib = None
 
 
@@ -92,6 +136,16 @@ def lib() -> ctypes.CDLL:
             "lrqat_adamw_step": [lp, ctypes.POINTER(AdamW), vp, vp, vp, vp, ctypes.POINTER(AdamWState), vp, vp, vp,
                                  vp],
         }
+        np_, cp, bp = ctypes.POINTER(Norm), ctypes.POINTER(KVCache), ctypes.POINTER(KVBatch)
+        i32, f32 = ctypes.c_int32, ctypes.c_float
+        sigs.update({
+            "lrqat_add_rmsnorm_fwd": [np_, i64, vp, vp, vp, vp, vp, vp, vp, vp],
+            "lrqat_add_rmsnorm_bwd": [np_, i64, vp, vp, vp, vp, vp, vp, ip, vp, sz, vp],
+            "lrqat_act_dequant": [np_, i64, vp, vp, vp, vp],
+            "lrqat_kv_write": [cp, bp, vp, i64, vp, i64, vp],
+            "lrqat_kv_read": [cp, bp, vp, i64, vp, i64, vp],
+            "lrqat_kv_attn": [cp, bp, i32, f32, i32, vp, i64, vp, i64, vp, sz, vp],
+        })
         for name, args in sigs.items():
             fn = getattr(L, name)
             fn.argtypes = args
@@ -114,6 +168,10 @@ def lib() -> ctypes.CDLL:
             fn = getattr(L, name)
             fn.argtypes = [lp, i64]
             fn.restype = ctypes.c_size_t
+        L.lrqat_add_rmsnorm_bwd_workspace_bytes.argtypes = [np_, i64]
+        L.lrqat_add_rmsnorm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.lrqat_kv_attn_workspace_bytes.argtypes = [cp, bp, i32, i32]
+        L.lrqat_kv_attn_workspace_bytes.restype = ctypes.c_size_t
         _lib = L
     return _lib
 
@@ -130,8 +188,8 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    import torch
-    return torch.cuda.current_stream().cuda_stream
+    from torch import _C
+    return _C._cuda_getCurrentRawStream(_C._cuda_getDevice())   # a tenth of torch.cuda.current_stream()'s time
 
 
 def last_error() -> str:
@@ -216,6 +274,66 @@ def adamw_step(layer: Layer, opt: AdamW, sqnorm, dA, dB, ds, state: dict, s, A, 
     st = AdamWState(*[_ptr(state[n]) for n, _ in AdamWState._fields_])
     _check(lib().lrqat_adamw_step(ctypes.byref(layer), ctypes.byref(opt), _ptr(sqnorm), _ptr(dA), _ptr(dB), _ptr(ds),
                                   ctypes.byref(st), _ptr(s), _ptr(A), _ptr(B), _stream(stream)))
+
+
+def add_rmsnorm_fwd(norm: Norm, T: int, X, R, gamma, H, Y, Y_q, s_y, stream=None) -> None:
+    """h = X + R (R and H may be None), y = gamma h / rms(h).  act_bits 0: Y = bf16(y); act_bits 8: per-token
+    codes Y_q with scales s_y and / or their values Y (the X_q of linear_fwd_quantized)."""
+    _check(lib().lrqat_add_rmsnorm_fwd(ctypes.byref(norm), T, _ptr(X), _ptr(R), _ptr(gamma), _ptr(H), _ptr(Y),
+                                       _ptr(Y_q), _ptr(s_y), _stream(stream)))
+
+
+def add_rmsnorm_bwd_workspace_bytes(norm: Norm, T: int) -> int:
+    return int(lib().lrqat_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(norm), T))
+
+
+def add_rmsnorm_bwd(norm: Norm, T: int, dY, dH, H, gamma, dX, dgamma, accumulate: bool, workspace,
+                    stream=None) -> None:
+    """Gradient of add_rmsnorm_fwd at the residual stream H (dH and dgamma may be None; without dgamma the
+    workspace may be None)."""
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(lib().lrqat_add_rmsnorm_bwd(ctypes.byref(norm), T, _ptr(dY), _ptr(dH), _ptr(H), _ptr(gamma), _ptr(dX),
+                                       _ptr(dgamma), 1 if accumulate else 0, _ptr(workspace), nbytes,
+                                       _stream(stream)))
+
+
+def act_dequant(norm: Norm, T: int, codes, s, X_hat, stream=None) -> None:
+    """X_hat = bf16(s codes): the values of activations kept as 8-bit codes and per-token scales."""
+    _check(lib().lrqat_act_dequant(ctypes.byref(norm), T, _ptr(codes), _ptr(s), _ptr(X_hat), _stream(stream)))
+
+
+def _rows(t, heads: int, d: int) -> int:
+    """Distance in elements of consecutive rows of a [rows, heads, head_dim] tensor or view."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise LrqatError(-1, f"rows of {heads} heads by {d} expected, dense within a row")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+
+
+def kv_write(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:
+    """Quantizes the batch's new keys and values, bf16 [rows, n_kv_heads, head_dim], into the cache."""
+    h, d = cache.n_kv_heads, cache.head_dim
+    _check(lib().lrqat_kv_write(ctypes.byref(cache), ctypes.byref(batch), _ptr(K), _rows(K, h, d), _ptr(V),
+                                _rows(V, h, d), _stream(stream)))
+
+
+def kv_read(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:
+    """Reads the batch's rows back into K and V, bf16 [rows, n_kv_heads, head_dim]."""
+    h, d = cache.n_kv_heads, cache.head_dim
+    _check(lib().lrqat_kv_read(ctypes.byref(cache), ctypes.byref(batch), _ptr(K), _rows(K, h, d), _ptr(V),
+                               _rows(V, h, d), _stream(stream)))
+
+
+def kv_attn_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window: int = 0) -> int:
+    return int(lib().lrqat_kv_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, window))
+
+
+def kv_attn(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, O, workspace, stream=None) -> None:
+    """Causal attention of the batch's rows Q over the cache into O, both bf16 [rows, n_heads, head_dim]."""
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    heads, d = Q.shape[1] if Q.dim() == 3 else 0, cache.head_dim
+    _check(lib().lrqat_kv_attn(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, _ptr(Q),
+                               _rows(Q, heads, d), _ptr(O), _rows(O, heads, d), _ptr(workspace), nbytes,
+                               _stream(stream)))
 
 
 def get_device_status(stream=None) -> None:

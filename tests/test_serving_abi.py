@@ -1,0 +1,126 @@
+"""The norm, cache and attention entry points reject bad arguments on the host before any CUDA work."""
+import ctypes
+
+import pytest
+
+from paper_2406_06385_gb300 import lrqat as LQ
+from paper_2406_06385_gb300.build import build
+
+OK = 16   # a 16-byte aligned address that is never followed
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build()
+    return LQ.lib()
+
+
+def _norm(**kw):
+    return LQ.Norm(**dict(dict(k=256, eps=1e-5, act_bits=8), **kw))
+
+
+def _fwd(lib, norm, T=4, X=OK, R=OK, gamma=OK, H=OK, Y=OK, Y_q=OK, s=OK):
+    return lib.lrqat_add_rmsnorm_fwd(ctypes.byref(norm), T, X, R, gamma, H, Y, Y_q, s, None)
+
+
+@pytest.mark.parametrize("kw,status", [(dict(k=0), -1), (dict(k=12), -2), (dict(k=16392), -2), (dict(eps=-1.0), -1),
+                                       (dict(eps=float("nan")), -1), (dict(act_bits=4), -2)])
+def test_norm_settings(lib, kw, status):
+    assert _fwd(lib, _norm(**kw)) == status and LQ.last_error()
+    assert lib.lrqat_act_dequant(ctypes.byref(_norm(**kw)), 4, OK, OK, OK, None) == status
+    assert lib.lrqat_add_rmsnorm_bwd(ctypes.byref(_norm(**kw)), 4, OK, OK, OK, OK, OK, None, 0, None, 0, None) == status
+    assert lib.lrqat_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(_norm(**kw)), 4) == 0
+
+
+def test_norm_pointers(lib):
+    n = _norm()
+    assert _fwd(lib, n, T=0) == -1
+    for name in ("X", "gamma", "H"):
+        assert _fwd(lib, n, **{name: None}) == -1, name
+    for name in ("X", "R", "gamma", "H", "Y", "Y_q", "s"):
+        assert _fwd(lib, n, **{name: 24}) == -3, name
+    assert _fwd(lib, n, Y=None, Y_q=None) == -1
+    assert _fwd(lib, n, s=None) == -1
+    assert _fwd(lib, _norm(act_bits=0)) == -1                     # codes of an unquantized norm
+    bwd = lambda dgamma, ws, size: lib.lrqat_add_rmsnorm_bwd(  # noqa: E731
+        ctypes.byref(n), 64, OK, None, OK, OK, OK, dgamma, 0, ws, size, None)
+    need = lib.lrqat_add_rmsnorm_bwd_workspace_bytes(ctypes.byref(n), 64)
+    assert need > 0 and bwd(OK, None, need) == -4 and bwd(OK, OK, need - 1) == -4 and bwd(24, OK, need) == -3
+    assert bwd(OK, 24, need) == -3
+    assert lib.lrqat_act_dequant(ctypes.byref(n), 4, OK, None, OK, None) == -1
+
+
+def _cache(**kw):
+    return LQ.KVCache(**dict(dict(n_blocks=8, n_kv_heads=2, head_dim=128, block=16, k_codes=OK, v_codes=OK,
+                                  k_scale=OK, v_scale=OK), **kw))
+
+
+def _batch(**kw):
+    return LQ.KVBatch(**dict(dict(n_seqs=2, max_blocks=4, len=OK, row_start=OK, block_table=OK, rows=6, max_rows=3,
+                                  max_len=64), **kw))
+
+
+def _calls(lib, c, b, x=OK, ld=256, heads=4, ldq=512, scale=1.0, window=0, ws=OK, size=1 << 30):
+    c, b = ctypes.byref(c), ctypes.byref(b)
+    return [lambda: lib.lrqat_kv_write(c, b, x, ld, OK, 256, None), lambda: lib.lrqat_kv_read(c, b, OK, 256, x, ld, None),
+            lambda: lib.lrqat_kv_attn(c, b, heads, scale, window, x, ldq, OK, 512, ws, size, None)]
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_blocks=0), -1), (dict(n_kv_heads=0), -1), (dict(head_dim=96), -2), (dict(block=8), -2), (dict(block=48), -2),
+    (dict(k_codes=None), -1), (dict(v_scale=None), -1), (dict(v_codes=24), -3), (dict(k_scale=8), -3)])
+def test_cache_settings(lib, kw, status):
+    for call in _calls(lib, _cache(**kw), _batch()):
+        assert call() == status and LQ.last_error()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_seqs=0), -1), (dict(n_seqs=65536), -2), (dict(max_blocks=0), -1), (dict(rows=-1), -1), (dict(max_rows=-1), -1),
+    (dict(max_len=-1), -1), (dict(max_len=65), -1), (dict(max_blocks=1 << 28), -2), (dict(len=None), -1),
+    (dict(row_start=None), -1), (dict(block_table=None), -1), (dict(len=18), -3), (dict(rows=1 << 31), -2)])
+def test_batch_settings(lib, kw, status):
+    for call in _calls(lib, _cache(), _batch(**kw)):
+        assert call() == status and LQ.last_error()
+
+
+def test_row_arrays(lib):
+    for call in _calls(lib, _cache(), _batch(), x=None, ldq=512):
+        assert call() == -1
+    for call in _calls(lib, _cache(), _batch(), x=24):
+        assert call() == -3
+    for call in _calls(lib, _cache(), _batch(), ld=248, ldq=504):
+        assert call() == -1                                       # rows closer together than a row is long
+    for call in _calls(lib, _cache(), _batch(), ld=257, ldq=513):
+        assert call() == -3
+    # a batch without rows is no work
+    for call in _calls(lib, _cache(), _batch(rows=0)):
+        assert call() == 0
+
+
+def test_attention_settings(lib):
+    attn = lambda c=None, b=None, **kw: _calls(lib, c or _cache(), b or _batch(), **kw)[2]()  # noqa: E731
+    assert attn(heads=0) == -1 and attn(heads=3) == -1
+    assert attn(window=-1) == -1
+    assert attn(scale=float("inf")) == -1 and attn(scale=float("nan")) == -1
+    long = _batch(max_blocks=4096, max_len=65536)
+    need = lib.lrqat_kv_attn_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(long), 4, 0)
+    assert need > 0
+    assert attn(b=long, ws=None, size=need) == -4 and attn(b=long, size=need - 1) == -4
+    assert attn(b=long, ws=24, size=need) == -3
+    assert lib.lrqat_kv_attn_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(long), 3, 0) == 0
+
+
+def test_binding_checks_tensor_layouts():
+    torch = pytest.importorskip("torch")
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.int8)
+    s = torch.zeros(4, 2)
+    assert LQ.KVCache.of(k, k, s, s).block == 16
+    for bad in ((k, k[:3], s, s), (k, k, s[:, :1], s), (k.transpose(1, 2), k, s, s)):
+        with pytest.raises(LQ.LrqatError):
+            LQ.KVCache.of(*bad)
+    n, t = torch.zeros(3, dtype=torch.int32), torch.zeros(3, 5, dtype=torch.int32)
+    with pytest.raises(LQ.LrqatError):
+        LQ.KVBatch.of(n, n, t, 3, 1, 16)
+    with pytest.raises(LQ.LrqatError):
+        LQ._rows(torch.zeros(3, 2, 64).transpose(0, 1), 3, 64)
+    assert LQ._rows(torch.zeros(3, 6, 64)[:, :2], 2, 64) == 384
