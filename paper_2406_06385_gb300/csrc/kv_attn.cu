@@ -14,20 +14,29 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "kernels.h"
 #include "serve.cuh"
 
 namespace lrqat {
 namespace {
 
-constexpr int kRows = 16;          // (token, head) rows of one tile: the M of mma.m16n8k16
 constexpr int kWarps = 4;
-constexpr int kStep = 16;          // keys of one step of a warp
+constexpr int kStep = 32;          // keys of one step of a warp, in two halves of 16
+constexpr int kStages = 2;
+constexpr int kWantPerSm = 12;     // thread blocks per SM that the keys are cut into
 
-__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          const uint32_t (&b)[2]) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
+}
+// Transposes an 8 x 8 matrix of halves whose row l / 4 lane l holds at columns 2 (l % 4), + 1.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   uint32_t r;
@@ -42,7 +51,11 @@ __device__ __forceinline__ uint32_t half_codes(uint32_t biased) {
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(0x64806480u));   // 1024 + 128
   return r;
 }
-
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 // 2^up / l, 0 for a row that saw no key (l = 0); up = m - n is at most log2 of the largest scale.
 __device__ __forceinline__ float out_factor(float l, float up) {
@@ -50,21 +63,22 @@ __device__ __forceinline__ float out_factor(float l, float up) {
   return l == 0.0f ? 0.0f : half / l * half;
 }
 
-// The tile of kRows rows `rt` of (sequence, key/value head): row i is token (16 rt + i) / group of
-// the sequence's rows and query head (16 rt + i) % group of the head's group.
+// The tile of `tile_rows` rows `rt` of (sequence, key/value head): row i is token
+// (tile_rows rt + i) / group of the sequence's rows and query head (tile_rows rt + i) % group of the
+// head's group.
 struct Tile {
   SeqRows seq;
   int rows;            // rows of the sequence and head, all tiles
   int r0;              // first row of this tile
   int pos_lo, pos_hi;  // positions of the tile's first and last row
-  int lo, hi;          // keys [lo, hi) that some row may see; lo a multiple of 16
+  int lo, hi;          // keys [lo, hi) that some row may see; lo a multiple of a step
 };
 __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile& t) {
   if (!seq_rows(a.kv, b, t.seq)) return false;
   t.rows = t.seq.n * a.group;
-  t.r0 = rt * kRows;
+  t.r0 = rt * a.tile_rows;
   if (t.r0 >= t.rows) return false;
-  const int last = min(t.r0 + kRows, t.rows) - 1;
+  const int last = min(t.r0 + a.tile_rows, t.rows) - 1;
   t.pos_lo = t.seq.first + t.r0 / a.group;
   t.pos_hi = t.seq.first + last / a.group;
   t.hi = max(t.pos_hi + 1, 0);
@@ -76,13 +90,64 @@ __device__ __forceinline__ int tile_splits(const AttnArgs& a, const Tile& t) {
   return t.hi > t.lo ? (t.hi - t.lo + a.chunk - 1) / a.chunk : 0;
 }
 
-// One thread block per (split, head and row tile, sequence).  A warp takes every fourth step of 16
-// keys and keeps its own maximum, sum and outputs; the warps join at the end.  Keys and values go
-// from global memory straight into the fragments of the matrix instructions: the order of the
-// head's dimensions inside a product is free, so each lane takes 16 consecutive bytes of a token.
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+
+// Where 16-byte piece q of token r (of 16) lies in a warp's shared memory, so that copying whole
+// tokens and the lanes' reads below are free of bank conflicts.
 template <int D>
-__global__ void __launch_bounds__(32 * kWarps) kv_attn_split_kernel(AttnArgs a) {
+__device__ __forceinline__ uint32_t key_place(uint32_t r, uint32_t q) {
+  return D == 128 ? r * 128 + (q ^ (r & 1) << 2) * 16 : r * 64 + q * 16;
+}
+template <int D>
+__device__ __forceinline__ uint32_t value_place(uint32_t r, uint32_t q) {
+  return D == 128 ? r * 128 + (q ^ (r & 6)) * 16 : (r ^ (r >> 2 & 1)) * 64 + (q ^ (r & 2)) * 16;
+}
+
+template <int D, int NT>
+struct SplitSmem {
+  static constexpr int kHalf = 16 * D;                                      // bytes of 16 keys
+  static constexpr int kWarpStage = 4 * kHalf;                              // keys, keys, values, values
+  static constexpr int kRing = kStages * kWarps * kWarpStage;
+  static constexpr int kOut = kWarps * 8 * NT * (D + 4) * 4;                // the join's outputs reuse the ring
+  static constexpr int kScales = kRing > kOut ? kRing : kOut;
+  static constexpr int kBytes = kScales + kStages * kWarps * 16;
+};
+
+// One thread block per (split, head and row tile, sequence); a tile has 8 NT (token, head) rows. A warp
+// takes every fourth step of 32 keys and keeps its own maxima, sum and outputs; the warps join at the
+// end.  Keys are the M of the first product (scores = K q^T) and the head's dimensions that of the
+// second (o^T = V^T P^T), so a tile of 8 rows wastes no tensor work and few registers, and one 8 x 8
+// transpose per 8 keys turns scores into the second product's operand.  The order of the dimensions
+// inside a product is free: each lane takes 16 consecutive bytes of a token.  A step's codes come
+// through a ring in shared memory, one step ahead, filled by the warp that reads it: warps never
+// wait for one another.
+template <int D, int NT>
+__global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_attn_split_kernel(AttnArgs a) {
+  using Sm = SplitSmem<D, NT>;
   constexpr int kC = D / 64;         // 64-dimension pieces of a token
+  constexpr int kRows = 8 * NT;
+  extern __shared__ __align__(16) uint8_t smem[];
   const int split = blockIdx.x, h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   Tile t;
@@ -91,20 +156,64 @@ __global__ void __launch_bounds__(32 * kWarps) kv_attn_split_kernel(AttnArgs a) 
   if (split > 0 && split >= ns) return;
   const int k0 = t.lo + split * a.chunk, k1 = min(t.hi, k0 + a.chunk);
 
-  // rows g and g + 8 of the tile: fragments of q, its power of two, positions
-  uint32_t qf[4 * kC][4];
-  float qs[2];
-  int pos[2];
+  const uint32_t ring = smem_addr(smem) + warp * Sm::kWarpStage;
+  const uint32_t scales = smem_addr(smem) + Sm::kScales + warp * 16;
+  constexpr uint32_t kStageBytes = kWarps * Sm::kWarpStage, kStageScales = kWarps * 16;
+  const int first_key = k0 + kStep * warp;
+  const int steps = first_key < k1 ? (k1 - first_key + kStep * kWarps - 1) / (kStep * kWarps) : 0;
+  const int32_t* table = a.kv.table + static_cast<int64_t>(b) * a.kv.max_blocks;
+  const uint32_t in_block = (1u << a.kv.block_log2) - 1;
+  // 16 keys from `key` on; the second half of a step may lie past the tile's keys, and then past the table
+  auto block_of = [&](int key) { return key < k1 ? __ldg(table + (key >> a.kv.block_log2)) : -2; };
+  int next_blk[2] = {block_of(first_key), block_of(first_key + 16)};
+  uint32_t skipped = 0;              // bit 2 s + u: half u of the step in stage s has no valid block
+  const uint32_t piece = lane % (D / 16), tok = lane / (D / 16);            // a copy instruction covers 512 / D tokens
+  auto issue = [&](int i) {
+    if (i < steps) {
+      const int key = first_key + i * kStep * kWarps, stage = i % kStages;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = t.r0 + g + 8 * i;
-    const int tok = r / a.group;
+      for (int u = 0; u < 2; ++u) {
+        const int blk = next_blk[u];
+        next_blk[u] = block_of(key + kStep * kWarps + 16 * u);
+        const uint32_t bit = 1u << (2 * stage + u);
+        if (static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks)) {
+          skipped &= ~bit;
+          const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
+          const int64_t off = ((at << a.kv.block_log2) + ((key + 16 * u) & in_block)) * D + lane * 16;
+          const int8_t* kp = a.kv.codes[0] + off;
+          const int8_t* vp = a.kv.codes[1] + off;
+          const uint32_t dst = ring + stage * kStageBytes + u * Sm::kHalf;
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            copy_async16(dst + key_place<D>(512 / D * j + tok, piece), kp + 512 * j);
+            copy_async16(dst + 2 * Sm::kHalf + value_place<D>(512 / D * j + tok, piece), vp + 512 * j);
+          }
+          if (lane < 2)
+            copy_async4(scales + stage * kStageScales + u * 8 + lane * 4, (lane ? a.kv.scale[1] : a.kv.scale[0]) + at);
+        } else {
+          skipped |= bit;
+          if (lane == 0 && blk != -2) atomicOr(a.kv.status, kStatusRange);
+        }
+      }
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) issue(i);
+
+  // row g of each 8: its operand fragments; rows 2 t4, + 1: power of two and position
+  uint32_t qf[NT][4 * kC][2];
+  float qs[NT][2];
+  int pos[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = t.r0 + 8 * nt + g;
+    const int tk = r / a.group;
     const bool in = r < t.rows;
-    pos[i] = in ? t.seq.first + tok : -1;
-    const uint16_t* q = a.Q + (t.seq.row0 + tok) * a.ldq + static_cast<int64_t>(h * a.group + r % a.group) * D;
+    const uint16_t* q = a.Q + (t.seq.row0 + tk) * a.ldq + static_cast<int64_t>(h * a.group + r % a.group) * D;
     float x[kC][16], top = 0.0f;
 #pragma unroll
-    for (int c = 0; c < kC; ++c) {
+    for (int c = 0; c < kC; ++c)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         float v[8];
@@ -115,157 +224,188 @@ __global__ void __launch_bounds__(32 * kWarps) kv_attn_split_kernel(AttnArgs a) 
           top = fmaxf(top, fabsf(v[e]));
         }
       }
-    }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const uint32_t e = min(max(__float_as_uint(top) >> 23, 1u), 253u);   // exponent of a normal power of two
-    qs[i] = __uint_as_float(e << 23);
     const float inv = __uint_as_float((254u - e) << 23);
 #pragma unroll
     for (int c = 0; c < kC; ++c)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        qf[4 * c + u][i] = pack_half(x[c][4 * u] * inv, x[c][4 * u + 1] * inv);
-        qf[4 * c + u][2 + i] = pack_half(x[c][4 * u + 2] * inv, x[c][4 * u + 3] * inv);
-      }
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          qf[nt][4 * c + u][k] = pack_half(x[c][4 * u + 2 * k] * inv, x[c][4 * u + 2 * k + 1] * inv);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      qs[nt][j] = __shfl_sync(0xffffffffu, __uint_as_float(e << 23), 4 * (2 * t4 + j));
+      const int rr = t.r0 + 8 * nt + 2 * t4 + j;
+      pos[nt][j] = rr < t.rows ? t.seq.first + rr / a.group : -1;
+    }
   }
 
-  float acc[D / 8][4];
+  float acc[NT][D / 16][4];
 #pragma unroll
-  for (int j = 0; j < D / 8; ++j)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
-  float m[2] = {-INFINITY, -INFINITY}, n[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+    for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[nt][j][e] = 0.0f;
+  // per row: the running maximum m; per row and lane (its own keys): the maximum n and the sum
+  float m[NT][2], n[NT][2], l[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) m[nt][j] = n[nt][j] = -INFINITY, l[nt][j] = 0.0f;
 
-  for (int key = k0 + kStep * warp; key < k1; key += kStep * kWarps) {
-    const int blk = seq_block(a.kv, b, key);
-    if (blk < 0) continue;
-    const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
-    const int64_t off = ((at << a.kv.block_log2) + (key & ((1 << a.kv.block_log2) - 1))) * D;
-    const int8_t* kp = a.kv.codes[0] + off + g * D + 16 * t4;
-    const int8_t* vp = a.kv.codes[1] + off + 2 * t4 * D + g * (D / 8);
-    uint4 kw[2][kC];
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int c = 0; c < kC; ++c) kw[hf][c] = __ldg(reinterpret_cast<const uint4*>(kp + 8 * hf * D + 64 * c));
-    uint32_t vw[4][D / 32];            // tokens 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-    for (int tk = 0; tk < 4; ++tk) {
-      const int8_t* p = vp + ((tk & 1) + 8 * (tk >> 1)) * D;
-      if constexpr (D == 128) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
-        vw[tk][0] = w.x, vw[tk][1] = w.y, vw[tk][2] = w.z, vw[tk][3] = w.w;
-      } else {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(p));
-        vw[tk][0] = w.x, vw[tk][1] = w.y;
-      }
-    }
-    const float sk = __ldg(a.kv.scale[0] + at), sv = __ldg(a.kv.scale[1] + at);
+  for (int i = 0; i < steps; ++i) {
+    copy_wait<kStages - 2>();
+    __syncwarp();                    // every lane's copies of this step are here; the last step has been read
+    issue(i + kStages - 1);
+    const int key = first_key + i * kStep * kWarps, stage = i % kStages;
+    const uint32_t src = ring + stage * kStageBytes;
+    const uint32_t skip = skipped >> (2 * stage) & 3u;
 
-    float s[2][4] = {};
+    float s[2][NT][4] = {};          // keys g, g + 8 of a half by rows 2 t4, + 1
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
-        const uint32_t w[4] = {kw[hf][c].x, kw[hf][c].y, kw[hf][c].z, kw[hf][c].w};
+        const uint4 w0 = lds128(src + u * Sm::kHalf + key_place<D>(g, 4 * c + t4));
+        const uint4 w1 = lds128(src + u * Sm::kHalf + key_place<D>(g + 8, 4 * c + t4));
+        const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t x = w[u] ^ 0x80808080u;
-          mma_16816(s[hf], qf[4 * c + u], half_codes<0x4140>(x), half_codes<0x4342>(x));
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t y0 = x0[k] ^ 0x80808080u, y1 = x1[k] ^ 0x80808080u;
+          const uint32_t a0 = half_codes<0x4140>(y0), a2 = half_codes<0x4342>(y0);
+          const uint32_t a1 = half_codes<0x4140>(y1), a3 = half_codes<0x4342>(y1);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_16816(s[u][nt], a0, a1, a2, a3, qf[nt][4 * c + k]);
         }
       }
 
-    const float coef = a.scale_log2 * sk, lsv = log2f(sv);
-    const bool all = key + kStep - 1 <= t.pos_lo && (a.window == 0 || key > t.pos_hi - a.window);
-    uint32_t p[4];
-    float alpha[2];
+    const uint4 sc = lds128(scales + stage * kStageScales);
+    const float coef[2] = {a.scale_log2 * __uint_as_float(sc.x), a.scale_log2 * __uint_as_float(sc.z)};
+    const float lsv[2] = {lg2(__uint_as_float(sc.y)), lg2(__uint_as_float(sc.w))};
+    const bool all = skip == 0 && key + kStep - 1 <= t.pos_lo && (a.window == 0 || key > t.pos_hi - a.window);
+    uint32_t p[2][NT][2];
+    float alpha[NT][2];
     bool moved = false;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float ci = coef * qs[i];
-      float mx = -INFINITY;
+    for (int nt = 0; nt < NT; ++nt) {
+      float P[2][4];
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+      for (int j = 0; j < 2; ++j) {
+        float z[2][2], x[2][2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float& x = s[hf][2 * i + e];
-          x = fmaf(x, ci, lsv);
-          if (!all) {
-            const int j = key + 8 * hf + 2 * t4 + e;
-            if (j > pos[i] || (a.window > 0 && j <= pos[i] - a.window)) x = -INFINITY;
+        for (int u = 0; u < 2; ++u) {
+          const float cu = coef[u] * qs[nt][j];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            z[u][e] = s[u][nt][2 * e + j] * cu;
+            x[u][e] = z[u][e] + lsv[u];
           }
-          mx = fmaxf(mx, x);
         }
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float m1 = fmaxf(m[i], mx), n1 = fmaxf(n[i], mx - lsv);
-      const float base = finite_max(m1), nbase = finite_max(n1);
-      alpha[i] = ex2(m[i] - base);
-      moved = moved || m1 != m[i];
-      float sum = 0.0f;
+        if (!all) {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const float p0 = ex2(s[hf][2 * i] - base), p1 = ex2(s[hf][2 * i + 1] - base);
-        p[2 * hf + i] = pack_half(p0, p1);
-        sum += p0 + p1;
-      }
-      // the step's part of the denominator, relative to 2^n1: its largest P is 2^{mx - m1}, so a step that
-      // contributes next to nothing to o, for its tiny scale, sums its terms relative to its own maximum
-      float to = base - lsv - nbase;
-      if (mx - base < -64.0f && mx > -INFINITY) {
-        sum = 0.0f;
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) sum += ex2(s[hf][2 * i] - mx) + ex2(s[hf][2 * i + 1] - mx);
-        to = mx - lsv - nbase;
+            for (int e = 0; e < 2; ++e) {
+              const int k = key + 16 * u + 8 * e + g;
+              if (k > pos[nt][j] || (a.window > 0 && k <= pos[nt][j] - a.window) || (skip >> u & 1))
+                z[u][e] = x[u][e] = -INFINITY;
+            }
+        }
+        float mx = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        const float m1 = fmaxf(m[nt][j], mx), base = finite_max(m1);
+        const float n1 = fmaxf(fmaxf(n[nt][j], fmaxf(z[0][0], z[0][1])), fmaxf(z[1][0], z[1][1]));
+        const float nbase = finite_max(n1);
+        alpha[nt][j] = ex2(m[nt][j] - base);
+        moved = moved || m1 != m[nt][j];
+        float sum = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            P[u][2 * e + j] = ex2(x[u][e] - base);
+            sum += ex2(z[u][e] - nbase);
+          }
+        l[nt][j] = fmaf(l[nt][j], ex2(n[nt][j] - nbase), sum);
+        m[nt][j] = m1;
+        n[nt][j] = n1;
       }
-      // a hidden block adds nothing, whatever its scale
-      l[i] = fmaf(l[i], ex2(n[i] - nbase), sum == 0.0f ? 0.0f : sum * ex2(to));
-      m[i] = m1;
-      n[i] = n1;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) p[u][nt][e] = transpose8(pack_half(P[u][2 * e], P[u][2 * e + 1]));
     }
     if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-      for (int j = 0; j < D / 8; ++j)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j][e] *= alpha[e >> 1];
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[nt][j][e] *= alpha[nt][e & 1];
     }
-    // a fragment of P: rows g, g + 8 by keys 2t, 2t + 1 and 2t + 8, 2t + 9
-    const uint32_t pa[4] = {p[0], p[1], p[2], p[3]};
 #pragma unroll
-    for (int w = 0; w < D / 32; ++w) {
-      const uint32_t x0 = vw[0][w] ^ 0x80808080u, x1 = vw[1][w] ^ 0x80808080u;
-      const uint32_t x2 = vw[2][w] ^ 0x80808080u, x3 = vw[3][w] ^ 0x80808080u;
-      const uint32_t lo0 = __byte_perm(x0, x1, 0x5140), hi0 = __byte_perm(x0, x1, 0x7362);
-      const uint32_t lo1 = __byte_perm(x2, x3, 0x5140), hi1 = __byte_perm(x2, x3, 0x7362);
-      mma_16816(acc[4 * w], pa, half_codes<0x4140>(lo0), half_codes<0x4140>(lo1));
-      mma_16816(acc[4 * w + 1], pa, half_codes<0x4342>(lo0), half_codes<0x4342>(lo1));
-      mma_16816(acc[4 * w + 2], pa, half_codes<0x4140>(hi0), half_codes<0x4140>(hi1));
-      mma_16816(acc[4 * w + 3], pa, half_codes<0x4342>(hi0), half_codes<0x4342>(hi1));
+    for (int u = 0; u < 2; ++u) {
+      uint32_t vw[4][D / 32];        // tokens 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9, dimensions g D/8 ..
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t r = 2 * t4 + (k & 1) + 8 * (k >> 1), at = src + (2 + u) * Sm::kHalf;
+        if constexpr (D == 128) {
+          const uint4 w = lds128(at + value_place<D>(r, g));
+          vw[k][0] = w.x ^ 0x80808080u, vw[k][1] = w.y ^ 0x80808080u;
+          vw[k][2] = w.z ^ 0x80808080u, vw[k][3] = w.w ^ 0x80808080u;
+        } else {
+          const uint2 w = lds64(at + value_place<D>(r, g >> 1) + (g & 1) * 8);
+          vw[k][0] = w.x ^ 0x80808080u, vw[k][1] = w.y ^ 0x80808080u;
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) {
+        const uint32_t lo0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), hi0 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+        const uint32_t lo1 = __byte_perm(vw[2][w], vw[3][w], 0x5140), hi1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+        const uint32_t a0 = half_codes<0x4140>(lo0), a1 = half_codes<0x4342>(lo0);
+        const uint32_t a2 = half_codes<0x4140>(lo1), a3 = half_codes<0x4342>(lo1);
+        const uint32_t b0 = half_codes<0x4140>(hi0), b1 = half_codes<0x4342>(hi0);
+        const uint32_t b2 = half_codes<0x4140>(hi1), b3 = half_codes<0x4342>(hi1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_16816(acc[nt][2 * w], a0, a1, a2, a3, p[u][nt]);
+          mma_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, p[u][nt]);
+        }
+      }
     }
   }
 
-  // join the warps: accumulator j of lane (g, t4) holds dimensions 2 t4 D/8 + j and (2 t4 + 1) D/8 + j
-  __shared__ float o_sm[kWarps][kRows][D + 4];
+  // join the lanes' sums and then the warps
   __shared__ float stat_sm[kWarps][kRows][3];
+  copy_wait<0>();
+  __syncthreads();                   // the ring becomes the warps' outputs
+  float (*o_sm)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(smem);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    if (t4 == 0) {
-      stat_sm[warp][g + 8 * i][0] = m[i];
-      stat_sm[warp][g + 8 * i][1] = n[i];
-      stat_sm[warp][g + 8 * i][2] = l[i];
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float nn = n[nt][j];
+#pragma unroll
+      for (int o = 4; o < 32; o *= 2) nn = fmaxf(nn, __shfl_xor_sync(0xffffffffu, nn, o));
+      float ll = l[nt][j] * ex2(n[nt][j] - finite_max(nn));
+#pragma unroll
+      for (int o = 4; o < 32; o *= 2) ll += __shfl_xor_sync(0xffffffffu, ll, o);
+      const int row = 8 * nt + 2 * t4 + j;
+      if (g == 0) stat_sm[warp][row][0] = m[nt][j], stat_sm[warp][row][1] = nn, stat_sm[warp][row][2] = ll;
+      // dimensions g D/8 + 2 i, + 1 lie in accumulator i
+#pragma unroll
+      for (int i = 0; i < D / 16; i += 2)
+        *reinterpret_cast<float4*>(&o_sm[warp][row][g * (D / 8) + 2 * i]) =
+            make_float4(acc[nt][i][j], acc[nt][i][2 + j], acc[nt][i + 1][j], acc[nt][i + 1][2 + j]);
     }
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int j = 0; j < D / 8; j += 4)
-        *reinterpret_cast<float4*>(&o_sm[warp][g + 8 * i][(2 * t4 + e) * (D / 8) + j]) =
-            make_float4(acc[j][2 * i + e], acc[j + 1][2 * i + e], acc[j + 2][2 * i + e], acc[j + 3][2 * i + e]);
-  }
   __syncthreads();
-  constexpr int kPer = kRows * D / (32 * kWarps);            // 16 or 8 dimensions of one row a thread
+  constexpr int kPer = kRows * D / (32 * kWarps);            // dimensions of one row a thread
   const int row = threadIdx.x / (D / kPer), d0 = threadIdx.x % (D / kPer) * kPer;
   const int r = t.r0 + row;
   if (r >= t.rows) return;
@@ -292,11 +432,9 @@ __global__ void __launch_bounds__(32 * kWarps) kv_attn_split_kernel(AttnArgs a) 
     const float inv = out_factor(ll, base - nbase);
     uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D + d0;
 #pragma unroll
-    for (int e = 0; e < kPer; e += 8) {
-      const float v[8] = {o[e] * inv,     o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv,
-                          o[e + 4] * inv, o[e + 5] * inv, o[e + 6] * inv, o[e + 7] * inv};
-      reinterpret_cast<uint4*>(out + e)[0] = pack8(v);
-    }
+    for (int e = 0; e < kPer; e += 4)
+      *reinterpret_cast<uint2*>(out + e) =
+          make_uint2(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv));
     return;
   }
   const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * kRows) + row;
@@ -306,22 +444,25 @@ __global__ void __launch_bounds__(32 * kWarps) kv_attn_split_kernel(AttnArgs a) 
   if (d0 == 0) *reinterpret_cast<float4*>(a.part_stat + slot * 4) = make_float4(mm, nn, ll, 0.0f);
 }
 
-// Joins the splits of a row, one warp per row, in the order of the splits.
+// Joins the splits of one row per thread block: the warps take interleaved splits and are then
+// added in order.
+constexpr int kJoinWarps = 8;
 template <int D>
-__global__ void __launch_bounds__(32 * kRows) kv_attn_join_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs a) {
   constexpr int kPer = D / 32;
-  const int h = blockIdx.x % a.kv.heads, rt = blockIdx.x / a.kv.heads, b = blockIdx.y;
-  const int row = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z, row = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   Tile t;
   if (!attn_tile(a, b, rt, t)) return;
   const int ns = tile_splits(a, t), r = t.r0 + row;
   if (ns <= 1 || r >= t.rows) return;
-  const int64_t slot0 = (((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits) * kRows + row;
+  const int64_t slot0 = (((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits) * a.tile_rows + row;
   const float4* stat = reinterpret_cast<const float4*>(a.part_stat) + slot0;
   float m = -INFINITY, n = -INFINITY;
   for (int s = lane; s < ns; s += 32) {
-    m = fmaxf(m, stat[s * kRows].x);
-    n = fmaxf(n, stat[s * kRows].y);
+    const float4 v = stat[static_cast<int64_t>(s) * a.tile_rows];
+    m = fmaxf(m, v.x);
+    n = fmaxf(n, v.y);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -331,63 +472,79 @@ __global__ void __launch_bounds__(32 * kRows) kv_attn_join_kernel(AttnArgs a) {
   const float base = finite_max(m), nbase = finite_max(n);
   float acc[kPer] = {}, l = 0.0f;
 #pragma unroll 4
-  for (int s = 0; s < ns; ++s) {
-    const float4 v = stat[s * kRows];
+  for (int s = warp; s < ns; s += warps) {
+    const float4 v = stat[static_cast<int64_t>(s) * a.tile_rows];
     const float f = ex2(v.x - base);
-    const float* p = a.part + (slot0 + static_cast<int64_t>(s) * kRows) * D + lane * kPer;
+    const float* p = a.part + (slot0 + static_cast<int64_t>(s) * a.tile_rows) * D + lane * kPer;
     l = fmaf(v.z, ex2(v.y - nbase), l);
-    if constexpr (kPer == 4) {
-      const float4 x = *reinterpret_cast<const float4*>(p);
-      acc[0] = fmaf(x.x, f, acc[0]), acc[1] = fmaf(x.y, f, acc[1]);
-      acc[2] = fmaf(x.z, f, acc[2]), acc[3] = fmaf(x.w, f, acc[3]);
-    } else {
-      const float2 x = *reinterpret_cast<const float2*>(p);
-      acc[0] = fmaf(x.x, f, acc[0]), acc[1] = fmaf(x.y, f, acc[1]);
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) {
+      const float2 x = *reinterpret_cast<const float2*>(p + e);
+      acc[e] = fmaf(x.x, f, acc[e]), acc[e + 1] = fmaf(x.y, f, acc[e + 1]);
     }
   }
+  __shared__ float part[kJoinWarps][D + 1];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) part[warp][lane * kPer + e] = acc[e];
+  if (lane == 0) part[warp][D] = l;
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  float o0 = 0.0f, o1 = 0.0f;
+  l = 0.0f;
+  for (int w = 0; w < warps; ++w) {
+    o0 += part[w][2 * threadIdx.x];
+    o1 += part[w][2 * threadIdx.x + 1];
+    l += part[w][D];
+  }
   const float inv = out_factor(l, base - nbase);
-  uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D + lane * kPer;
-  if constexpr (kPer == 4)
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
-  else
-    *reinterpret_cast<uint32_t*>(out) = pack_bf16(acc[0] * inv, acc[1] * inv);
+  uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
+  reinterpret_cast<uint32_t*>(out)[threadIdx.x] = pack_bf16(o0 * inv, o1 * inv);
 }
 
-template <int D>
+template <int D, int NT>
 cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
+  using Sm = SplitSmem<D, NT>;
   const dim3 grid(a.splits, a.kv.heads * a.row_tiles, a.kv.n_seqs);
-  kv_attn_split_kernel<D><<<grid, 32 * kWarps, 0, stream>>>(a);
-  cudaError_t e = cudaGetLastError();
+  static bool smem_set[kMaxDevices];
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT>), Sm::kBytes, smem_set);
+  if (e != cudaSuccess) return e;
+  kv_attn_split_kernel<D, NT><<<grid, 32 * kWarps, Sm::kBytes, stream>>>(a);
+  e = cudaGetLastError();
   if (e != cudaSuccess || a.splits <= 1) return e;
-  kv_attn_join_kernel<D><<<dim3(a.kv.heads * a.row_tiles, a.kv.n_seqs), 32 * kRows, 0, stream>>>(a);
+  const int warps = a.splits >= 4 * kJoinWarps ? kJoinWarps : a.splits >= 8 ? kJoinWarps / 2 : 2;   // >= D / 64
+  const dim3 join(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs);
+  kv_attn_join_kernel<D><<<join, 32 * warps, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 // The keys are cut so that the tiles of the largest batch the bounds allow fill the machine about
-// four times over (ragged sequences then even out), in pieces of at least 64 keys: one step of each warp.
+// four times over (ragged sequences then even out), in pieces of at least 128 keys: one step of each warp.
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
-  a.row_tiles = static_cast<int>((rows + kRows - 1) / kRows);
+  a.tile_rows = rows <= 8 ? 8 : 16;
+  a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;
   int64_t keys = a.kv.max_len;
   if (a.window > 0) {
-    const int64_t w = static_cast<int64_t>(a.window) + kRows + 2 * kStep;
+    const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kStep;
     keys = keys < w ? keys : w;
   }
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
-  const int64_t want = static_cast<int64_t>(sms) * 12;
+  const int64_t want = static_cast<int64_t>(sms) * kWantPerSm;
+  constexpr int64_t kLeast = kStep * kWarps;
   int64_t chunk = (keys * tiles + want - 1) / want;
-  chunk = (chunk + 63) / 64 * 64;
-  if (chunk < 64) chunk = 64;
+  chunk = (chunk + kLeast - 1) / kLeast * kLeast;
+  if (chunk < kLeast) chunk = kLeast;
   a.chunk = static_cast<int>(chunk);
   const int64_t splits = (keys + chunk - 1) / chunk;
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);
 }
 
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream) {
-  return a.kv.d == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+  if (a.kv.d == 128) return a.tile_rows == 8 ? launch<128, 1>(a, stream) : launch<128, 2>(a, stream);
+  return a.tile_rows == 8 ? launch<64, 1>(a, stream) : launch<64, 2>(a, stream);
 }
 
 }  // namespace lrqat

@@ -81,16 +81,18 @@ struct AttnArgs {
   int64_t ldo;
   float scale_log2;         // softmax scale times log2(e)
   int window;               // 0: none
-  int chunk;                // keys of one split, a multiple of 64
+  int chunk;                // keys of one split
   int splits;               // most splits of a row tile
-  int row_tiles;            // tiles of 16 (token, head) rows of one sequence and key/value head
-  float* part;              // [seq][head][tile][split][16][d] unnormalised outputs (splits > 1)
-  float* part_stat;         // [seq][head][tile][split][16][4] maxima m and n, denominator
+  int tile_rows;            // (token, head) rows of a tile
+  int row_tiles;            // tiles of one sequence and key/value head
+  float* part;              // [seq][head][tile][split][tile_rows][d] unnormalised outputs (splits > 1)
+  float* part_stat;         // [seq][head][tile][split][tile_rows][4] maxima m and n, denominator
 };
-// Sets chunk, splits and row_tiles for the batch's bounds.
+// Sets chunk, splits, tile_rows and row_tiles for the batch's bounds.
 void plan_attn(AttnArgs& a, int sms);
 inline int64_t attn_part_rows(const AttnArgs& a) {
-  return a.splits > 1 ? static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles * a.splits * 16 : 0;
+  return a.splits > 1 ? static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles * a.splits * a.tile_rows
+                      : 0;
 }
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream);
 
