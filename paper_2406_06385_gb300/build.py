@@ -19,8 +19,9 @@ LIB_DIR = os.path.join(PKG, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "liblrqat.so")
 
 SOURCES = ["elementwise.cu", "fused_gemm.cu", "fused_pair.cu", "dw.cu", "dw_pair.cu", "merge.cu", "optim.cu", "norm.cu",
-           "kv_cache.cu", "kv_attn.cu", "lrqat_api.cu"]
-HEADERS = ["kernels.h", "merge.h", "ptx.cuh", "quant.cuh", "serve.h", "serve.cuh"]
+           "kv_cache.cu", "kv_attn.cu", "kv_prompt.cu", "lrqat_api.cu"]
+HEADERS = ["kernels.h", "merge.h", "ptx.cuh", "quant.cuh", "serve.h", "serve.cuh",
+           "attn.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

@@ -10,18 +10,17 @@
 // So P fits 11-bit half precision and the codes (|c| <= 128) are exact in it; a row of q is first divided by the power of two of its largest
 // magnitude, which half precision also holds (exact but for elements below 2^-14 of the largest).
 // Scores, maxima, sums and outputs are 32-bit.
-#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "attn.cuh"
 #include "kernels.h"
-#include "serve.cuh"
 
 namespace lrqat {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kStep = 32;          // keys of one step of a warp, in two halves of 16
+constexpr int kStep = kKeyAlign;   // keys of one step of a warp, in two halves of 16
 constexpr int kStages = 2;
 constexpr int kWantPerSm = 12;     // thread blocks per SM that the keys are cut into
 
@@ -38,58 +37,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// Bytes `sel` of a word of codes biased by 128 as two halves: the half 0x6400 | u is 1024 + u.
-template <uint32_t kSel>
-__device__ __forceinline__ uint32_t half_codes(uint32_t biased) {
-  const uint32_t h = __byte_perm(biased, 0x64646464u, kSel);
-  uint32_t r;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(0x64806480u));   // 1024 + 128
-  return r;
-}
-__device__ __forceinline__ float lg2(float x) {
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
-// 2^up / l, 0 for a row that saw no key (l = 0); up = m - n is at most log2 of the largest scale.
-__device__ __forceinline__ float out_factor(float l, float up) {
-  const float half = ex2(0.5f * up);                   // 2^up itself may be subnormal
-  return l == 0.0f ? 0.0f : half / l * half;
-}
-
-// The tile of `tile_rows` rows `rt` of (sequence, key/value head): row i is token
-// (tile_rows rt + i) / group of the sequence's rows and query head (tile_rows rt + i) % group of the
-// head's group.
-struct Tile {
-  SeqRows seq;
-  int rows;            // rows of the sequence and head, all tiles
-  int r0;              // first row of this tile
-  int pos_lo, pos_hi;  // positions of the tile's first and last row
-  int lo, hi;          // keys [lo, hi) that some row may see; lo a multiple of a step
-};
-__device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile& t) {
-  if (!seq_rows(a.kv, b, t.seq)) return false;
-  t.rows = t.seq.n * a.group;
-  t.r0 = rt * a.tile_rows;
-  if (t.r0 >= t.rows) return false;
-  const int last = min(t.r0 + a.tile_rows, t.rows) - 1;
-  t.pos_lo = t.seq.first + t.r0 / a.group;
-  t.pos_hi = t.seq.first + last / a.group;
-  t.hi = max(t.pos_hi + 1, 0);
-  t.lo = a.window > 0 ? max(t.pos_lo - a.window + 1, 0) & ~(kStep - 1) : 0;
-  return true;
-}
-
-__device__ __forceinline__ int tile_splits(const AttnArgs& a, const Tile& t) {
-  return t.hi > t.lo ? (t.hi - t.lo + a.chunk - 1) / a.chunk : 0;
-}
-
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -502,14 +449,21 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
 }
 
 template <int D, int NT>
-cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
+cudaError_t launch_split(const AttnArgs& a, cudaStream_t stream) {
   using Sm = SplitSmem<D, NT>;
   const dim3 grid(a.splits, a.kv.heads * a.row_tiles, a.kv.n_seqs);
   static bool smem_set[kMaxDevices];
-  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT>), Sm::kBytes, smem_set);
+  const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT>), Sm::kBytes, smem_set);
   if (e != cudaSuccess) return e;
   kv_attn_split_kernel<D, NT><<<grid, 32 * kWarps, Sm::kBytes, stream>>>(a);
-  e = cudaGetLastError();
+  return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
+  const cudaError_t e = a.tile_rows == kPromptRows ? launch_kv_prompt(a, stream)
+                        : a.tile_rows == 8         ? launch_split<D, 1>(a, stream)
+                                                   : launch_split<D, 2>(a, stream);
   if (e != cudaSuccess || a.splits <= 1) return e;
   const int warps = a.splits >= 4 * kJoinWarps ? kJoinWarps : a.splits >= 8 ? kJoinWarps / 2 : 2;   // >= D / 64
   const dim3 join(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs);
@@ -519,32 +473,35 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-// The keys are cut so that the tiles of the largest batch the bounds allow fill the machine about
-// four times over (ragged sequences then even out), in pieces of at least 128 keys: one step of each warp.
+// Up to 16 rows per sequence and key/value head the keys' bytes bound the call, and 8- or 16-row tiles of
+// the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
+// all of them.  The keys are cut so that the tiles of the largest batch the bounds allow fill the
+// machine about four (prompt kernel: two) times over, so that ragged sequences even out, in pieces of at
+// least 128 keys, one step of each warp (prompt kernel: four tiles of 128 keys).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
-  a.tile_rows = rows <= 8 ? 8 : 16;
+  a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
+  const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;
   int64_t keys = a.kv.max_len;
   if (a.window > 0) {
-    const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kStep;
+    const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kKeyAlign;
     keys = keys < w ? keys : w;
   }
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
-  const int64_t want = static_cast<int64_t>(sms) * kWantPerSm;
-  constexpr int64_t kLeast = kStep * kWarps;
+  const int64_t want = static_cast<int64_t>(sms) * (prompt ? 2 : kWantPerSm), unit = 128, least = prompt ? 512 : 128;
   int64_t chunk = (keys * tiles + want - 1) / want;
-  chunk = (chunk + kLeast - 1) / kLeast * kLeast;
-  if (chunk < kLeast) chunk = kLeast;
+  chunk = (chunk + unit - 1) / unit * unit;
+  if (chunk < least) chunk = least;
+  if (prompt && tiles >= want) chunk = (keys + unit) / unit * unit;
   a.chunk = static_cast<int>(chunk);
   const int64_t splits = (keys + chunk - 1) / chunk;
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);
 }
 
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream) {
-  if (a.kv.d == 128) return a.tile_rows == 8 ? launch<128, 1>(a, stream) : launch<128, 2>(a, stream);
-  return a.tile_rows == 8 ? launch<64, 1>(a, stream) : launch<64, 2>(a, stream);
+  return a.kv.d == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
 }
 
 }  // namespace lrqat

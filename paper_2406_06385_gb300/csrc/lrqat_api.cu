@@ -679,7 +679,8 @@ int attn_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t 
   a->window = window;
   plan_attn(*a, sm_count());
   if (static_cast<int64_t>(a->kv.max_rows) * a->group > (1 << 24) ||
-      static_cast<int64_t>(a->kv.heads) * a->row_tiles > 65535)
+      static_cast<int64_t>(a->kv.heads) * a->row_tiles > 65535 ||
+      static_cast<int64_t>(a->splits) * a->kv.heads * a->kv.n_seqs > INT32_MAX)
     return fail(LRQAT_ERR_UNSUPPORTED, "too many (token, head) rows in one sequence");
   return LRQAT_OK;
 }
@@ -1426,6 +1427,7 @@ int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int3
   DeviceInfo* dev = nullptr;
   LRQAT_TRY(device_info(&dev));
   a.kv.status = dev->status;
+  a.timeout_ns = kWaitTimeoutNs;
   a.Q = Q;
   a.ldq = ldq;
   a.O = O;

@@ -86,6 +86,7 @@ struct AttnArgs {
   int tile_rows;            // (token, head) rows of a tile
   int row_tiles;            // tiles of one sequence and key/value head
   float* part;              // [seq][head][tile][split][tile_rows][d] unnormalised outputs (splits > 1)
+  uint64_t timeout_ns;      // limit of one wait inside a kernel
   float* part_stat;         // [seq][head][tile][split][tile_rows][4] maxima m and n, denominator
 };
 // Sets chunk, splits, tile_rows and row_tiles for the batch's bounds.
@@ -94,6 +95,8 @@ inline int64_t attn_part_rows(const AttnArgs& a) {
   return a.splits > 1 ? static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles * a.splits * a.tile_rows
                       : 0;
 }
+constexpr int kPromptRows = 256;   // tile_rows of the prompt kernel (kv_prompt.cu)
+cudaError_t launch_kv_prompt(const AttnArgs& a, cudaStream_t stream);
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream);
 
 }  // namespace lrqat
