@@ -6,13 +6,13 @@
 // all heads of a group share the keys) and walks over tiles of 128 keys.  Per key tile:
 //   producer warps   turn the int8 codes into halves (exact) in the swizzled layout of the matrix
 //                    instructions: [keys][64 dimensions], K read K-major, V read MN-major;
-//   one thread       issues S = Q K^T (128 x 128 per row half) and O += P V with P read from tensor
-//                    memory, alternating the two row halves: while one half's softmax runs, the tensor
-//                    cores work on the other;
+//   two threads      (one per half of the rows) issue S = Q K^T for 64 keys at a time and O += P V with P
+//                    read from tensor memory.  A half has two score buffers: while its softmax works on
+//                    one, the tensor cores fill the other;
 //   softmax warps    one thread per row: maximum, P = 2^{z' - m} as halves back into tensor memory, over
 //                    the scores they came from.  m moves only when a row's maximum has grown by more than
 //                    2^8 (P <= 256 is exact enough in half precision and fits), so O is rarely rescaled.
-// Scores and O live in tensor memory: 2 x 128 and 2 x d columns.
+// Scores and O live in tensor memory: 2 x 2 x 64 and 2 x d columns.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -24,18 +24,22 @@
 namespace lrqat {
 namespace {
 
-constexpr int kTileKeys = 128;
+constexpr int kTileKeys = 128;               // keys converted at a time
+constexpr int kStepKeys = 64;                // keys of one softmax step: one of a half's two score buffers
 constexpr int kGroups = kTileKeys / 16;      // a cache block holds a multiple of 16 tokens
 constexpr int kStages = 2;
 constexpr int kScaleSlots = 4;
-constexpr int kSoftmaxWarps = 8, kProducerWarps = 4;
-constexpr int kThreads = 32 * (kSoftmaxWarps + kProducerWarps + 1);
+constexpr int kSoftmaxWarps = 8, kProducerWarps = 8, kMmaWarp = kSoftmaxWarps + kProducerWarps;
+constexpr int kThreads = 32 * (kMmaWarp + 4);                // five warpgroups; of the last, two warps work
+// Registers a thread of each role: over the warpgroups their sum is what the block is launched with.
+constexpr int kLaunchRegs = 96, kSoftmaxRegs = 136, kProducerRegs = 80, kMmaRegs = 40;
+static_assert(2 * kSoftmaxRegs + 2 * kProducerRegs + kMmaRegs <= 5 * kLaunchRegs, "registers of the warpgroups");
 constexpr float kLazy = 8.0f;                // how far a maximum may run ahead of m
-constexpr float kTame = 64.0f;               // spread of log2 of the value scales that one exponential serves
+constexpr float kTame = 64.0f;               // how far log2 of the value scales may lie from the first one's
 
 enum : int {
-  B_QFULL = 0, B_KFULL = 2, B_VFULL = 4, B_KEMPTY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 12, B_OFULL = 14,
-  B_SCALES = 16, B_DRAIN = 20, B_COUNT = 21
+  B_QFULL = 0, B_KFULL = 2, B_VFULL = 4, B_KEMPTY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 14, B_OFULL = 18,
+  B_SCALES = 20, B_DONE = 24, B_COUNT = 26
 };
 
 template <int D>
@@ -43,8 +47,9 @@ struct PromptSmem {
   static constexpr uint32_t kBox = 128 * 128;                  // 128 rows of 64 halves
   static constexpr uint32_t kOperand = kBox * (D / 64);        // 128 rows of one operand
   static constexpr uint32_t kQ = 0, kK = 2 * kOperand, kV = kK + kStages * kOperand;
-  static constexpr uint32_t kScale = kV + kStages * kOperand;  // [slot][coef 8, log2 s_v 8]
-  static constexpr uint32_t kBytes = kScale + kScaleSlots * 2 * kGroups * 4;
+  static constexpr uint32_t kScale = kV + kStages * kOperand;  // [slot][coefficient 8, log2 s_v 8, weight 8]
+  static constexpr uint32_t kSlot = 3 * kGroups * 4;
+  static constexpr uint32_t kBytes = kScale + kScaleSlots * kSlot + 16;     // and ref
 };
 
 // D[tmem] (+)= A[tmem] B[smem], kind::f16: A's row r in lane r, two halves a column.
@@ -71,6 +76,37 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+// Uses of v stay behind this point, and so behind the wait for the load that fills v.
+__device__ __forceinline__ void tmem_ready32(float (&v)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
+                      "+f"(v[i + 6]), "+f"(v[i + 7]));
+}
+__device__ __forceinline__ float ld_shared_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared_f32(uint32_t at, float v) {
+  asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+}
+template <bool kValue>
+struct Flag {
+  static constexpr bool value = kValue;
+};
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// True in one lane of a converged warp; unlike a test of the lane number it tells the compiler that one
+// thread is left, whose operands can stay in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void drain(uint32_t bar, uint64_t timeout_ns) {
@@ -80,13 +116,11 @@ __device__ __forceinline__ void drain(uint32_t bar, uint64_t timeout_ns) {
   }
 }
 
-// 16 codes as 16 halves: two 16-byte pieces.
-__device__ __forceinline__ void store_codes(uint32_t box, uint32_t row, uint32_t piece, const uint4& w) {
-  const uint32_t x[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
-#pragma unroll
-  for (uint32_t i = 0; i < 2; ++i)
-    st_shared_v4(box + swz_offset(row, 2 * piece + i, 128), half_codes<0x4140>(x[2 * i]), half_codes<0x4342>(x[2 * i]),
-                 half_codes<0x4140>(x[2 * i + 1]), half_codes<0x4342>(x[2 * i + 1]));
+// 16 codes as 16 halves, two 16-byte pieces at `at0` and `at1`.
+__device__ __forceinline__ void store_codes(uint32_t at0, uint32_t at1, const uint4& w) {
+  const uint32_t x0 = w.x ^ 0x80808080u, x1 = w.y ^ 0x80808080u, x2 = w.z ^ 0x80808080u, x3 = w.w ^ 0x80808080u;
+  st_shared_v4(at0, half_codes<0x4140>(x0), half_codes<0x4342>(x0), half_codes<0x4140>(x1), half_codes<0x4342>(x1));
+  st_shared_v4(at1, half_codes<0x4140>(x2), half_codes<0x4342>(x2), half_codes<0x4140>(x3), half_codes<0x4342>(x3));
 }
 
 template <int D>
@@ -115,21 +149,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
 
   if (threadIdx.x == 0) {
     abort_s = 0;
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar(B_SFULL + i), 1);
+      mbar_init(bar(B_PFULL + i), 4);
+    }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(B_QFULL + i), 4);
       mbar_init(bar(B_KFULL + i), kProducerWarps);
       mbar_init(bar(B_VFULL + i), kProducerWarps);
-      mbar_init(bar(B_KEMPTY + i), 1);
-      mbar_init(bar(B_VEMPTY + i), 1);
-      mbar_init(bar(B_SFULL + i), 1);
-      mbar_init(bar(B_PFULL + i), 4);
+      mbar_init(bar(B_KEMPTY + i), halves);
+      mbar_init(bar(B_VEMPTY + i), halves);
       mbar_init(bar(B_OFULL + i), 1);
+      mbar_init(bar(B_DONE + i), 1);
     }
     for (int i = 0; i < kScaleSlots; ++i) mbar_init(bar(B_SCALES + i), kProducerWarps);
-    mbar_init(bar(B_DRAIN), 1);
     mbar_fence_init();
   }
-  if (warp == kSoftmaxWarps + kProducerWarps) tmem_alloc(smem_u32(&tmem_base_s), 512);
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&tmem_base_s), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -137,6 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   const WaitCtl ctl{&abort_s, a.kv.status, a.timeout_ns};
 
   if (warp < kSoftmaxWarps) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     // ------------------------------------------------------------ one thread per row
     const int half = warp >> 2;
     if (half < halves) {
@@ -179,135 +216,148 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
 
       const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
       const uint32_t t_s = tmem + lanes + 128u * half, t_o = tmem + lanes + 256u + D * half;
-      float m = -INFINITY, n = -INFINITY, l = 0.0f;
-      float lv_min = INFINITY, lv_max = -INFINITY;       // log2 of the value scales so far
-      bool ok = true;
-      for (int j = 0; j < tiles; ++j) {
-        ok = wait_bounded(bar(B_SCALES + j % kScaleSlots), (j / kScaleSlots) & 1u, ctl, 1) &&
-             wait_bounded(bar(B_SFULL + half), j & 1u, ctl, 2);
-        if (!__all_sync(0xffffffffu, ok)) break;
+      // The denominator is l 2^{m - ref} with ref = log2 of the first value scale: a group's P count with weight
+      // 2^{ref - log2 s_v}, which the producers prepare.  Once a scale lies more than 2^kTame away from the first
+      // (a weight of -1), P may vanish where a term of the denominator does not: from then on it is l 2^n, summed
+      // from exponentials of its own relative to the running maximum n.
+      float m = -INFINITY, n = 0.0f, l = 0.0f;
+      bool wild = false, ok = true;
+      float s[2][32], coef[4], lsv[4], weight[4];
+      // scores and scales of step i
+      auto fetch = [&](int i) {
+        const int j = i >> 1, sub = i & 1;
+        ok = wait_bounded(bar(B_SFULL + 2 * half + sub), j & 1u, ctl, 2) &&
+             (sub == 1 || wait_bounded(bar(B_SCALES + j % kScaleSlots), (j / kScaleSlots) & 1u, ctl, 1));
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
         tc_fence_after();
-        float coef[kGroups], lsv[kGroups];
-        float tile_min = INFINITY, tile_max = -INFINITY;
-        const uint32_t slot = smem + Sm::kScale + (j % kScaleSlots) * 2 * kGroups * 4;
-#pragma unroll
-        for (int i = 0; i < kGroups; i += 4) {
-          const uint4 c = ld_shared_v4(slot + 4 * i), v = ld_shared_v4(slot + 4 * (kGroups + i));
-          const uint32_t cc[4] = {c.x, c.y, c.z, c.w}, vv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            coef[i + e] = __uint_as_float(cc[e]) * qs;
-            lsv[i + e] = __uint_as_float(vv[e]);
-            tile_max = fmaxf(tile_max, lsv[i + e]);
-            tile_min = fminf(tile_min, lsv[i + e] == -INFINITY ? INFINITY : lsv[i + e]);
-          }
-        }
-        lv_min = fminf(lv_min, tile_min);
-        lv_max = fmaxf(lv_max, tile_max);
-        const bool tame = lv_max - lv_min < kTame;
-        const int key = k0 + j * kTileKeys;
-        const bool all = key + kTileKeys - 1 <= h_lo && (a.window == 0 || key > h_hi - a.window);
+        tmem_ld32(t_s + kStepKeys * sub, s[0]);
+        tmem_ld32(t_s + kStepKeys * sub + 32, s[1]);
+        const uint32_t slot = smem + Sm::kScale + (j % kScaleSlots) * Sm::kSlot + 16 * sub;
+        const uint4 c = ld_shared_v4(slot), v = ld_shared_v4(slot + 4 * kGroups), w = ld_shared_v4(slot + 8 * kGroups);
+        coef[0] = __uint_as_float(c.x) * qs, coef[1] = __uint_as_float(c.y) * qs;
+        coef[2] = __uint_as_float(c.z) * qs, coef[3] = __uint_as_float(c.w) * qs;
+        lsv[0] = __uint_as_float(v.x), lsv[1] = __uint_as_float(v.y), lsv[2] = __uint_as_float(v.z), lsv[3] = __uint_as_float(v.w);
+        weight[0] = __uint_as_float(w.x), weight[1] = __uint_as_float(w.y);
+        weight[2] = __uint_as_float(w.z), weight[3] = __uint_as_float(w.w);
+        tmem_ld_wait();
+        tmem_ready32(s[0]);
+        tmem_ready32(s[1]);
+      };
+      if (tiles > 0) fetch(0);
+      for (int i = 0; i < 2 * tiles && ok; ++i) {
+        const int sub = i & 1;
+        const uint32_t t_p = t_s + kStepKeys * sub;      // this step's scores and, over them, its P
+        const int key = k0 + i * kStepKeys;
+        const bool all = key + kStepKeys - 1 <= h_lo && (a.window == 0 || key > h_hi - a.window);
         const int c_hi = pos - key;                      // columns c_lo .. c_hi of this row are visible
-        const int c_lo = a.window > 0 ? pos - a.window + 1 - key : 0;
-
-        // the largest z' (and z) of the row
-        float mx = -INFINITY, zx = -INFINITY;
+        const int c_lo = a.window > 0 ? c_hi - a.window + 1 : 0;
+        if (!all) {
 #pragma unroll
-        for (int c = 0; c < kTileKeys; c += 32) {
-          float s[32];
-          tmem_ld32(t_s + c, s);
-          tmem_ld_wait();
-          if (!all) {
+          for (int c = 0; c < kStepKeys; ++c)
+            if (c > c_hi || c < c_lo) s[c / 32][c % 32] = -INFINITY;
+        }
+        float g[4], mx = -INFINITY;                      // the largest score of a group, the largest z' of the row
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (c + e > c_hi || c + e < c_lo) s[e] = -INFINITY;
-          }
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            float g = s[16 * u];
-#pragma unroll
-            for (int e = 1; e < 16; ++e) g = fmaxf(g, s[16 * u + e]);
-            const float z = g * coef[c / 16 + u];
-            zx = fmaxf(zx, z);
-            mx = fmaxf(mx, z + lsv[c / 16 + u]);
-          }
+        for (int u = 0; u < 4; ++u) {
+          const float* v = &s[u / 2][16 * (u % 2)];
+          float g0 = max3(v[0], v[1], v[2]), g1 = max3(v[3], v[4], v[5]);
+          g0 = max3(g0, v[6], v[7]), g1 = max3(g1, v[8], v[9]);
+          g0 = max3(g0, v[10], v[11]), g1 = max3(g1, v[12], v[13]);
+          g[u] = max3(g0, g1, fmaxf(v[14], v[15]));
+          mx = fmaxf(mx, fmaf(g[u], coef[u], lsv[u]));
         }
         const float m1 = mx > m + kLazy || m == -INFINITY ? fmaxf(m, mx) : m;
-        const float base = finite_max(m1);
-        const float alpha = ex2(m - base);
-        if (j > 0 && __any_sync(0xffffffffu, m1 != m)) {
-          ok = wait_bounded(bar(B_OFULL + half), (j - 1) & 1u, ctl, 3);
-          if (!__all_sync(0xffffffffu, ok)) break;
-          tc_fence_after();
+        if (__any_sync(0xffffffffu, m1 != m)) {
+          const float alpha = ex2(m - finite_max(m1));
+          if (!wild) l *= alpha;
+          if (i > 0) {
+            ok = wait_bounded(bar(B_OFULL + half), (i - 1) & 1u, ctl, 3);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < D; c += 16) {
-            float o[16];
-            uint32_t w[16];
-            tmem_ld16(t_o + c, o);
+            for (int c = 0; c < D; c += 16) {
+              float o[16];
+              uint32_t w[16];
+              tmem_ld16(t_o + c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * alpha);
+              tmem_st16(t_o + c, w);
+            }
+          }
+          m = m1;
+        }
+        const float base = finite_max(m);
+        if (fminf(fminf(weight[0], weight[1]), fminf(weight[2], weight[3])) < 0.0f || wild) {
+          const float ref = ld_shared_f32(smem + Sm::kScale + kScaleSlots * Sm::kSlot);
+          float zx = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) zx = fmaxf(zx, g[u] * coef[u]);
+          const float was = wild ? n : base - ref, n1 = l == 0.0f ? zx : fmaxf(was, zx), nbase = finite_max(n1);
+          l = l == 0.0f ? 0.0f : l * ex2(was - nbase);
+          n = nbase;
+          wild = true;
+#pragma unroll 1
+          for (int u = 0; u < 4; ++u) {
+            const uint32_t slot = smem + Sm::kScale + ((i >> 1) % kScaleSlots) * Sm::kSlot + 16 * sub + 4 * u;
+            const float cu = ld_shared_f32(slot) * qs, lv = ld_shared_f32(slot + 4 * kGroups);
+            float x[16];
+            tmem_ld16(t_p + 16 * u, x);
             tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * alpha);
-            tmem_st16(t_o + c, w);
+            for (int e = 0; e < 16; ++e) {               // hidden keys and groups without a block add nothing
+              const bool seen = lv != -INFINITY && (all || (16 * u + e <= c_hi && 16 * u + e >= c_lo));
+              l += seen ? ex2(fmaf(x[e], cu, -nbase)) : 0.0f;
+            }
           }
         }
-        m = m1;
-        // the denominator relative to 2^n
-        const float n1 = tame ? fmaxf(n, m1 - lv_min) : fmaxf(n, zx);
-        const float nbase = finite_max(n1);
-        l *= ex2(n - nbase);
-        n = n1;
+        float part[4];                                   // a group's sum of P
+        auto weights = [&](auto masked) {
 #pragma unroll
-        for (int c = 0; c < kTileKeys; c += 32) {
-          float s[32];
-          uint32_t p[16];
-          tmem_ld32(t_s + c, s);
-          tmem_ld_wait();
+          for (int c = 0; c < kStepKeys; c += 32) {
+            uint32_t p[16];
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float cu = coef[c / 16 + u], du = lsv[c / 16 + u] - base;
-            float2 sum = make_float2(0.0f, 0.0f);
+            for (int u = 0; u < 2; ++u) {
+              const float cu = coef[c / 16 + u], du = lsv[c / 16 + u] - base;
+              const float* v = &s[c / 32][16 * u];
+              float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-              float2 x = __ffma2_rn(make_float2(s[16 * u + e], s[16 * u + e + 1]), make_float2(cu, cu), make_float2(du, du));
-              if (!all) {
-                const int k = c + 16 * u + e;
-                if (k > c_hi || k < c_lo) x.x = -INFINITY;
-                if (k + 1 > c_hi || k + 1 < c_lo) x.y = -INFINITY;
+              for (int e = 0; e < 16; e += 2) {
+                float2 x = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(cu, cu), make_float2(du, du));
+                if (decltype(masked)::value) {           // a coefficient of 0 or NaN must not bring a hidden key back
+                  x.x = v[e] == -INFINITY ? -INFINITY : x.x;
+                  x.y = v[e + 1] == -INFINITY ? -INFINITY : x.y;
+                }
+                x.x = ex2(x.x);
+                x.y = ex2(x.y);
+                sum = __fadd2_rn(sum, x);
+                p[8 * u + e / 2] = pack_half(x.x, x.y);
               }
-              x.x = ex2(x.x);
-              x.y = ex2(x.y);
-              sum = __fadd2_rn(sum, x);
-              p[8 * u + e / 2] = pack_half(x.x, x.y);
+              part[c / 16 + u] = sum.x + sum.y;
             }
-            if (tame) {
-              const float part = sum.x + sum.y;          // a hidden group adds nothing, whatever its scale
-              l = part == 0.0f ? l : fmaf(part, ex2(base - lsv[c / 16 + u] - nbase), l);
-            }
+            tmem_st16(t_p + c / 2, p);
           }
-          if (!tame) {
-            // scales far apart: P may vanish where a term of the denominator does not
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const bool seen = lsv[(c + e) / 16] != -INFINITY && (all || (c + e <= c_hi && c + e >= c_lo));
-              l += seen ? ex2(fmaf(s[e], coef[(c + e) / 16], -nbase)) : 0.0f;
-            }
-          }
-          tmem_st16(t_s + c / 2, p);
-        }
+        };
+        if (all) weights(Flag<false>{});
+        else weights(Flag<true>{});
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_PFULL + half));
+        if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * half + sub));
+        if (!wild) l += fmaf(part[0], weight[0], part[1] * weight[1]) + fmaf(part[2], weight[2], part[3] * weight[3]);
+        if (i + 1 < 2 * tiles) fetch(i + 1);
       }
+      if (!wild) n = m == -INFINITY ? 0.0f : m - ld_shared_f32(smem + Sm::kScale + kScaleSlots * Sm::kSlot);
       if (tiles > 0) {
-        ok = ok && wait_bounded(bar(B_OFULL + half), (tiles - 1) & 1u, ctl, 4);
+        ok = ok && wait_bounded(bar(B_DONE + half), 0u, ctl, 4);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
       }
       if (ok) {
         const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) +
                              128 * half + r_in;
-        const float f = ns <= 1 ? out_factor(l, finite_max(m) - finite_max(n)) : 1.0f;
+        const float f = ns <= 1 ? out_factor(l, finite_max(m) - n) : 1.0f;
         uint16_t* out = a.O + (t.seq.row0 + tok) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
@@ -334,54 +384,62 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
               *reinterpret_cast<float4*>(a.part + slot * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
-        if (ns > 1 && in) *reinterpret_cast<float4*>(a.part_stat + slot * 4) = make_float4(m, n, l, 0.0f);
+        if (ns > 1 && in)
+          *reinterpret_cast<float4*>(a.part_stat + slot * 4) = make_float4(m, l == 0.0f ? -INFINITY : n, l, 0.0f);
       }
     }
-  } else if (warp < kSoftmaxWarps + kProducerWarps) {
+  } else if (warp < kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
     // ------------------------------------------------------------ codes into operands
-    // A warp has 32 tokens of the tile, two groups of 16.  A load instruction takes 64 bytes of 8
-    // tokens: four lanes a token, so that the stores of 8 lanes (two rows) hit distinct banks.
+    // A warp has one group of 16 tokens of the tile.  A load instruction takes 64 bytes of 8 tokens: four
+    // lanes a token, so that the stores of 8 lanes (two rows) hit distinct banks.
     const int w = warp - kSoftmaxWarps;
-    const uint32_t piece = lane & 3, sub = lane >> 2;
+    const uint32_t piece = lane & 3, row = lane >> 2;
     const uint32_t in_block = (1u << a.kv.block_log2) - 1;
     const int32_t* table = a.kv.table + static_cast<int64_t>(b) * a.kv.max_blocks;
-    // lanes 0 and 1: the cache block of the warp's group `lane` of a tile (-1: none, -2: past the keys)
+    // the cache block of the warp's group of a tile (-1: none, -2: past the keys)
     auto block_of = [&](int j) {
-      const int key = k0 + j * kTileKeys + 32 * w + 16 * (lane & 1);
+      const int key = k0 + j * kTileKeys + 16 * w;
       if (j >= tiles || key >= k1) return -2;
       const int blk = __ldg(table + (key >> a.kv.block_log2));
       return static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks) ? blk : -1;
     };
-    uint4 kr[4 * kBoxes], vr[4 * kBoxes];
-    auto load = [&](uint4 (&reg)[4 * kBoxes], const int8_t* codes, int j, int blk) {
+    uint4 kr[2 * kBoxes], vr[2 * kBoxes];
+    auto load = [&](uint4 (&reg)[2 * kBoxes], const int8_t* codes, int j, int blk) {
+      const int key = k0 + j * kTileKeys + 16 * w;
+      const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
+      const int8_t* p = codes + ((at << a.kv.block_log2) + (key & in_block) + row) * D + 16 * piece;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int bu = __shfl_sync(0xffffffffu, blk, u);
-        const int key = k0 + j * kTileKeys + 32 * w + 16 * u;
-        const int64_t at = static_cast<int64_t>(bu) * a.kv.heads + h;
-        const int8_t* p = codes + ((at << a.kv.block_log2) + (key & in_block) + sub) * D + 16 * piece;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (uint32_t x = 0; x < kBoxes; ++x)
-            reg[(2 * u + i) * kBoxes + x] =
-                bu >= 0 ? __ldg(reinterpret_cast<const uint4*>(p + 8 * i * D + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
-      }
-    };
-    auto store = [&](const uint4 (&reg)[4 * kBoxes], uint32_t operand) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (uint32_t x = 0; x < kBoxes; ++x)
-          store_codes(operand + x * Sm::kBox, 32 * w + 8 * i + sub, piece, reg[i * kBoxes + x]);
+          reg[i * kBoxes + x] = blk >= 0 ? __ldg(reinterpret_cast<const uint4*>(p + 8 * i * D + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    // row 16 w + 8 i + row of a box: the swizzle depends on the row within 8 alone
+    const uint32_t off0 = (16 * w + row) * 128 + ((2 * piece) ^ row) * 16, off1 = off0 ^ 16u;
+    auto store = [&](const uint4 (&reg)[2 * kBoxes], uint32_t operand) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (uint32_t x = 0; x < kBoxes; ++x)
+          store_codes(operand + off0 + (x * Sm::kBox + 1024 * i), operand + off1 + (x * Sm::kBox + 1024 * i),
+                      reg[i * kBoxes + x]);
     };
     auto scale_of = [&](const float* scale, int blk) {
-      return lane < 2 && blk >= 0 ? __ldg(scale + static_cast<int64_t>(blk) * a.kv.heads + h) : 0.0f;
+      return blk >= 0 ? __ldg(scale + static_cast<int64_t>(blk) * a.kv.heads + h) : 0.0f;
     };
     int blk = block_of(0), blk_next = block_of(1);
     float sk = scale_of(a.kv.scale[0], blk), sv = scale_of(a.kv.scale[1], blk);
     load(kr, a.kv.codes[0], 0, blk);
     load(vr, a.kv.codes[1], 0, blk);
+    // log2 of the value scale of the first key's block, 0 where that has none
+    float ref = 0.0f;
+    if (tiles > 0) {
+      const int first = __ldg(table + (k0 >> a.kv.block_log2));
+      const float v = scale_of(a.kv.scale[1], static_cast<uint32_t>(first) < static_cast<uint64_t>(a.kv.n_blocks) ? first : -1);
+      ref = v > 0.0f && v < INFINITY ? lg2(v) : 0.0f;
+    }
+    if (w == 0 && lane == 0) st_shared_f32(smem + Sm::kScale + kScaleSlots * Sm::kSlot, ref);
     bool ok = true;
     for (int j = 0; j < tiles; ++j) {
       const uint32_t stage = j % kStages, par = ((j / kStages) & 1u) ^ 1u;
@@ -389,14 +447,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       // were computed after the softmax of three tiles ago
       ok = wait_bounded(bar(B_KEMPTY + stage), par, ctl, 5);
       if (!__all_sync(0xffffffffu, ok)) break;
-      if (lane < 2) {
+      if (lane == 0) {
         if (blk == -1) atomicOr(a.kv.status, kStatusRange);
-        const uint32_t at = smem + Sm::kScale + (j % kScaleSlots) * 2 * kGroups * 4 + 4 * (2 * w + lane);
-        const float c = blk >= 0 ? fabsf(a.scale_log2) * sk : 0.0f, v = blk >= 0 ? lg2(sv) : -INFINITY;
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(c) : "memory");
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * kGroups), "f"(v) : "memory");
+        const uint32_t at = smem + Sm::kScale + (j % kScaleSlots) * Sm::kSlot + 4 * w;
+        const float v = blk >= 0 ? lg2(sv) : -INFINITY, away = ref - v;
+        st_shared_f32(at, blk >= 0 ? fabsf(a.scale_log2) * sk : 0.0f);
+        st_shared_f32(at + 4 * kGroups, v);
+        // NaN: its P are NaN themselves where they are seen
+        st_shared_f32(at + 8 * kGroups, blk < 0 ? 0.0f : away != away ? 1.0f : fabsf(away) < kTame ? ex2(away) : -1.0f);
       }
-      const int cur_next = blk_next;
       store(kr, smem + Sm::kK + stage * Sm::kOperand);
       fence_proxy_async_smem();
       __syncwarp();
@@ -404,70 +463,73 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
         mbar_arrive(bar(B_SCALES + j % kScaleSlots));
         mbar_arrive(bar(B_KFULL + stage));
       }
+      blk = blk_next;
       blk_next = block_of(j + 2);
-      load(kr, a.kv.codes[0], j + 1, cur_next);
-      sk = scale_of(a.kv.scale[0], cur_next);
-      sv = scale_of(a.kv.scale[1], cur_next);
-      blk = cur_next;
+      load(kr, a.kv.codes[0], j + 1, blk);
+      sk = scale_of(a.kv.scale[0], blk);
+      sv = scale_of(a.kv.scale[1], blk);
       ok = wait_bounded(bar(B_VEMPTY + stage), par, ctl, 6);
       if (!__all_sync(0xffffffffu, ok)) break;
       store(vr, smem + Sm::kV + stage * Sm::kOperand);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(B_VFULL + stage));
-      load(vr, a.kv.codes[1], j + 1, cur_next);
+      load(vr, a.kv.codes[1], j + 1, blk);
     }
-  } else if (lane == 0) {
-    // ------------------------------------------------------------ MMA issuer
-    const uint32_t idesc_s = make_idesc_f16(128, kTileKeys, 0), idesc_o = make_idesc_f16(128, D, 1);
-    const uint64_t d_q = make_sdesc(smem + Sm::kQ, 16, 1024, SWZ_128B), d_k = make_sdesc(smem + Sm::kK, 16, 1024, SWZ_128B);
-    const uint64_t d_v = make_sdesc(smem + Sm::kV, Sm::kBox, 1024, SWZ_128B);
-    auto scores = [&](int half, uint32_t stage) {
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    // one thread per row half
+    const int half = warp - kMmaWarp;
+    if (half < halves && elect_one()) {
+      const uint32_t idesc_s = make_idesc_f16(128, kStepKeys, 0), idesc_o = make_idesc_f16(128, D, 1);
+      const uint64_t d_q = make_sdesc(smem + Sm::kQ + half * Sm::kOperand, 16, 1024, SWZ_128B);
+      const uint64_t d_k = make_sdesc(smem + Sm::kK, 16, 1024, SWZ_128B);
+      const uint64_t d_v = make_sdesc(smem + Sm::kV, Sm::kBox, 1024, SWZ_128B);
+      const uint32_t t_s = tmem + 128u * half, t_o = tmem + 256u + D * half;
+      auto scores = [&](uint32_t stage, uint32_t sub) {
 #pragma unroll
-      for (uint32_t ks = 0; ks < D / 16; ++ks) {
-        const uint32_t off = (Sm::kBox * (ks >> 2) + 32u * (ks & 3)) >> 4;
-        mma_bf16(tmem + 128u * half, d_q + half * (Sm::kOperand >> 4) + off, d_k + stage * (Sm::kOperand >> 4) + off,
-                 idesc_s, ks > 0 ? 1u : 0u);
-      }
-      mma_commit(bar(B_SFULL + half));
-    };
-    bool ok = true;
-    for (int half = 0; half < halves && ok && tiles > 0; ++half) {
-      ok = wait_spin_bounded(bar(B_QFULL + half), 0, ctl, 7) && (half > 0 || wait_spin_bounded(bar(B_KFULL), 0, ctl, 8));
-      if (!ok) break;
-      tc_fence_after();
-      scores(half, 0);
-      if (half == halves - 1) mma_commit(bar(B_KEMPTY));
-    }
-    for (int j = 0; j < tiles && ok; ++j) {
-      const uint32_t stage = j % kStages, next = (j + 1) % kStages;
-      for (int half = 0; half < halves && ok; ++half) {
-        ok = (half > 0 || wait_spin_bounded(bar(B_VFULL + stage), (j / kStages) & 1u, ctl, 9)) &&
-             wait_spin_bounded(bar(B_PFULL + half), j & 1u, ctl, 10);
-        if (!ok) break;
+        for (uint32_t ks = 0; ks < D / 16; ++ks) {
+          const uint32_t off = (Sm::kBox * (ks >> 2) + 32u * (ks & 3)) >> 4;
+          mma_bf16(t_s + kStepKeys * sub, d_q + off, d_k + stage * (Sm::kOperand >> 4) + sub * (kStepKeys * 128 >> 4) + off,
+                   idesc_s, ks > 0 ? 1u : 0u);
+        }
+        mma_commit(bar(B_SFULL + 2 * half + sub));
+      };
+      bool ok = tiles > 0 && wait_spin_bounded(bar(B_QFULL + half), 0, ctl, 7) && wait_spin_bounded(bar(B_KFULL), 0, ctl, 8);
+      if (ok) {
         tc_fence_after();
-#pragma unroll
-        for (uint32_t ks = 0; ks < kTileKeys / 16; ++ks)
-          mma_f16_ts(tmem + 256u + D * half, tmem + 128u * half + 8 * ks, d_v + stage * (Sm::kOperand >> 4) + 128 * ks,
-                     idesc_o, j > 0 || ks > 0 ? 1u : 0u);
-        mma_commit(bar(B_OFULL + half));
-        if (half == halves - 1) mma_commit(bar(B_VEMPTY + stage));
-        if (j + 1 < tiles) {
-          ok = half > 0 || wait_spin_bounded(bar(B_KFULL + next), ((j + 1) / kStages) & 1u, ctl, 11);
-          if (!ok) break;
+        scores(0, 0);
+        scores(0, 1);
+        mma_commit(bar(B_KEMPTY));
+      }
+      for (int j = 0; j < tiles && ok; ++j) {
+        const uint32_t stage = j % kStages, next = (j + 1) % kStages;
+        ok = wait_spin_bounded(bar(B_VFULL + stage), (j / kStages) & 1u, ctl, 9);
+        for (uint32_t sub = 0; sub < 2 && ok; ++sub) {
+          if (!(ok = wait_spin_bounded(bar(B_PFULL + 2 * half + sub), j & 1u, ctl, 10))) break;
           tc_fence_after();
-          scores(half, next);                            // in order after the product that reads P from the same columns
-          if (half == halves - 1) mma_commit(bar(B_KEMPTY + next));
+#pragma unroll
+          for (uint32_t ks = 0; ks < kStepKeys / 16; ++ks)
+            mma_f16_ts(t_o, t_s + kStepKeys * sub + 8 * ks, d_v + stage * (Sm::kOperand >> 4) + 128 * (4 * sub + ks), idesc_o,
+                       j > 0 || sub > 0 || ks > 0 ? 1u : 0u);
+          mma_commit(bar(B_OFULL + half));
+          if (sub == 1) mma_commit(bar(B_VEMPTY + stage));
+          if (j + 1 < tiles) {
+            if (sub == 0 && !(ok = wait_spin_bounded(bar(B_KFULL + next), ((j + 1) / kStages) & 1u, ctl, 11))) break;
+            tc_fence_after();
+            scores(next, sub);                           // in order after the product that reads P from the same columns
+            if (sub == 1) mma_commit(bar(B_KEMPTY + next));
+          }
         }
       }
+      // every matrix instruction has completed: O is read, and the memories are released
+      mma_commit(bar(B_DONE + half));
+      drain(bar(B_DONE + half), a.timeout_ns);
     }
-    // every matrix instruction has completed before the memories are released
-    mma_commit(bar(B_DRAIN));
-    drain(bar(B_DRAIN), a.timeout_ns);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kSoftmaxWarps + kProducerWarps) {
+  if (warp == kMmaWarp) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
