@@ -29,11 +29,11 @@ constexpr int kStepKeys = 64;                // keys of one softmax step: one of
 constexpr int kGroups = kTileKeys / 16;      // a cache block holds a multiple of 16 tokens
 constexpr int kStages = 2;
 constexpr int kScaleSlots = 4;
-constexpr int kSoftmaxWarps = 8, kProducerWarps = 8, kMmaWarp = kSoftmaxWarps + kProducerWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 4);                // five warpgroups; of the last, two warps work
+constexpr int kSoftmaxWarps = 8, kProducerWarps = 4, kMmaWarp = kSoftmaxWarps + kProducerWarps;
+constexpr int kThreads = 32 * (kMmaWarp + 4);                // four warpgroups; of the last, two warps work
 // Registers a thread of each role: over the warpgroups their sum is what the block is launched with.
-constexpr int kLaunchRegs = 96, kSoftmaxRegs = 136, kProducerRegs = 80, kMmaRegs = 40;
-static_assert(2 * kSoftmaxRegs + 2 * kProducerRegs + kMmaRegs <= 5 * kLaunchRegs, "registers of the warpgroups");
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 184, kProducerRegs = 104, kMmaRegs = 40;
+static_assert(2 * kSoftmaxRegs + kProducerRegs + kMmaRegs <= 4 * kLaunchRegs, "registers of the warpgroups");
 constexpr float kLazy = 8.0f;                // how far a maximum may run ahead of m
 constexpr float kTame = 64.0f;               // how far log2 of the value scales may lie from the first one's
 
@@ -391,42 +391,47 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   } else if (warp < kMmaWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
     // ------------------------------------------------------------ codes into operands
-    // A warp has one group of 16 tokens of the tile.  A load instruction takes 64 bytes of 8 tokens: four
-    // lanes a token, so that the stores of 8 lanes (two rows) hit distinct banks.
+    // A warp has 32 tokens of the tile, two groups of 16.  A load instruction takes 64 bytes of 8 tokens:
+    // four lanes a token, so that the stores of 8 lanes (two rows) hit distinct banks.
     const int w = warp - kSoftmaxWarps;
     const uint32_t piece = lane & 3, row = lane >> 2;
     const uint32_t in_block = (1u << a.kv.block_log2) - 1;
     const int32_t* table = a.kv.table + static_cast<int64_t>(b) * a.kv.max_blocks;
-    // the cache block of the warp's group of a tile (-1: none, -2: past the keys)
+    // lanes 0 and 1: the cache block of the warp's group `lane` of a tile (-1: none, -2: past the keys)
     auto block_of = [&](int j) {
-      const int key = k0 + j * kTileKeys + 16 * w;
+      const int key = k0 + j * kTileKeys + 32 * w + 16 * (lane & 1);
       if (j >= tiles || key >= k1) return -2;
       const int blk = __ldg(table + (key >> a.kv.block_log2));
       return static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks) ? blk : -1;
     };
-    uint4 kr[2 * kBoxes], vr[2 * kBoxes];
-    auto load = [&](uint4 (&reg)[2 * kBoxes], const int8_t* codes, int j, int blk) {
-      const int key = k0 + j * kTileKeys + 16 * w;
-      const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
-      const int8_t* p = codes + ((at << a.kv.block_log2) + (key & in_block) + row) * D + 16 * piece;
+    uint4 kr[4 * kBoxes], vr[4 * kBoxes];
+    auto load = [&](uint4 (&reg)[4 * kBoxes], const int8_t* codes, int j, int blk) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int u = 0; u < 2; ++u) {
+        const int bu = __shfl_sync(0xffffffffu, blk, u);
+        const int key = k0 + j * kTileKeys + 32 * w + 16 * u;
+        const int64_t at = static_cast<int64_t>(bu) * a.kv.heads + h;
+        const int8_t* p = codes + ((at << a.kv.block_log2) + (key & in_block) + row) * D + 16 * piece;
 #pragma unroll
-        for (uint32_t x = 0; x < kBoxes; ++x)
-          reg[i * kBoxes + x] = blk >= 0 ? __ldg(reinterpret_cast<const uint4*>(p + 8 * i * D + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (uint32_t x = 0; x < kBoxes; ++x)
+            reg[(2 * u + i) * kBoxes + x] =
+                bu >= 0 ? __ldg(reinterpret_cast<const uint4*>(p + 8 * i * D + 64 * x)) : make_uint4(0u, 0u, 0u, 0u);
+      }
     };
-    // row 16 w + 8 i + row of a box: the swizzle depends on the row within 8 alone
-    const uint32_t off0 = (16 * w + row) * 128 + ((2 * piece) ^ row) * 16, off1 = off0 ^ 16u;
-    auto store = [&](const uint4 (&reg)[2 * kBoxes], uint32_t operand) {
+    // row 32 w + 8 i + row of a box: the swizzle depends on the row within 8 alone
+    const uint32_t off0 = (32 * w + row) * 128 + ((2 * piece) ^ row) * 16, off1 = off0 ^ 16u;
+    auto store = [&](const uint4 (&reg)[4 * kBoxes], uint32_t operand) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (uint32_t x = 0; x < kBoxes; ++x)
           store_codes(operand + off0 + (x * Sm::kBox + 1024 * i), operand + off1 + (x * Sm::kBox + 1024 * i),
                       reg[i * kBoxes + x]);
     };
     auto scale_of = [&](const float* scale, int blk) {
-      return blk >= 0 ? __ldg(scale + static_cast<int64_t>(blk) * a.kv.heads + h) : 0.0f;
+      return lane < 2 && blk >= 0 ? __ldg(scale + static_cast<int64_t>(blk) * a.kv.heads + h) : 0.0f;
     };
     int blk = block_of(0), blk_next = block_of(1);
     float sk = scale_of(a.kv.scale[0], blk), sv = scale_of(a.kv.scale[1], blk);
@@ -447,9 +452,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       // were computed after the softmax of three tiles ago
       ok = wait_bounded(bar(B_KEMPTY + stage), par, ctl, 5);
       if (!__all_sync(0xffffffffu, ok)) break;
-      if (lane == 0) {
+      if (lane < 2) {
         if (blk == -1) atomicOr(a.kv.status, kStatusRange);
-        const uint32_t at = smem + Sm::kScale + (j % kScaleSlots) * Sm::kSlot + 4 * w;
+        const uint32_t at = smem + Sm::kScale + (j % kScaleSlots) * Sm::kSlot + 4 * (2 * w + lane);
         const float v = blk >= 0 ? lg2(sv) : -INFINITY, away = ref - v;
         st_shared_f32(at, blk >= 0 ? fabsf(a.scale_log2) * sk : 0.0f);
         st_shared_f32(at + 4 * kGroups, v);
