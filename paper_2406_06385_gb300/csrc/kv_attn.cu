@@ -21,8 +21,9 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kStep = kKeyAlign;   // keys of one step of a warp, in two halves of 16
-constexpr int kStages = 2;
-constexpr int kWantPerSm = 12;     // thread blocks per SM that the keys are cut into
+constexpr int kStages = 2, kValueStages = 1;   // steps of keys and of values in a warp's ring
+constexpr int kPerSm = 16 / kWarps;        // thread blocks an SM holds (with 16 rows: half of them)
+constexpr int kCutPerSm = 2 * kPerSm;      // and blocks per SM that the keys are cut into
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                           const uint32_t (&b)[2]) {
@@ -62,8 +63,8 @@ __device__ __forceinline__ uint32_t value_place(uint32_t r, uint32_t q) {
 template <int D, int NT>
 struct SplitSmem {
   static constexpr int kHalf = 16 * D;                                      // bytes of 16 keys
-  static constexpr int kWarpStage = 4 * kHalf;                              // keys, keys, values, values
-  static constexpr int kRing = kStages * kWarps * kWarpStage;
+  static constexpr int kWarpStage = 2 * kHalf;                              // 32 keys, or their values
+  static constexpr int kRing = (kStages + kValueStages) * kWarps * kWarpStage;
   static constexpr int kOut = kWarps * 8 * NT * (D + 4) * 4;                // the join's outputs reuse the ring
   static constexpr int kScales = kRing > kOut ? kRing : kOut;
   static constexpr int kBytes = kScales + kStages * kWarps * 16;
@@ -75,16 +76,16 @@ struct SplitSmem {
 // second (o^T = V^T P^T), so a tile of 8 rows wastes no tensor work and few registers, and one 8 x 8
 // transpose per 8 keys turns scores into the second product's operand.  The order of the dimensions
 // inside a product is free: each lane takes 16 consecutive bytes of a token.  A step's codes come
-// through a ring in shared memory, one step ahead, filled by the warp that reads it: warps never
-// wait for one another.
+// through a ring in shared memory filled by the warp that reads it: warps never wait for one another.
 template <int D, int NT>
-__global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_attn_split_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv_attn_split_kernel(AttnArgs a) {
   using Sm = SplitSmem<D, NT>;
   constexpr int kC = D / 64;         // 64-dimension pieces of a token
   constexpr int kRows = 8 * NT;
   extern __shared__ __align__(16) uint8_t smem[];
   const int split = blockIdx.x, h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Tile t;
   if (!attn_tile(a, b, rt, t)) return;
   const int ns = tile_splits(a, t);
@@ -103,7 +104,11 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
   int next_blk[2] = {block_of(first_key), block_of(first_key + 16)};
   uint32_t skipped = 0;              // bit 2 s + u: half u of the step in stage s has no valid block
   const uint32_t piece = lane % (D / 16), tok = lane / (D / 16);            // a copy instruction covers 512 / D tokens
-  auto issue = [&](int i) {
+  // where the keys copied last lie, and those before them: the values that are copied next
+  int64_t k_off[2] = {-1, -1}, v_off[2] = {-1, -1};
+  static_assert(kStages == 2 && kValueStages == 1, "the values' offsets run one step behind the keys'");
+  // keys and scales of step i, and (later) its values: each stage is refilled as soon as it has been read
+  auto issue_keys = [&](int i) {
     if (i < steps) {
       const int key = first_key + i * kStep * kWarps, stage = i % kStages;
 #pragma unroll
@@ -111,18 +116,16 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
         const int blk = next_blk[u];
         next_blk[u] = block_of(key + kStep * kWarps + 16 * u);
         const uint32_t bit = 1u << (2 * stage + u);
+        v_off[u] = k_off[u];
+        k_off[u] = -1;
         if (static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks)) {
           skipped &= ~bit;
           const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
-          const int64_t off = ((at << a.kv.block_log2) + ((key + 16 * u) & in_block)) * D + lane * 16;
-          const int8_t* kp = a.kv.codes[0] + off;
-          const int8_t* vp = a.kv.codes[1] + off;
+          k_off[u] = ((at << a.kv.block_log2) + ((key + 16 * u) & in_block)) * D + lane * 16;
+          const int8_t* p = a.kv.codes[0] + k_off[u];
           const uint32_t dst = ring + stage * kStageBytes + u * Sm::kHalf;
 #pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            copy_async16(dst + key_place<D>(512 / D * j + tok, piece), kp + 512 * j);
-            copy_async16(dst + 2 * Sm::kHalf + value_place<D>(512 / D * j + tok, piece), vp + 512 * j);
-          }
+          for (int j = 0; j < D / 32; ++j) copy_async16(dst + key_place<D>(512 / D * j + tok, piece), p + 512 * j);
           if (lane < 2)
             copy_async4(scales + stage * kStageScales + u * 8 + lane * 4, (lane ? a.kv.scale[1] : a.kv.scale[0]) + at);
         } else {
@@ -130,11 +133,29 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
           if (lane == 0 && blk != -2) atomicOr(a.kv.status, kStatusRange);
         }
       }
+    } else {
+      v_off[0] = k_off[0], v_off[1] = k_off[1];
+    }
+    copy_commit();
+  };
+  auto issue_values = [&](int i, const int64_t (&off)[2]) {
+    if (i < steps) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (off[u] < 0) continue;
+        const int8_t* p = a.kv.codes[1] + off[u];
+        const uint32_t dst = ring + (kStages + i % kValueStages) * kStageBytes + u * Sm::kHalf;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) copy_async16(dst + value_place<D>(512 / D * j + tok, piece), p + 512 * j);
+      }
     }
     copy_commit();
   };
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) issue(i);
+  for (int i = 0; i < kStages; ++i) {
+    issue_keys(i);
+    if (i < kValueStages) issue_values(i, k_off);
+  }
 
   // row g of each 8: its operand fragments; rows 2 t4, + 1: power of two and position
   uint32_t qf[NT][4 * kC][2];
@@ -193,12 +214,11 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
     for (int j = 0; j < 2; ++j) m[nt][j] = n[nt][j] = -INFINITY, l[nt][j] = 0.0f;
 
   for (int i = 0; i < steps; ++i) {
-    copy_wait<kStages - 2>();
-    __syncwarp();                    // every lane's copies of this step are here; the last step has been read
-    issue(i + kStages - 1);
+    copy_wait<kStages + kValueStages - 1>();
+    __syncwarp();                    // every lane's copies of this step's keys are here
     const int key = first_key + i * kStep * kWarps, stage = i % kStages;
     const uint32_t src = ring + stage * kStageBytes;
-    const uint32_t skip = skipped >> (2 * stage) & 3u;
+    const uint32_t skip = skipped >> (2 * stage) & 3u;   // before the stage takes another step's keys
 
     float s[2][NT][4] = {};          // keys g, g + 8 of a half by rows 2 t4, + 1
 #pragma unroll
@@ -219,6 +239,8 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
       }
 
     const uint4 sc = lds128(scales + stage * kStageScales);
+    __syncwarp();                    // the keys and scales have been read
+    issue_keys(i + kStages);
     const float coef[2] = {a.scale_log2 * __uint_as_float(sc.x), a.scale_log2 * __uint_as_float(sc.z)};
     const float lsv[2] = {lg2(__uint_as_float(sc.y)), lg2(__uint_as_float(sc.w))};
     const bool all = skip == 0 && key + kStep - 1 <= t.pos_lo && (a.window == 0 || key > t.pos_hi - a.window);
@@ -284,12 +306,14 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[nt][j][e] *= alpha[nt][e & 1];
     }
+    copy_wait<kStages + kValueStages - 1>();
+    __syncwarp();                    // and this step's values
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       uint32_t vw[4][D / 32];        // tokens 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9, dimensions g D/8 ..
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t r = 2 * t4 + (k & 1) + 8 * (k >> 1), at = src + (2 + u) * Sm::kHalf;
+        const uint32_t r = 2 * t4 + (k & 1) + 8 * (k >> 1), at = ring + (kStages + i % kValueStages) * kStageBytes + u * Sm::kHalf;
         if constexpr (D == 128) {
           const uint4 w = lds128(at + value_place<D>(r, g));
           vw[k][0] = w.x ^ 0x80808080u, vw[k][1] = w.y ^ 0x80808080u;
@@ -314,6 +338,8 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
         }
       }
     }
+    __syncwarp();                    // the values have been read
+    issue_values(i + kValueStages, v_off);
   }
 
   // join the lanes' sums and then the warps
@@ -379,8 +405,8 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? 12 : 8) / kWarps) kv_a
   if (d0 == 0) *reinterpret_cast<float4*>(a.part_stat + slot * 4) = make_float4(mm, nn, ll, 0.0f);
 }
 
-// Joins the splits of one row per thread block: the warps take interleaved splits and are then
-// added in order.
+// Joins the splits of one row per thread block: the warps take interleaved splits, each relative to its own
+// maxima, and are then added in order.
 constexpr int kJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs a) {
@@ -388,48 +414,44 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
   const int h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z, row = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   Tile t;
-  if (!attn_tile(a, b, rt, t)) return;
-  const int ns = tile_splits(a, t), r = t.r0 + row;
+  const bool in = attn_tile(a, b, rt, t);
+  asm volatile("griddepcontrol.wait;" ::: "memory");         // the parts are there
+  const int ns = in ? tile_splits(a, t) : 0, r = t.r0 + row;
   if (ns <= 1 || r >= t.rows) return;
   const int64_t slot0 = (((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits) * a.tile_rows + row;
-  const float4* stat = reinterpret_cast<const float4*>(a.part_stat) + slot0;
-  float m = -INFINITY, n = -INFINITY;
-  for (int s = lane; s < ns; s += 32) {
-    const float4 v = stat[static_cast<int64_t>(s) * a.tile_rows];
-    m = fmaxf(m, v.x);
-    n = fmaxf(n, v.y);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, o));
-  }
-  const float base = finite_max(m), nbase = finite_max(n);
-  float acc[kPer] = {}, l = 0.0f;
+  float m = -INFINITY, n = -INFINITY, acc[kPer] = {}, l = 0.0f;
 #pragma unroll 4
   for (int s = warp; s < ns; s += warps) {
-    const float4 v = stat[static_cast<int64_t>(s) * a.tile_rows];
-    const float f = ex2(v.x - base);
-    const float* p = a.part + (slot0 + static_cast<int64_t>(s) * a.tile_rows) * D + lane * kPer;
-    l = fmaf(v.z, ex2(v.y - nbase), l);
+    const int64_t slot = slot0 + static_cast<int64_t>(s) * a.tile_rows;
+    const float4 v = *reinterpret_cast<const float4*>(a.part_stat + 4 * slot);
+    const float* p = a.part + slot * D + lane * kPer;
+    const float m1 = fmaxf(m, v.x), n1 = fmaxf(n, v.y);
+    const float keep = ex2(m - finite_max(m1)), f = ex2(v.x - finite_max(m1));
+    l = fmaf(l, ex2(n - finite_max(n1)), v.z * ex2(v.y - finite_max(n1)));
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) {
       const float2 x = *reinterpret_cast<const float2*>(p + e);
-      acc[e] = fmaf(x.x, f, acc[e]), acc[e + 1] = fmaf(x.y, f, acc[e + 1]);
+      acc[e] = fmaf(acc[e], keep, x.x * f), acc[e + 1] = fmaf(acc[e + 1], keep, x.y * f);
     }
+    m = m1;
+    n = n1;
   }
-  __shared__ float part[kJoinWarps][D + 1];
+  __shared__ float part[kJoinWarps][D + 3];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) part[warp][lane * kPer + e] = acc[e];
-  if (lane == 0) part[warp][D] = l;
+  if (lane == 0) part[warp][D] = m, part[warp][D + 1] = n, part[warp][D + 2] = l;
   __syncthreads();
   if (threadIdx.x >= D / 2) return;
+  m = n = -INFINITY;
+  for (int w = 0; w < warps; ++w) m = fmaxf(m, part[w][D]), n = fmaxf(n, part[w][D + 1]);
+  const float base = finite_max(m), nbase = finite_max(n);
   float o0 = 0.0f, o1 = 0.0f;
   l = 0.0f;
   for (int w = 0; w < warps; ++w) {
-    o0 += part[w][2 * threadIdx.x];
-    o1 += part[w][2 * threadIdx.x + 1];
-    l += part[w][D];
+    const float f = ex2(part[w][D] - base);
+    o0 = fmaf(part[w][2 * threadIdx.x], f, o0);
+    o1 = fmaf(part[w][2 * threadIdx.x + 1], f, o1);
+    l = fmaf(part[w][D + 2], ex2(part[w][D + 1] - nbase), l);
   }
   const float inv = out_factor(l, base - nbase);
   uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
@@ -453,19 +475,28 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
                         : a.tile_rows == 8         ? launch_split<D, 1>(a, stream)
                                                    : launch_split<D, 2>(a, stream);
   if (e != cudaSuccess || a.splits <= 1) return e;
-  const int warps = a.splits >= 4 * kJoinWarps ? kJoinWarps : a.splits >= 8 ? kJoinWarps / 2 : 2;   // >= D / 64
-  const dim3 join(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs);
-  kv_attn_join_kernel<D><<<join, 32 * warps, 0, stream>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs);
+  cfg.blockDim = dim3(32 * (a.splits > 4 ? kJoinWarps : kJoinWarps / 2));   // at least D / 2 threads
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its blocks line up behind the last splits
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kv_attn_join_kernel<D>, a);
 }
 
 }  // namespace
 
 // Up to 16 rows per sequence and key/value head the keys' bytes bound the call, and 8- or 16-row tiles of
 // the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
-// all of them.  The keys are cut so that the tiles of the largest batch the bounds allow fill the
-// machine about four (prompt kernel: two) times over, so that ragged sequences even out, in pieces of at
-// least 128 keys, one step of each warp (prompt kernel: four tiles of 128 keys).
+// all of them.  The keys of a tile are cut so that the tiles of the largest batch the bounds allow fill the
+// machine about twice, in pieces of at least 128 keys (a step of each warp; prompt kernel: 512), or 4096
+// where the tiles alone fill it: a piece costs about 3 us beside its keys, the start and the join.  Measured,
+// 32 query and 8 key/value heads of 128: two sequences of 131002 tokens 93 us (79 for the bytes at the copy
+// rate; cut four times as fine 104, half as fine 89), 64 ragged sequences up to 8101 tokens 92 us (66; 84,
+// 114), one of 1030 tokens 6.0 us; 16 x 5 rows of 40 full heads, window 2048, 41 us (30).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
@@ -478,7 +509,8 @@ void plan_attn(AttnArgs& a, int sms) {
     keys = keys < w ? keys : w;
   }
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
-  const int64_t want = static_cast<int64_t>(sms) * (prompt ? 2 : kWantPerSm), unit = 128, least = prompt ? 512 : 128;
+  const int64_t want = static_cast<int64_t>(sms) * (prompt ? 2 : kCutPerSm), unit = 128;
+  const int64_t least = prompt ? 512 : tiles >= static_cast<int64_t>(sms) * (a.tile_rows == 8 ? kPerSm : kPerSm / 2) ? 4096 : 128;
   int64_t chunk = (keys * tiles + want - 1) / want;
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk < least) chunk = least;

@@ -77,11 +77,12 @@ class KVCache(ctypes.Structure):
     def of(cls, k_codes, v_codes, k_scale, v_scale) -> "KVCache":
         """`k_codes`, `v_codes`: int8 [n_blocks, n_kv_heads, block, head_dim]; `k_scale`, `v_scale`: fp32
         [n_blocks, n_kv_heads]; all dense.  The cache keeps the tensors alive."""
-        for t, shape in ((k_codes, k_codes.shape), (v_codes, k_codes.shape), (k_scale, k_codes.shape[:2]),
-                         (v_scale, k_codes.shape[:2])):
-            if t.shape != shape or not t.is_contiguous():
-                raise LrqatError(-1, "cache tensors must be dense and of matching shapes")
-        n_blocks, heads, block, d = k_codes.shape
+        shape = k_codes.shape
+        if (len(shape) != 4 or v_codes.shape != shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]
+                or not (k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
+                        and v_scale.is_contiguous())):
+            raise LrqatError(-1, "cache tensors must be dense and of matching shapes")
+        n_blocks, heads, block, d = shape
         cache = cls(n_blocks, heads, d, block, _ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale))
         cache.tensors = (k_codes, v_codes, k_scale, v_scale)
         return cache
@@ -304,9 +305,10 @@ def act_dequant(norm: Norm, T: int, codes, s, X_hat, stream=None) -> None:
 
 def _rows(t, heads: int, d: int) -> int:
     """Distance in elements of consecutive rows of a [rows, heads, head_dim] tensor or view."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d or stride[2] != 1 or (heads > 1 and stride[1] != d):
         raise LrqatError(-1, f"rows of {heads} heads by {d} expected, dense within a row")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * d)
+    return stride[0] if shape[0] > 1 else max(stride[0], heads * d)
 
 
 def kv_write(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:
@@ -330,7 +332,8 @@ def kv_attn_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window
 def kv_attn(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, O, workspace, stream=None) -> None:
     """Causal attention of the batch's rows Q over the cache into O, both bf16 [rows, n_heads, head_dim]."""
     nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    heads, d = Q.shape[1] if Q.dim() == 3 else 0, cache.head_dim
+    shape, d = Q.shape, cache.head_dim
+    heads = shape[1] if len(shape) == 3 else 0
     _check(lib().lrqat_kv_attn(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, _ptr(Q),
                                _rows(Q, heads, d), _ptr(O), _rows(O, heads, d), _ptr(workspace), nbytes,
                                _stream(stream)))
