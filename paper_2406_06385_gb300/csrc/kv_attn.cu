@@ -23,7 +23,6 @@ constexpr int kWarps = 4;
 constexpr int kStep = kKeyAlign;   // keys of one step of a warp, in two halves of 16
 constexpr int kStages = 2, kValueStages = 1;   // steps of keys and of values in a warp's ring
 constexpr int kPerSm = 16 / kWarps;        // thread blocks an SM holds (with 16 rows: half of them)
-constexpr int kCutPerSm = 2 * kPerSm;      // and blocks per SM that the keys are cut into
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                           const uint32_t (&b)[2]) {
@@ -492,11 +491,12 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 // Up to 16 rows per sequence and key/value head the keys' bytes bound the call, and 8- or 16-row tiles of
 // the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
 // all of them.  The keys of a tile are cut so that the tiles of the largest batch the bounds allow fill the
-// machine about twice, in pieces of at least 128 keys (a step of each warp; prompt kernel: 512), or 4096
-// where the tiles alone fill it: a piece costs about 3 us beside its keys, the start and the join.  Measured,
-// 32 query and 8 key/value heads of 128: two sequences of 131002 tokens 93 us (79 for the bytes at the copy
-// rate; cut four times as fine 104, half as fine 89), 64 ragged sequences up to 8101 tokens 92 us (66; 84,
-// 114), one of 1030 tokens 6.0 us; 16 x 5 rows of 40 full heads, window 2048, 41 us (30).
+// machine about twice, or four times where there are many tiles (many sequences, whose lengths differ), in
+// pieces of at least 128 keys (a step of each warp; prompt kernel: 512), or 4096 where the tiles alone fill
+// it: a piece costs about 3 us beside its keys, the start and the join.  Measured, 32 query and 8 key/value
+// heads of 128: two sequences of 131002 tokens 93 us (79 for the bytes at the copy rate; cut twice as fine
+// 100, half as fine 89), 64 ragged sequences up to 8101 tokens 85 us (66; half as fine 92, a quarter 114),
+// one of 1030 tokens 6.0 us; 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in four 49).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
@@ -509,8 +509,9 @@ void plan_attn(AttnArgs& a, int sms) {
     keys = keys < w ? keys : w;
   }
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
-  const int64_t want = static_cast<int64_t>(sms) * (prompt ? 2 : kCutPerSm), unit = 128;
-  const int64_t least = prompt ? 512 : tiles >= static_cast<int64_t>(sms) * (a.tile_rows == 8 ? kPerSm : kPerSm / 2) ? 4096 : 128;
+  const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
+  const int64_t want = at_once * (prompt || 4 * tiles < at_once ? 2 : 4);
+  const int64_t unit = 128, least = prompt ? 512 : tiles >= at_once ? 4096 : 128;
   int64_t chunk = (keys * tiles + want - 1) / want;
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk < least) chunk = least;
