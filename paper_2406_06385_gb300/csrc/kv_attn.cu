@@ -103,10 +103,9 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   int next_blk[2] = {block_of(first_key), block_of(first_key + 16)};
   uint32_t skipped = 0;              // bit 2 s + u: half u of the step in stage s has no valid block
   const uint32_t piece = lane % (D / 16), tok = lane / (D / 16);            // a copy instruction covers 512 / D tokens
-  // where the keys copied last lie, and those before them: the values that are copied next
-  int64_t k_off[2] = {-1, -1}, v_off[2] = {-1, -1};
-  static_assert(kStages == 2 && kValueStages == 1, "the values' offsets run one step behind the keys'");
-  // keys and scales of step i, and (later) its values: each stage is refilled as soon as it has been read
+  int64_t off[2] = {-1, -1};         // where the keys copied last lie: the values that are copied next
+  static_assert(kStages == 2 && kValueStages == 1, "order of the copies: keys 0, values 0, keys 1, values 1, keys 2, ...");
+  // the keys and scales of step i, then its values
   auto issue_keys = [&](int i) {
     if (i < steps) {
       const int key = first_key + i * kStep * kWarps, stage = i % kStages;
@@ -115,13 +114,12 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
         const int blk = next_blk[u];
         next_blk[u] = block_of(key + kStep * kWarps + 16 * u);
         const uint32_t bit = 1u << (2 * stage + u);
-        v_off[u] = k_off[u];
-        k_off[u] = -1;
+        off[u] = -1;
         if (static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks)) {
           skipped &= ~bit;
           const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
-          k_off[u] = ((at << a.kv.block_log2) + ((key + 16 * u) & in_block)) * D + lane * 16;
-          const int8_t* p = a.kv.codes[0] + k_off[u];
+          off[u] = ((at << a.kv.block_log2) + ((key + 16 * u) & in_block)) * D + lane * 16;
+          const int8_t* p = a.kv.codes[0] + off[u];
           const uint32_t dst = ring + stage * kStageBytes + u * Sm::kHalf;
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) copy_async16(dst + key_place<D>(512 / D * j + tok, piece), p + 512 * j);
@@ -132,12 +130,10 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
           if (lane == 0 && blk != -2) atomicOr(a.kv.status, kStatusRange);
         }
       }
-    } else {
-      v_off[0] = k_off[0], v_off[1] = k_off[1];
     }
     copy_commit();
   };
-  auto issue_values = [&](int i, const int64_t (&off)[2]) {
+  auto issue_values = [&](int i) {
     if (i < steps) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -150,11 +146,9 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
     }
     copy_commit();
   };
-#pragma unroll
-  for (int i = 0; i < kStages; ++i) {
-    issue_keys(i);
-    if (i < kValueStages) issue_values(i, k_off);
-  }
+  issue_keys(0);
+  issue_values(0);
+  issue_keys(1);
 
   // row g of each 8: its operand fragments; rows 2 t4, + 1: power of two and position
   uint32_t qf[NT][4 * kC][2];
@@ -213,7 +207,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
     for (int j = 0; j < 2; ++j) m[nt][j] = n[nt][j] = -INFINITY, l[nt][j] = 0.0f;
 
   for (int i = 0; i < steps; ++i) {
-    copy_wait<kStages + kValueStages - 1>();
+    copy_wait<2>();                  // in flight: this step's values and the next one's keys
     __syncwarp();                    // every lane's copies of this step's keys are here
     const int key = first_key + i * kStep * kWarps, stage = i % kStages;
     const uint32_t src = ring + stage * kStageBytes;
@@ -238,8 +232,6 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
       }
 
     const uint4 sc = lds128(scales + stage * kStageScales);
-    __syncwarp();                    // the keys and scales have been read
-    issue_keys(i + kStages);
     const float coef[2] = {a.scale_log2 * __uint_as_float(sc.x), a.scale_log2 * __uint_as_float(sc.z)};
     const float lsv[2] = {lg2(__uint_as_float(sc.y)), lg2(__uint_as_float(sc.w))};
     const bool all = skip == 0 && key + kStep - 1 <= t.pos_lo && (a.window == 0 || key > t.pos_hi - a.window);
@@ -305,7 +297,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[nt][j][e] *= alpha[nt][e & 1];
     }
-    copy_wait<kStages + kValueStages - 1>();
+    copy_wait<1>();                  // in flight: the next step's keys
     __syncwarp();                    // and this step's values
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -337,8 +329,9 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
         }
       }
     }
-    __syncwarp();                    // the values have been read
-    issue_values(i + kValueStages, v_off);
+    __syncwarp();                    // the step has been read
+    issue_values(i + 1);
+    issue_keys(i + 2);
   }
 
   // join the lanes' sums and then the warps
@@ -494,9 +487,9 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 // machine about twice, or four times where there are many tiles (many sequences, whose lengths differ), in
 // pieces of at least 128 keys (a step of each warp; prompt kernel: 512), or 4096 where the tiles alone fill
 // it: a piece costs about 3 us beside its keys, the start and the join.  Measured, 32 query and 8 key/value
-// heads of 128: two sequences of 131002 tokens 93 us (79 for the bytes at the copy rate; cut twice as fine
+// heads of 128: two sequences of 131002 tokens 91 us (79 for the bytes at the copy rate; cut twice as fine
 // 100, half as fine 89), 64 ragged sequences up to 8101 tokens 85 us (66; half as fine 92, a quarter 114),
-// one of 1030 tokens 6.0 us; 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in four 49).
+// one of 1030 tokens 6.0 us; 16 x 5 rows of 40 full heads, window 2048, 40 us (30; cut in four 49).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;

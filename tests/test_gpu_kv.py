@@ -290,6 +290,35 @@ def test_infinite_and_nan_queries_stay_in_their_rows():
     assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], ref[~hit])
 
 
+@pytest.mark.parametrize("seqs,heads,group,block,window", [
+    ([(1030, 1)], 8, 4, 16, 0), ([(40000, 1), (33000, 1)], 8, 4, 32, 0), ([(9000, 4), (5000, 4)], 8, 4, 64, 0),
+    ([(3000, 5)] * 3, 16, 1, 16, 2048), ([(6000, 1)] * 6 + [(200, 1)] * 6, 8, 1, 128, 0), ([(4000, 300)], 4, 4, 64, 0)])
+def test_results_do_not_depend_on_where_the_cache_lies(seqs, heads, group, block, window):
+    """The same bits whether the cache comes from memory (a buffer larger than the L2 cache was written before) or
+    from L2, and close to float64: no copy is used before it has arrived."""
+    t = torch()
+    p = Paged(seqs, heads, 128, block, seed=15)
+    vals = _fill(p)
+    bits, q = p.random_rows(heads * group)
+    Q, batch = to_dev(bits), p.batch()
+    junk = t.empty(1 << 28, dtype=t.float32, device="cuda")
+    out = []
+    for i in range(6):
+        if i < 4:
+            junk.fill_(float(i))
+        out.append(_attn(p, batch, Q, 0.1, window, heads * group))
+    LQ.get_device_status()
+    assert all(t.equal(o, out[0]) for o in out)
+    got = bits_to_f32(out[0]).astype(np.float64)
+    at = 0
+    for b, (length, n) in enumerate(seqs):
+        row = slice(at + n - 1, at + n)                     # the newest row of each sequence
+        at += n
+        ref, mass, seen = SO.attention(q[row], *vals[b], length, 0.1, window)
+        bound = 2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * mass + (seen[:, None, None] * 2.0 ** -25) * np.abs(vals[b][1]).max()
+        assert (np.abs(got[row] - ref) <= bound).all()
+
+
 def test_strided_rows_other_streams_and_graphs():
     """Q and O as parts of wider rows; the call on a side stream; a captured call replayed for other lengths within the
     captured bounds."""
