@@ -469,7 +469,7 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
   if (e != cudaSuccess || a.splits <= 1) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs);
-  cfg.blockDim = dim3(32 * (a.splits > 4 ? kJoinWarps : kJoinWarps / 2));   // at least D / 2 threads
+  cfg.blockDim = dim3(32 * (a.splits > 32 ? kJoinWarps : a.splits > 8 ? kJoinWarps / 2 : 2));   // at least D / 2 threads
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its blocks line up behind the last splits

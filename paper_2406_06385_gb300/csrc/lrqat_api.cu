@@ -678,7 +678,7 @@ int attn_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t 
                 cache->n_kv_heads);
   if (window < 0) return fail(LRQAT_ERR_INVALID_ARG, "window must be >= 0");
   a->group = n_heads / cache->n_kv_heads;
-  a->window = window;
+  a->window = window < a->kv.max_len ? window : 0;   // a window as long as the sequences hides nothing
   plan_attn(*a, sm_count());
   if (static_cast<int64_t>(a->kv.max_rows) * a->group > (1 << 24) ||
       static_cast<int64_t>(a->kv.heads) * a->row_tiles > 65535 ||

@@ -143,13 +143,14 @@ __device__ __forceinline__ float2 warp_sum2(float2 v) {
 // and mean(g h) are reduced together.  The next kBwdStages rows are on their way into shared memory
 // meanwhile; a thread copies, waits for and reads its own words only, so no barrier guards them, and
 // registers hold nothing but the sums.  What bounds it is the chain load, sums, exchange, gradient of a row
-// against three blocks an SM: 16384 rows of 5120 with dH in 123 us, 5.5 TB/s (rows held in registers with the
+// against three blocks an SM: 16384 rows of 5120 with dH in 122 us, 5.5 TB/s (rows held in registers with the
 // next one prefetched: 135 us, without prefetch 130; three or four stages leave room for two blocks: 129, 170).
 constexpr int kBwdStages = 2;
 constexpr int kBwdSmem = 200 * 1024, kSmemPerSm = 220 * 1024;  // most shared memory of a block, of an SM's blocks
 template <int V>
 __global__ void __launch_bounds__(512, V == 4 ? 1 : 2) add_rmsnorm_bwd_kernel(NormBwdArgs a, int wpr) {
   extern __shared__ uint4 words[];                             // [stage][H, dY, dH][V][thread]
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the sum of dgamma may line up
   __shared__ float2 red[2][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wr = warp / wpr;
@@ -251,17 +252,17 @@ __global__ void __launch_bounds__(512, V == 4 ? 1 : 2) add_rmsnorm_bwd_kernel(No
 // dgamma[j] = sum of part[.][j] in a fixed order: a block owns 8 float4 columns, its 32 row lanes add
 // interleaved rows and a fixed tree adds the lanes.
 constexpr int kSumRows = 32;
-__global__ void __launch_bounds__(8 * kSumRows) dgamma_sum_kernel(const float4* __restrict__ part, int64_t np,
-                                                                  int64_t k4, float4* __restrict__ out,
-                                                                  int accumulate) {
+__global__ void __launch_bounds__(8 * kSumRows) dgamma_sum_kernel(const float4* part, int64_t np, int64_t k4,
+                                                                  float4* out, int accumulate) {
   __shared__ float4 red[kSumRows][8];
+  asm volatile("griddepcontrol.wait;" ::: "memory");           // the partial sums are there
   const int row = threadIdx.x >> 3, col = threadIdx.x & 7;
   const int64_t j = static_cast<int64_t>(blockIdx.x) * 8 + col;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   if (j < k4) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t p = row; p < np; p += kSumRows) {
-      const float4 v = part[p * k4 + j];
+      const float4 v = __ldcg(part + p * k4 + j);               // written while this grid may already be waiting
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
     }
   }
@@ -391,10 +392,17 @@ cudaError_t launch_add_rmsnorm_bwd(const NormBwdArgs& a, int sms, cudaStream_t s
                                    : launch_bwd<4>(a, p.rs.wpr, grid, threads, p.smem, stream);
   if (e != cudaSuccess || !a.dgamma) return e;
   const int64_t k4 = a.k / 4;
-  dgamma_sum_kernel<<<static_cast<unsigned>((k4 + 7) / 8), 8 * kSumRows, 0, stream>>>(
-      reinterpret_cast<const float4*>(a.part), p.grid * p.rs.rpb, k4, reinterpret_cast<float4*>(a.dgamma),
-      a.accumulate);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>((k4 + 7) / 8));
+  cfg.blockDim = dim3(8 * kSumRows);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, dgamma_sum_kernel, reinterpret_cast<const float4*>(a.part),
+                            static_cast<int64_t>(p.grid * p.rs.rpb), k4, reinterpret_cast<float4*>(a.dgamma), a.accumulate);
 }
 
 cudaError_t launch_act_dequant(const int8_t* codes, const float* scale, int64_t T, int64_t k, uint16_t* x_hat,

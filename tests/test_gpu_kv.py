@@ -216,6 +216,30 @@ def test_attention(seqs, heads, group, d, block, window):
     assert t.equal(O, _attn(p, p.batch(), to_dev(bits), scale, window, heads * group))
 
 
+@pytest.mark.parametrize("new", [1, 40])
+def test_windows_as_long_as_the_sequences_hide_nothing(new):
+    t = torch()
+    p = Paged([(300, new), (77, new)], 2, 128, 16, seed=16)
+    vals = _fill(p)
+    bits, q = p.random_rows(8)
+    O = _attn(p, p.batch(), to_dev(bits), 0.1, 0, 8)
+    _check(p, vals, O, q, 0.1, 0)
+    for window in (300, 301, 2 ** 31 - 1):
+        assert t.equal(O, _attn(p, p.batch(), to_dev(bits), 0.1, window, 8))
+
+
+def test_many_short_sequences():
+    """Hundreds of sequences of all small lengths, a third of them idle slots."""
+    rng = np.random.default_rng(17)
+    seqs = [(0, 1) if i % 3 == 2 else (int(rng.integers(1, 70)), 1) for i in range(400)]
+    p = Paged(seqs, 4, 64, 16, seed=17)
+    vals = _fill(p)
+    bits, q = p.random_rows(8)
+    O = _attn(p, p.batch(), to_dev(bits), 0.2, 0, 8)
+    LQ.get_device_status()
+    _check(p, vals, O, q, 0.2, 0)
+
+
 @pytest.mark.parametrize("seqs", [[(700, 1), (40, 1)], [(300, 150)]])
 def test_attention_with_scales_far_apart(seqs):
     """Blocks whose scales lie many orders of magnitude apart: values as large as 1e20 behind negligible weights, tiny

@@ -171,6 +171,20 @@ def test_backward(T, k, dh):
     assert np.array_equal(acc.cpu().numpy(), start + dgamma.cpu().numpy())
 
 
+@pytest.mark.parametrize("T,k", [(70, 4096), (700, 1024)])
+def test_gradient_may_be_written_in_place(T, k):
+    t = torch()
+    d = _inputs(T, k, 13, ["dY", "dH", "H", "gamma"])
+    dX, dgamma = _bwd(d, T, k)
+    norm = LQ.Norm(k, EPS, 8)
+    ws = empty((LQ.add_rmsnorm_bwd_workspace_bytes(norm, T),), t.uint8)
+    for over in ("dY", "dH"):
+        dev = {n: to_dev(v[0]) for n, v in d.items()}
+        again = empty((k,), t.float32)
+        LQ.add_rmsnorm_bwd(norm, T, dev["dY"], dev["dH"], dev["H"], dev["gamma"], dev[over], again, False, ws)
+        assert t.equal(dev[over], dX) and t.equal(again, dgamma), over
+
+
 def test_backward_against_differences():
     """<dY, y> changes along a direction v by <dX, v>: central differences of the float64 norm at the bf16 inputs; dX
     in bf16 keeps 2^-9 of each of its elements."""
