@@ -10,8 +10,9 @@
 //                    read from tensor memory.  A half has two score buffers: while its softmax works on
 //                    one, the tensor cores fill the other;
 //   softmax warps    one thread per row: maximum, P = 2^{z' - m} as halves back into tensor memory, over
-//                    the scores they came from.  m moves only when a row's maximum has grown by more than
-//                    2^8 (P <= 256 is exact enough in half precision and fits), so O is rarely rescaled.
+//                    the scores they came from.  m is the maximum of the first keys a row sees; it moves (and O
+//                    is rescaled) only when a sum of P has grown beyond what half precision holds, so that
+//                    most steps look for no maximum at all.
 // Scores and O live in tensor memory: 2 x 2 x 64 and 2 x d columns.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -34,7 +35,7 @@ constexpr int kThreads = 32 * (kMmaWarp + 4);                // four warpgroups;
 // Registers a thread of each role: over the warpgroups their sum is what the block is launched with.
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 184, kProducerRegs = 104, kMmaRegs = 40;
 static_assert(2 * kSoftmaxRegs + kProducerRegs + kMmaRegs <= 4 * kLaunchRegs, "registers of the warpgroups");
-constexpr float kLazy = 8.0f;                // how far a maximum may run ahead of m
+constexpr float kMostP = 32768.0f;           // largest sum of 16 P before m follows the maximum
 constexpr float kTame = 64.0f;               // how far log2 of the value scales may lie from the first one's
 
 enum : int {
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       // 2^{ref - log2 s_v}, which the producers prepare.  Once a scale lies more than 2^kTame away from the first
       // (a weight of -1), P may vanish where a term of the denominator does not: from then on it is l 2^n, summed
       // from exponentials of its own relative to the running maximum n.
-      float m = -INFINITY, n = 0.0f, l = 0.0f;
+      float m = in ? -INFINITY : 0.0f, n = 0.0f, l = 0.0f;
       bool wild = false, ok = true;
       float s[2][32], coef[4], lsv[4], weight[4];
       // scores and scales of step i
@@ -257,90 +258,102 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
           for (int c = 0; c < kStepKeys; ++c)
             if (c > c_hi || c < c_lo) s[c / 32][c % 32] = -INFINITY;
         }
-        float g[4], mx = -INFINITY;                      // the largest score of a group, the largest z' of the row
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float* v = &s[u / 2][16 * (u % 2)];
-          float g0 = max3(v[0], v[1], v[2]), g1 = max3(v[3], v[4], v[5]);
-          g0 = max3(g0, v[6], v[7]), g1 = max3(g1, v[8], v[9]);
-          g0 = max3(g0, v[10], v[11]), g1 = max3(g1, v[12], v[13]);
-          g[u] = max3(g0, g1, fmaxf(v[14], v[15]));
-          mx = fmaxf(mx, fmaf(g[u], coef[u], lsv[u]));
-        }
-        const float m1 = mx > m + kLazy || m == -INFINITY ? fmaxf(m, mx) : m;
-        if (__any_sync(0xffffffffu, m1 != m)) {
-          const float alpha = ex2(m - finite_max(m1));
-          if (!wild) l *= alpha;
-          if (i > 0) {
-            ok = wait_bounded(bar(B_OFULL + half), (i - 1) & 1u, ctl, 3);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            tc_fence_after();
+        if (fminf(fminf(weight[0], weight[1]), fminf(weight[2], weight[3])) < 0.0f || wild) {
+          const uint32_t slot = smem + Sm::kScale + ((i >> 1) % kScaleSlots) * Sm::kSlot + 16 * sub;
+          const float was = wild ? n : finite_max(m) - ld_shared_f32(smem + Sm::kScale + kScaleSlots * Sm::kSlot);
+          wild = true;
+          float n1 = l == 0.0f ? -INFINITY : was;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
-              float o[16];
-              uint32_t w[16];
-              tmem_ld16(t_o + c, o);
+          for (int turn = 0; turn < 2; ++turn) {         // the largest z, then the sum
+#pragma unroll 1
+            for (int u = 0; u < 4; ++u) {
+              const float cu = ld_shared_f32(slot + 4 * u) * qs;
+              const bool block = ld_shared_f32(slot + 4 * kGroups + 4 * u) != -INFINITY;
+              float x[16];
+              tmem_ld16(t_p + 16 * u, x);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * alpha);
-              tmem_st16(t_o + c, w);
-            }
-          }
-          m = m1;
-        }
-        const float base = finite_max(m);
-        if (fminf(fminf(weight[0], weight[1]), fminf(weight[2], weight[3])) < 0.0f || wild) {
-          const float ref = ld_shared_f32(smem + Sm::kScale + kScaleSlots * Sm::kSlot);
-          float zx = -INFINITY;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) zx = fmaxf(zx, g[u] * coef[u]);
-          const float was = wild ? n : base - ref, n1 = l == 0.0f ? zx : fmaxf(was, zx), nbase = finite_max(n1);
-          l = l == 0.0f ? 0.0f : l * ex2(was - nbase);
-          n = nbase;
-          wild = true;
-#pragma unroll 1
-          for (int u = 0; u < 4; ++u) {
-            const uint32_t slot = smem + Sm::kScale + ((i >> 1) % kScaleSlots) * Sm::kSlot + 16 * sub + 4 * u;
-            const float cu = ld_shared_f32(slot) * qs, lv = ld_shared_f32(slot + 4 * kGroups);
-            float x[16];
-            tmem_ld16(t_p + 16 * u, x);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {               // hidden keys and groups without a block add nothing
-              const bool seen = lv != -INFINITY && (all || (16 * u + e <= c_hi && 16 * u + e >= c_lo));
-              l += seen ? ex2(fmaf(x[e], cu, -nbase)) : 0.0f;
-            }
-          }
-        }
-        float part[4];                                   // a group's sum of P
-        auto weights = [&](auto masked) {
-#pragma unroll
-          for (int c = 0; c < kStepKeys; c += 32) {
-            uint32_t p[16];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const float cu = coef[c / 16 + u], du = lsv[c / 16 + u] - base;
-              const float* v = &s[c / 32][16 * u];
-              float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-              for (int e = 0; e < 16; e += 2) {
-                float2 x = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(cu, cu), make_float2(du, du));
-                if (decltype(masked)::value) {           // a coefficient of 0 or NaN must not bring a hidden key back
-                  x.x = v[e] == -INFINITY ? -INFINITY : x.x;
-                  x.y = v[e + 1] == -INFINITY ? -INFINITY : x.y;
-                }
-                x.x = ex2(x.x);
-                x.y = ex2(x.y);
-                sum = __fadd2_rn(sum, x);
-                p[8 * u + e / 2] = pack_half(x.x, x.y);
+              for (int e = 0; e < 16; ++e) {             // hidden keys and groups without a block add nothing
+                const bool seen = block && (all || (16 * u + e <= c_hi && 16 * u + e >= c_lo));
+                if (turn == 0) n1 = seen ? fmaxf(n1, x[e] * cu) : n1;
+                else l += seen ? ex2(fmaf(x[e], cu, -n)) : 0.0f;
               }
-              part[c / 16 + u] = sum.x + sum.y;
             }
-            tmem_st16(t_p + c / 2, p);
+            if (turn == 0) {
+              n = finite_max(n1);
+              l = l == 0.0f ? 0.0f : l * ex2(was - n);
+            }
           }
-        };
-        if (all) weights(Flag<false>{});
-        else weights(Flag<true>{});
+        }
+        // P relative to the m so far.  The row's maximum is only looked for where there is none yet, or where a sum of
+        // P shows that scores have outrun m beyond what half precision holds.
+        float part[4], base;                             // a group's sum of P
+        bool look = __any_sync(0xffffffffu, m == -INFINITY);
+#pragma unroll 1
+        for (int turn = 0; turn < 2; ++turn) {
+          if (look) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float* v = &s[u / 2][16 * (u % 2)];
+              float g0 = max3(v[0], v[1], v[2]), g1 = max3(v[3], v[4], v[5]);
+              g0 = max3(g0, v[6], v[7]), g1 = max3(g1, v[8], v[9]);
+              g0 = max3(g0, v[10], v[11]), g1 = max3(g1, v[12], v[13]);
+              mx = fmaxf(mx, fmaf(max3(g0, g1, fmaxf(v[14], v[15])), coef[u], lsv[u]));
+            }
+            const float m1 = fmaxf(m, mx), alpha = ex2(m - finite_max(m1));
+            if (!wild) l *= alpha;
+            if (i > 0) {
+              ok = wait_bounded(bar(B_OFULL + half), (i - 1) & 1u, ctl, 3);
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                float o[16];
+                uint32_t w[16];
+                tmem_ld16(t_o + c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * alpha);
+                tmem_st16(t_o + c, w);
+              }
+            }
+            m = m1;
+          }
+          base = finite_max(m);
+          auto weights = [&](auto masked) {
+#pragma unroll
+            for (int c = 0; c < kStepKeys; c += 32) {
+              uint32_t p[16];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const float cu = coef[c / 16 + u], du = lsv[c / 16 + u] - base;
+                const float* v = &s[c / 32][16 * u];
+                float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                  float2 x = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(cu, cu), make_float2(du, du));
+                  if (decltype(masked)::value) {         // a coefficient of 0 or NaN must not bring a hidden key back
+                    x.x = v[e] == -INFINITY ? -INFINITY : x.x;
+                    x.y = v[e + 1] == -INFINITY ? -INFINITY : x.y;
+                  }
+                  x.x = ex2(x.x);
+                  x.y = ex2(x.y);
+                  sum = __fadd2_rn(sum, x);
+                  p[8 * u + e / 2] = pack_half(x.x, x.y);
+                }
+                part[c / 16 + u] = sum.x + sum.y;
+              }
+              tmem_st16(t_p + c / 2, p);
+            }
+          };
+          if (all) weights(Flag<false>{});
+          else weights(Flag<true>{});
+          look = __any_sync(0xffffffffu, fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) > kMostP);
+          if (!look) break;
+        }
+        if (!ok) break;
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
