@@ -38,7 +38,7 @@ __device__ __forceinline__ float2 warp_sum_max(float2 v) {
 // max|h gamma|; rounding is monotone, so max|y| = fl(R max|h gamma|) exactly and no second
 // exchange is needed.  Bound by memory: what counts is loads in flight, so the fewest threads a row
 // (four words each) and as many rows at once as 64 registers a thread allow.  16384 rows of 5120 with
-// residual: 99.6 us, 6.74 TB/s; with two words a thread 115 us, with one 150 us.
+// residual: 99.3 us, 6.76 TB/s; with two words a thread 115 us, with one 150 us.
 template <int V>
 __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsnorm_fwd_kernel(NormFwdArgs a, int wpr) {
   __shared__ float2 red[32];
@@ -131,11 +131,13 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsno
 
 __device__ __forceinline__ float2 warp_sum2(float2 v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-  }
+  for (int o = 16; o > 0; o >>= 1)
+    v = __fadd2_rn(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
   return v;
+}
+__device__ __forceinline__ void unpack4x2(const uint4& v, float2 (&x)[4]) {
+  x[0] = make_float2(bf16_lo(v.x), bf16_hi(v.x)), x[1] = make_float2(bf16_lo(v.y), bf16_hi(v.y));
+  x[2] = make_float2(bf16_lo(v.z), bf16_hi(v.z)), x[3] = make_float2(bf16_lo(v.w), bf16_hi(v.w));
 }
 
 // A row group takes rows t, t + stride, ...; its threads keep the dgamma sums of their
@@ -143,8 +145,10 @@ __device__ __forceinline__ float2 warp_sum2(float2 v) {
 // and mean(g h) are reduced together.  The next kBwdStages rows are on their way into shared memory
 // meanwhile; a thread copies, waits for and reads its own words only, so no barrier guards them, and
 // registers hold nothing but the sums.  What bounds it is the chain load, sums, exchange, gradient of a row
-// against three blocks an SM: 16384 rows of 5120 with dH in 122 us, 5.5 TB/s (rows held in registers with the
-// next one prefetched: 135 us, without prefetch 130; three or four stages leave room for two blocks: 129, 170).
+// against three blocks an SM, and its instructions (packed pairs and rsqrtf, within two units in the last
+// place of 32 bits, count: 122 us with scalars and a division by the root): 16384 rows of 5120 with dH in
+// 116 us, 5.8 TB/s, the sum of dgamma included (rows held in registers with the next one prefetched: 12 us
+// more, without prefetch 7; three or four stages leave room for two blocks: 6, 47 more).
 constexpr int kBwdStages = 2;
 constexpr int kBwdSmem = 200 * 1024, kSmemPerSm = 220 * 1024;  // most shared memory of a block, of an SM's blocks
 template <int V>
@@ -177,11 +181,11 @@ __global__ void __launch_bounds__(512, V == 4 ? 1 : 2) add_rmsnorm_bwd_kernel(No
     }
     copy_commit();
   };
-  float acc[V][8];
+  float2 acc[V][4];
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[i][e] = 0.0f;
+    for (int e = 0; e < 4; ++e) acc[i][e] = make_float2(0.0f, 0.0f);
 #pragma unroll
   for (int i = 0; i < kBwdStages; ++i) load(i, group + i * stride);
   int turn = 0;
@@ -190,50 +194,50 @@ __global__ void __launch_bounds__(512, V == 4 ? 1 : 2) add_rmsnorm_bwd_kernel(No
     const int64_t t = t0 + wr, base = t * k8;
     const int stage = turn % kBwdStages, ph = turn & 1;
     copy_wait<kBwdStages - 1>();
-    float2 sm = make_float2(0.0f, 0.0f);
+    float2 hh = make_float2(0.0f, 0.0f), gh = hh;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int j = sub + nthr * i;
       const bool in = t < a.T && j < k8;
-      float h[8], y[8], g[8];
-      unpack8(in ? *word(stage, 0, i) : zero, h);
-      unpack8(in ? *word(stage, 1, i) : zero, y);
-      unpack8(in ? __ldg(G + j) : zero, g);
+      float2 h[4], y[4], g[4];
+      unpack4x2(in ? *word(stage, 0, i) : zero, h);
+      unpack4x2(in ? *word(stage, 1, i) : zero, y);
+      unpack4x2(in ? __ldg(G + j) : zero, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sm.x = fmaf(h[e], h[e], sm.x);
-        sm.y = fmaf(y[e] * g[e], h[e], sm.y);
+      for (int e = 0; e < 4; ++e) {
+        hh = __ffma2_rn(h[e], h[e], hh);
+        gh = __ffma2_rn(__fmul2_rn(y[e], g[e]), h[e], gh);
       }
     }
-    sm = warp_sum2(sm);
+    float2 sm = warp_sum2(make_float2(hh.x + hh.y, gh.x + gh.y));
     if (wpr > 1) {
       if (lane == 0) red[ph][warp] = sm;
       __syncthreads();
       sm = make_float2(0.0f, 0.0f);
-      for (int w = 0; w < wpr; ++w) {
-        const float2 o = red[ph][wr * wpr + w];
-        sm.x += o.x;
-        sm.y += o.y;
-      }
+#pragma unroll 4
+      for (int w = 0; w < wpr; ++w) sm = __fadd2_rn(sm, red[ph][wr * wpr + w]);
     }
     if (t < a.T) {
-      const float rstd = 1.0f / sqrtf(sm.x * inv_k + a.eps);
-      const float c = rstd * rstd * (sm.y * inv_k);
+      const float rstd = rsqrtf(sm.x * inv_k + a.eps);
+      const float c = -rstd * (rstd * rstd * (sm.y * inv_k));
+      const float2 rstd2 = make_float2(rstd, rstd), c2 = make_float2(c, c);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int j = sub + nthr * i;
         if (j >= k8) break;
-        float h[8], y[8], g[8], d[8];
-        unpack8(*word(stage, 0, i), h);
-        unpack8(*word(stage, 1, i), y);
-        unpack8(a.dH ? *word(stage, 2, i) : zero, d);
-        unpack8(__ldg(G + j), g);
+        float2 h[4], y[4], g[4], d[4];
+        unpack4x2(*word(stage, 0, i), h);
+        unpack4x2(*word(stage, 1, i), y);
+        unpack4x2(a.dH ? *word(stage, 2, i) : zero, d);
+        unpack4x2(__ldg(G + j), g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          acc[i][e] = fmaf(y[e], h[e] * rstd, acc[i][e]);
-          d[e] = fmaf(rstd, y[e] * g[e] - h[e] * c, d[e]);
+        for (int e = 0; e < 4; ++e) {
+          acc[i][e] = __ffma2_rn(y[e], __fmul2_rn(h[e], rstd2), acc[i][e]);
+          d[e] = __ffma2_rn(rstd2, __fmul2_rn(y[e], g[e]), __ffma2_rn(c2, h[e], d[e]));
         }
-        reinterpret_cast<uint4*>(a.dX)[base + j] = pack8(d);
+        reinterpret_cast<uint4*>(a.dX)[base + j] =
+            make_uint4(pack_bf16(d[0].x, d[0].y), pack_bf16(d[1].x, d[1].y), pack_bf16(d[2].x, d[2].y),
+                       pack_bf16(d[3].x, d[3].y));
       }
     }
     load(stage, t + kBwdStages * stride);
@@ -244,8 +248,8 @@ __global__ void __launch_bounds__(512, V == 4 ? 1 : 2) add_rmsnorm_bwd_kernel(No
     const int j = sub + nthr * i;
     if (j >= k8) break;
     float4* dst = reinterpret_cast<float4*>(a.part + group * a.k) + 2 * j;
-    dst[0] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-    dst[1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+    dst[0] = make_float4(acc[i][0].x, acc[i][0].y, acc[i][1].x, acc[i][1].y);
+    dst[1] = make_float4(acc[i][2].x, acc[i][2].y, acc[i][3].x, acc[i][3].y);
   }
 }
 
