@@ -7,8 +7,9 @@
 // maximum, P_j = 2^{z'_j - m} lies in [0, 1] and is what a key contributes to o, whatever the scales
 // of the blocks are.  The denominator, the sum of P_j / s_v, is kept relative to a running
 // maximum n of its own, that of z_j log2(e): scales of one sequence may lie as far apart as fp32 reaches.
-// So P fits 11-bit half precision and the codes (|c| <= 128) are exact in it; a row of q is first divided by the power of two of its largest
-// magnitude, which half precision also holds (exact but for elements below 2^-14 of the largest).
+// So P fits 11-bit half precision and the codes (|c| <= 128) are exact in it; a row of q is first divided
+// by the power of two of its largest magnitude, which half precision also holds (exact but for elements
+// below 2^-14 of the largest).
 // Scores, maxima, sums and outputs are 32-bit.
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -76,6 +77,8 @@ struct SplitSmem {
 // transpose per 8 keys turns scores into the second product's operand.  The order of the dimensions
 // inside a product is free: each lane takes 16 consecutive bytes of a token.  A step's codes come
 // through a ring in shared memory filled by the warp that reads it: warps never wait for one another.
+// Bound by the copies in flight (48 KB a block, four blocks an SM) and, close behind, by issue slots (58%
+// in use, half of them for turning codes into halves): 64 ragged sequences at 72% of the memory's rate.
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv_attn_split_kernel(AttnArgs a) {
   using Sm = SplitSmem<D, NT>;
@@ -485,11 +488,14 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 // the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
 // all of them.  The keys of a tile are cut so that the tiles of the largest batch the bounds allow fill the
 // machine about twice, or four times where there are many tiles (many sequences, whose lengths differ), in
-// pieces of at least 128 keys (a step of each warp; prompt kernel: 512), or 4096 where the tiles alone fill
-// it: a piece costs about 3 us beside its keys, the start and the join.  Measured, 32 query and 8 key/value
-// heads of 128: two sequences of 131002 tokens 91 us (79 for the bytes at the copy rate; cut twice as fine
-// 100, half as fine 89), 64 ragged sequences up to 8101 tokens 85 us (66; half as fine 92, a quarter 114),
-// one of 1030 tokens 6.0 us; 16 x 5 rows of 40 full heads, window 2048, 40 us (30; cut in four 49).
+// pieces of at least 128 keys (a step of each warp; prompt kernel: 512).  A piece costs about 3 us beside its
+// keys, the start and the join, so tiles that fill the machine by themselves are cut into 4096 keys or more
+// (8-row tiles that fill it less than twice, whose last wave is far from full: 2304), and up to 1024 keys
+// stay whole where tiles fill half of it.  Measured, 8 key/value heads of 128: two sequences of 131002
+// tokens 91 us (79 for the bytes at the copy rate; cut twice as fine 100, half as fine 89), 64 ragged
+// sequences up to 8101 tokens 81 us (66; half as fine 93, a quarter 115), one of 1030 tokens 6.1 us, 64 of
+// 1001 tokens 28 us (cut in four 36), 100 of 4001 tokens 140 us (whole 150), 200 of 2501 tokens 158 us (cut
+// in two 172); 16 x 5 rows of 40 full heads, window 2048, 40 us (30; cut in four 48).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
@@ -504,7 +510,10 @@ void plan_attn(AttnArgs& a, int sms) {
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
   const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
   const int64_t want = at_once * (prompt || 4 * tiles < at_once ? 2 : 4);
-  const int64_t unit = 128, least = prompt ? 512 : tiles >= at_once ? 4096 : 128;
+  const int64_t unit = 128;
+  int64_t least = prompt ? 512 : 128;
+  if (!prompt && tiles >= at_once) least = a.tile_rows == 8 && tiles < 2 * at_once ? 2304 : 4096;
+  else if (!prompt && 2 * tiles >= at_once && keys <= 1024) least = 1024;
   int64_t chunk = (keys * tiles + want - 1) / want;
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk < least) chunk = least;

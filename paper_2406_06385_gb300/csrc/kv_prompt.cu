@@ -14,6 +14,14 @@
 //                    is rescaled) only when a sum of P has grown beyond what half precision holds, so that
 //                    most steps look for no maximum at all.
 // Scores and O live in tensor memory: 2 x 2 x 64 and 2 x d columns.
+//
+// Four prompts of up to 4000 tokens behind 500 older ones, 32 query and 8 key/value heads of 128: 524 us,
+// 971 TFLOP/s, 51% of the rate of a plain product.  Bound by the softmax warps: a tile of 256 rows and 128
+// keys takes about 3700 cycles, its matrix instructions 2033; without the softmax's arithmetic the call
+// would take 407 us, without the producers' stores 479, almost without matrix instructions still 505.  Start
+// and end of a block cost 17000 cycles of its about 90000.  Measured against it: two threads a row 686 (the
+// exchange of their maxima), one 128-key score buffer 834, persistent blocks that load the next rows' q
+// early 709, eight producer warps with 136 softmax registers 574.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cstdint>
