@@ -85,13 +85,20 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   constexpr int kC = D / 64;         // 64-dimension pieces of a token
   constexpr int kRows = 8 * NT;
   extern __shared__ __align__(16) uint8_t smem[];
-  const int split = blockIdx.x, h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z;
+  const int h = blockIdx.x % a.kv.heads, rt = blockIdx.x / a.kv.heads, b = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Tile t;
   if (!attn_tile(a, b, rt, t)) return;
+  // Whole pieces first, every tile's shorter one (or its piece number a.splits - 1) in the end, where it fills
+  // gaps: 20 ragged sequences of up to 5000 tokens with 40 heads 103 -> 97 us, 90 of up to 3000 with 8 heads
+  // 65 -> 60, 64 of up to 8100 no faster (82 -> 83).
   const int ns = tile_splits(a, t);
-  if (split > 0 && split >= ns) return;
+  const bool last = blockIdx.z + 1 == gridDim.z;
+  const int split = last ? max(ns - 1, 0) : static_cast<int>(blockIdx.z);
+  if (last ? ns > 0 && ns < a.splits && (t.hi - t.lo) % a.chunk == 0
+           : (split + 1) * static_cast<int64_t>(a.chunk) > t.hi - t.lo)
+    return;
   const int k0 = t.lo + split * a.chunk, k1 = min(t.hi, k0 + a.chunk);
 
   const uint32_t ring = smem_addr(smem) + warp * Sm::kWarpStage;
@@ -456,7 +463,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
 template <int D, int NT>
 cudaError_t launch_split(const AttnArgs& a, cudaStream_t stream) {
   using Sm = SplitSmem<D, NT>;
-  const dim3 grid(a.splits, a.kv.heads * a.row_tiles, a.kv.n_seqs);
+  const dim3 grid(a.kv.heads * a.row_tiles, a.kv.n_seqs, a.splits);
   static bool smem_set[kMaxDevices];
   const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT>), Sm::kBytes, smem_set);
   if (e != cudaSuccess) return e;
@@ -492,10 +499,10 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 // keys, the start and the join, so tiles that fill the machine by themselves are cut into 4096 keys or more
 // (8-row tiles that fill it less than twice, whose last wave is far from full: 2304), and up to 1024 keys
 // stay whole where tiles fill half of it.  Measured, 8 key/value heads of 128: two sequences of 131002
-// tokens 91 us (79 for the bytes at the copy rate; cut twice as fine 100, half as fine 89), 64 ragged
-// sequences up to 8101 tokens 81 us (66; half as fine 93, a quarter 115), one of 1030 tokens 6.1 us, 64 of
-// 1001 tokens 28 us (cut in four 36), 100 of 4001 tokens 140 us (whole 150), 200 of 2501 tokens 158 us (cut
-// in two 172); 16 x 5 rows of 40 full heads, window 2048, 40 us (30; cut in four 48).
+// tokens 91 us (79 for the bytes at the copy rate; cut twice as fine 100), 64 ragged sequences up to 8101
+// tokens 83 us (66; in five pieces at most, in two 90, whole 116, in sixteen 88), one of 1030 tokens 6.1 us,
+// 64 of 1001 tokens 28 us (cut in four 36), 100 of 4001 tokens 137 us (whole 151), 200 of 2501 tokens 162 us
+// (cut in two 171); 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in two 48).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
