@@ -240,6 +240,20 @@ def test_many_short_sequences():
     _check(p, vals, O, q, 0.2, 0)
 
 
+@pytest.mark.parametrize("longest", [2048, 2049, 2000])
+@pytest.mark.parametrize("new,window", [(1, 0), (2, 0), (1, 1024)])
+def test_sequences_that_end_where_pieces_do(longest, new, window):
+    """Lengths at, before and behind the ends of the pieces that the keys are cut into (multiples of 128 and
+    256 here), next to idle slots and to a longest sequence with and without a short last piece."""
+    lens = [n for m in (128, 256, 512, 1024, 1920) for n in (m - 1, m, m + 1)] + [new, longest]
+    p = Paged([(n, new) for n in lens] + [(0, new)], 1, 128, 16, seed=longest + new)
+    vals = _fill(p)
+    bits, q = p.random_rows(4)
+    O = _attn(p, p.batch(), to_dev(bits), 0.1, window, 4)
+    LQ.get_device_status()
+    _check(p, vals, O, q, 0.1, window)
+
+
 @pytest.mark.parametrize("seqs", [[(700, 1), (40, 1)], [(300, 150)]])
 def test_attention_with_scales_far_apart(seqs):
     """Blocks whose scales lie many orders of magnitude apart: values as large as 1e20 behind negligible weights, tiny
