@@ -156,6 +156,18 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
     }
     copy_commit();
   };
+  // q is asked for ahead of the ring's bytes, which would keep it waiting
+  uint4 qw[NT][kC][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = t.r0 + 8 * nt + g;
+    const uint16_t* q = a.Q + (t.seq.row0 + r / a.group) * a.ldq + static_cast<int64_t>(h * a.group + r % a.group) * D;
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        qw[nt][c][u] = r < t.rows ? __ldg(reinterpret_cast<const uint4*>(q + 64 * c + 16 * t4) + u) : make_uint4(0u, 0u, 0u, 0u);
+  }
   issue_keys(0);
   issue_values(0);
   issue_keys(1);
@@ -166,17 +178,13 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   int pos[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = t.r0 + 8 * nt + g;
-    const int tk = r / a.group;
-    const bool in = r < t.rows;
-    const uint16_t* q = a.Q + (t.seq.row0 + tk) * a.ldq + static_cast<int64_t>(h * a.group + r % a.group) * D;
     float x[kC][16], top = 0.0f;
 #pragma unroll
     for (int c = 0; c < kC; ++c)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         float v[8];
-        unpack8(in ? __ldg(reinterpret_cast<const uint4*>(q + 64 * c + 16 * t4) + u) : make_uint4(0u, 0u, 0u, 0u), v);
+        unpack8(qw[nt][c][u], v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[c][8 * u + e] = v[e];
