@@ -507,10 +507,12 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 // keys, the start and the join, so tiles that fill the machine by themselves are cut into 4096 keys or more
 // (8-row tiles that fill it less than twice, whose last wave is far from full: 2304), and up to 1024 keys
 // stay whole where tiles fill half of it.  Measured, 8 key/value heads of 128: two sequences of 131002
-// tokens 91 us (79 for the bytes at the copy rate; cut twice as fine 100), 64 ragged sequences up to 8101
+// tokens 88 us (79 for the bytes at the copy rate; cut twice as fine 92), 64 ragged sequences up to 8101
 // tokens 83 us (66; in five pieces at most, in two 90, whole 116, in sixteen 88), one of 1030 tokens 6.1 us,
 // 64 of 1001 tokens 28 us (cut in four 36), 100 of 4001 tokens 137 us (whole 151), 200 of 2501 tokens 162 us
-// (cut in two 171); 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in two 48).
+// (cut in two 171); 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in two 48).  Where all pieces
+// are of one length they come in one wave: one sequence of 32001 tokens 20 us (two waves 24, 10 for its
+// bytes), 4 drafted tokens behind 32000 24 us (31), 12 windows of 1000 tokens 10.6 us (12).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
@@ -530,6 +532,9 @@ void plan_attn(AttnArgs& a, int sms) {
   if (!prompt && tiles >= at_once) least = a.tile_rows == 8 && tiles < 2 * at_once ? 2304 : 4096;
   else if (!prompt && 2 * tiles >= at_once && keys <= 1024) least = 1024;
   int64_t chunk = (keys * tiles + want - 1) / want;
+  // one or two sequences, or windows shorter than the sequences: pieces of equal length, so one wave of them
+  if (!prompt && 2 * tiles <= at_once && (a.kv.n_seqs <= 2 || 2 * keys <= a.kv.max_len))
+    chunk = (keys + at_once / tiles - 1) / (at_once / tiles);
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk < least) chunk = least;
   if (prompt && tiles >= want) chunk = (keys + unit) / unit * unit;
