@@ -77,13 +77,14 @@ class KVCache(ctypes.Structure):
     def of(cls, k_codes, v_codes, k_scale, v_scale) -> "KVCache":
         """`k_codes`, `v_codes`: int8 [n_blocks, n_kv_heads, block, head_dim]; `k_scale`, `v_scale`: fp32
         [n_blocks, n_kv_heads]; all dense.  The cache keeps the tensors alive."""
-        shape = k_codes.shape
-        if (len(shape) != 4 or v_codes.shape != shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]
+        shape, scales = k_codes.shape, k_scale.shape
+        if (len(shape) != 4 or v_codes.shape != shape or scales != shape[:2] or v_scale.shape != scales
                 or not (k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
                         and v_scale.is_contiguous())):
             raise LrqatError(-1, "cache tensors must be dense and of matching shapes")
         n_blocks, heads, block, d = shape
-        cache = cls(n_blocks, heads, d, block, _ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale))
+        cache = cls(n_blocks, heads, d, block, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(),
+                    v_scale.data_ptr())
         cache.tensors = (k_codes, v_codes, k_scale, v_scale)
         return cache
 
@@ -102,7 +103,8 @@ class KVBatch(ctypes.Structure):
         if (lens.shape != (n_seqs,) or row_start.shape != (n_seqs + 1,)
                 or not (lens.is_contiguous() and row_start.is_contiguous() and block_table.is_contiguous())):
             raise LrqatError(-1, "lens, row_start and block_table must be dense, of n_seqs, n_seqs + 1 and n_seqs rows")
-        batch = cls(n_seqs, max_blocks, _ptr(lens), _ptr(row_start), _ptr(block_table), rows, max_rows, max_len)
+        batch = cls(n_seqs, max_blocks, lens.data_ptr(), row_start.data_ptr(), block_table.data_ptr(), rows, max_rows,
+                    max_len)
         batch.tensors = (lens, row_start, block_table)
         return batch
 
@@ -186,11 +188,16 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_torch_c = None
+
+
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    from torch import _C
-    return _C._cuda_getCurrentRawStream(_C._cuda_getDevice())   # a tenth of torch.cuda.current_stream()'s time
+    global _torch_c
+    if _torch_c is None:
+        from torch import _C as _torch_c
+    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())   # a tenth of current_stream()'s time
 
 
 def last_error() -> str:
