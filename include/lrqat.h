@@ -269,8 +269,8 @@ int lrqat_merge(const lrqat_layer* layer, const void* Phi0, const uint16_t* A, c
  *   s = max|y| / 127 (1 for a row of zeros),  c = round(y / s),  y_hat = s c.
  * Everything between the inputs and the rounded outputs is fp32 (y is not rounded to
  * bf16 before the quantizer, as it is where lrqat_act_quant reads a stored y).  A row
- * that holds a NaN or an infinity, or whose sum of squares overflows fp32, gets a NaN
- * scale.  k: a multiple of 8, at most 16384. */
+ * that holds a NaN or an infinity in h or in h gamma, or in which the sum of squares, h gamma
+ * or y overflows fp32, gets a NaN scale.  k: a multiple of 8, at most 16384. */
 typedef struct {
   int64_t k;
   float eps;        /* >= 0                                              */

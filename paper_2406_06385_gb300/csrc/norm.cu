@@ -28,7 +28,7 @@ __device__ __forceinline__ float2 warp_sum_max(float2 v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y = fmaxf(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
+    v.y = max_nan(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
   }
   return v;
 }
@@ -79,10 +79,9 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsno
     }
     if (a.H && in) reinterpret_cast<uint4*>(a.H)[base + j] = pack8(hg[i]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      hg[i][e] *= gg[e];
-      sm.y = fmaxf(sm.y, fabsf(hg[i][e]));
-    }
+    for (int e = 0; e < 8; ++e) hg[i][e] *= gg[e];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) sm.y = max3_abs_nan(sm.y, hg[i][e], hg[i][e + 1]);
   }
   sm = warp_sum_max(sm);
   if (wpr > 1) {
@@ -92,7 +91,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsno
     for (int w = 0; w < wpr; ++w) {
       const float2 o = red[wr * wpr + w];
       sm.x += o.x;
-      sm.y = fmaxf(sm.y, o.y);
+      sm.y = max_nan(sm.y, o.y);
     }
   }
   if (!live) return;
@@ -107,8 +106,10 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsno
     }
     return;
   }
-  // a row with a NaN or an infinity has rstd NaN or 0 and max|y| NaN: its scale is NaN
-  const float amax = isfinite(sm.x) ? sm.y * rstd : __int_as_float(0x7FFFFFFF);
+  // a NaN or an infinity in h (the sum is not finite) or in h gamma (the maximum, which keeps a NaN, is not)
+  // makes the scale NaN, so that the codes, which cannot say so, read back as NaN
+  const float top = sm.y * rstd;
+  const float amax = isfinite(sm.x) && isfinite(top) ? top : __int_as_float(0x7FFFFFFF);
   const float s = amax == 0.0f ? 1.0f : __fdiv_rn(amax, 127.0f);
   const float inv = __frcp_rn(s);
   if (sub == 0 && a.s_y) a.s_y[t] = s;

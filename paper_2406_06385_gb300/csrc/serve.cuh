@@ -27,7 +27,12 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 // leaves that integer, in two's complement, in the low bits of the sum.
 constexpr float kRoundMagic = 12582912.0f;
 
-// max(|a|, |b|, |c|), NaN if one of them is.
+// max(a, b) and max(|a|, |b|, |c|), NaN if one of them is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float max3_abs_nan(float a, float b, float c) {
   float r;
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));

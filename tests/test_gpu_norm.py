@@ -213,3 +213,23 @@ def test_calls_run_on_the_stream_they_are_given():
     LQ.add_rmsnorm_fwd(LQ.Norm(k, EPS, 8), T, X, R, gamma, H2, Y2, None, s2, stream=side)
     side.synchronize()
     assert t.equal(Y, Y2) and t.equal(s, s2)
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("T,k", [(1, 4096), (5, 264), (400, 1000), (7, 5120), (2, 8200)])
+def test_a_weight_that_is_not_finite_poisons_every_row(T, k, bad):
+    """gamma holds a NaN or an infinity: every row's scale is NaN, so the values, written at once or rebuilt from the
+    codes, are NaN alike (0 times infinity included); without the quantizer only that column is lost."""
+    t = torch()
+    d = _inputs(T, k, 21, ["X", "R", "gamma"])
+    j = k - 3
+    bits = {n: v[0].copy() for n, v in d.items()}
+    bits["gamma"][j] = {True: 0x7FC0, False: 0x7F80 if bad > 0 else 0xFF80}[bool(np.isnan(bad))]
+    bits["X"][T - 1, j] = bits["R"][T - 1, j] = 0
+    _, Y, q, s = _fwd(bits, LQ.Norm(k, EPS, 8), T, k, True, "Yqs")
+    back = empty((T, k), t.int16)
+    LQ.act_dequant(LQ.Norm(k, EPS, 8), T, q, s, back)
+    assert np.isnan(s.cpu().numpy()).all() and np.isnan(bits_to_f32(Y)).all() and np.isnan(bits_to_f32(back)).all()
+    assert np.isnan(_fwd(bits, LQ.Norm(k, EPS, 8), T, k, True, "qs")[3].cpu().numpy()).all()
+    plain = bits_to_f32(_fwd(bits, LQ.Norm(k, EPS, 0), T, k, True, "Y")[1])
+    assert not np.isfinite(plain[:, j]).any() and np.isfinite(np.delete(plain, j, 1)).all()
