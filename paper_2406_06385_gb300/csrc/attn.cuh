@@ -30,7 +30,8 @@ __device__ __forceinline__ float lg2(float x) {
   return y;
 }
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
-// 2^up / l, 0 for a row that saw no key (l = 0); up = m - n is at most log2 of the largest scale.
+// 2^up / l, 0 for a row that saw no key (l = 0); up = m - n is at most log2 of the largest scale, and -infinity
+// where every value scale that the row saw is 0.
 __device__ __forceinline__ float out_factor(float l, float up) {
   const float half = ex2(0.5f * up);                   // 2^up itself may be subnormal
   return l == 0.0f ? 0.0f : half / l * half;

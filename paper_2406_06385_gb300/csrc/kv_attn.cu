@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
     }
   }
   if (ns <= 1) {
-    const float inv = out_factor(ll, base - nbase);
+    const float inv = out_factor(ll, mm - nbase);
     uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D + d0;
 #pragma unroll
     for (int e = 0; e < kPer; e += 4)
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
     o1 = fmaf(part[w][2 * threadIdx.x + 1], f, o1);
     l = fmaf(part[w][D + 2], ex2(part[w][D + 1] - nbase), l);
   }
-  const float inv = out_factor(l, base - nbase);
+  const float inv = out_factor(l, m - nbase);
   uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
   reinterpret_cast<uint32_t*>(out)[threadIdx.x] = pack_bf16(o0 * inv, o1 * inv);
 }

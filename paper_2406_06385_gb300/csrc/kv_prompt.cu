@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       if (ok) {
         const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) +
                              128 * half + r_in;
-        const float f = ns <= 1 ? out_factor(l, finite_max(m) - n) : 1.0f;
+        const float f = ns <= 1 ? out_factor(l, m - n) : 1.0f;
         uint16_t* out = a.O + (t.seq.row0 + tok) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {

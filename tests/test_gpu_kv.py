@@ -473,3 +473,17 @@ def _restore(p, vals):
         i = codes[:, 0].abs().argmax(1)
         h = t.arange(p.heads, device="cuda")
         p.scale[kv][blk] = (v[h, i] / codes[h, 0, i]).float()
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+@pytest.mark.parametrize("length", [100, 5000])
+def test_values_that_are_all_zero_give_zero_whatever_the_scores(new, length):
+    """Every visible value scale is 0 and every score lies hundreds of powers of two below 0."""
+    p = Paged([(length, new)], 2, 128, 16, seed=21)
+    _fill(p, lambda kv, used, scale: scale * np.float32(kv == 0))
+    p.codes[0].clamp_(min=1)
+    bits, q = p.random_rows(4)
+    bits |= 0x8000                                         # every element of q is negative
+    O = _attn(p, p.batch(), to_dev(bits), 300.0, 0, 4)
+    LQ.get_device_status()
+    assert (bits_to_f32(O) == 0).all()
