@@ -312,8 +312,9 @@ int lrqat_act_dequant(const lrqat_norm* norm, int64_t T, const int8_t* codes, co
 /* ---- 8-bit key / value cache (the KV8 of the W4A8KV8 runs, Sec. 4) ----------------
  * A pool of blocks of `block` tokens.  Codes are int8 [n_blocks, n_kv_heads, block,
  * head_dim], with one fp32 scale per block and head, [n_blocks, n_kv_heads]:
- * value = scale * code.  A block belongs to one sequence while it is written (several
- * sequences may read it); nothing has to be cleared before its first use. */
+ * value = scale * code; a scale may be 0 (a block of zeros quantized elsewhere).  A block
+ * belongs to one sequence while it is written (several sequences may read it); nothing has
+ * to be cleared before its first use. */
 typedef struct {
   int64_t n_blocks;
   int32_t n_kv_heads;

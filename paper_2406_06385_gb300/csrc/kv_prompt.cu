@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
 #pragma unroll 1
             for (int u = 0; u < 4; ++u) {
               const float cu = ld_shared_f32(slot + 4 * u) * qs;
-              const bool block = ld_shared_f32(slot + 4 * kGroups + 4 * u) != -INFINITY;
+              const bool block = ld_shared_f32(slot + 8 * kGroups + 4 * u) != 0.0f;   // weight 0: no block
               float x[16];
               tmem_ld16(t_p + 16 * u, x);
               tmem_ld_wait();
@@ -479,7 +479,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
         const float v = blk >= 0 ? lg2(sv) : -INFINITY, away = ref - v;
         st_shared_f32(at, blk >= 0 ? fabsf(a.scale_log2) * sk : 0.0f);
         st_shared_f32(at + 4 * kGroups, v);
-        // NaN: its P are NaN themselves where they are seen
+        // 0: no block; NaN: its P are NaN themselves where they are seen; a value scale of 0 is an infinity away:
+        // its keys add nothing to O and their share to the denominator
         st_shared_f32(at + 8 * kGroups, blk < 0 ? 0.0f : away != away ? 1.0f : fabsf(away) < kTame ? ex2(away) : -1.0f);
       }
       store(kr, smem + Sm::kK + stage * Sm::kOperand);

@@ -487,3 +487,21 @@ def test_values_that_are_all_zero_give_zero_whatever_the_scores(new, length):
     O = _attn(p, p.batch(), to_dev(bits), 300.0, 0, 4)
     LQ.get_device_status()
     assert (bits_to_f32(O) == 0).all()
+
+
+@pytest.mark.parametrize("new", [1, 6, 40, 300])
+def test_blocks_with_a_value_scale_of_zero_count_in_the_denominator(new):
+    """A cache that was quantized elsewhere may hold blocks of zeros with scale 0: their keys take their share of the
+    softmax and their values add nothing, whichever kernel the number of rows leads to."""
+    p = Paged([(300, new), (47, min(new, 47))], 2, 128, 16, seed=20)
+
+    def zeros(kv, used, scale):
+        if kv == 1:
+            scale[::2] = 0.0
+        return scale
+
+    vals = _fill(p, zeros)
+    bits, q = p.random_rows(4)
+    O = _attn(p, p.batch(), to_dev(bits), 0.1, 0, 4)
+    LQ.get_device_status()
+    _check(p, vals, O, q, 0.1, 0)
