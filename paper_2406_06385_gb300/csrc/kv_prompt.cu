@@ -44,7 +44,10 @@ constexpr int kThreads = 32 * (kMmaWarp + 4);                // four warpgroups;
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 184, kProducerRegs = 104, kMmaRegs = 40;
 static_assert(2 * kSoftmaxRegs + kProducerRegs + kMmaRegs <= 4 * kLaunchRegs, "registers of the warpgroups");
 constexpr float kMostP = 32768.0f;           // largest sum of 16 P before m follows the maximum
-constexpr float kTame = 64.0f;               // how far log2 of the value scales may lie from the first one's
+// How far log2 of the value scales may lie from the first one's for P to serve the denominator too.  Against m, which a
+// key behind the largest of them may set, P of a key behind the smallest is 2^{-2 kTame} times its share e^z, and P is
+// zero below 2^-126: 62 powers of two are left for the share, 31 for the number of keys and 31 for a sum's bits.
+constexpr float kTame = 32.0f;
 
 enum : int {
   B_QFULL = 0, B_KFULL = 2, B_VFULL = 4, B_KEMPTY = 6, B_VEMPTY = 8, B_SFULL = 10, B_PFULL = 14, B_OFULL = 18,
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
       const uint32_t t_s = tmem + lanes + 128u * half, t_o = tmem + lanes + 256u + D * half;
       // The denominator is l 2^{m - ref} with ref = log2 of the first value scale: a group's P count with weight
-      // 2^{ref - log2 s_v}, which the producers prepare.  Once a scale lies more than 2^kTame away from the first
+      // 2^{ref - log2 s_v}, which the producers prepare.  Once a scale lies 2^kTame or more away from the first
       // (a weight of -1), P may vanish where a term of the denominator does not: from then on it is l 2^n, summed
       // from exponentials of its own relative to the running maximum n.
       float m = in ? -INFINITY : 0.0f, n = 0.0f, l = 0.0f;

@@ -505,3 +505,30 @@ def test_blocks_with_a_value_scale_of_zero_count_in_the_denominator(new):
     O = _attn(p, p.batch(), to_dev(bits), 0.1, 0, 4)
     LQ.get_device_status()
     _check(p, vals, O, q, 0.1, 0)
+
+
+@pytest.mark.parametrize("seqs", [[(700, 1), (40, 1)], [(300, 150)], [(2000, 70)]])
+def test_value_scales_on_both_sides_of_the_first_one(seqs):
+    """Blocks 2^63 above and 2^63 below the first one's scale of about 1: the small ones carry as much of the
+    denominator as the large ones.  Bound: as for scales far apart."""
+    p = Paged(seqs, 2, 128, 16, seed=22)
+
+    def both(kv, used, scale):
+        if kv == 0:
+            return scale
+        slot = {int(i): n for n, i in enumerate(used)}
+        for ids in p.blocks:
+            for j, i in enumerate(ids):
+                scale[slot[i]] = 1.0 if j == 0 else 2.0 ** (63 if j % 2 else -63) * p.rng.uniform(0.6, 0.9)
+        return scale
+
+    vals = _fill(p, both)
+    bits, q = p.random_rows(4)
+    O = _attn(p, p.batch(), to_dev(bits), 0.1, 0, 4)
+    LQ.get_device_status()
+    got = bits_to_f32(O).astype(np.float64)
+    for b, length, n, at in _seq_rows(p.seqs):
+        ref, mass, seen = SO.attention(q[at], *vals[b], length, 0.1)
+        z = 0.1 * np.abs(np.einsum("nhd,lhd->nhl", q[at].astype(np.float64), np.repeat(vals[b][0], 2, 1))).max()
+        bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + (z + 100) * 2.0 ** -21 + seen[:, None, None] * 2.0 ** -18) * mass.max(2, keepdims=True)
+        assert (np.abs(got[at] - ref) <= bound).all()
