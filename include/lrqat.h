@@ -347,8 +347,9 @@ typedef struct {
 
 /* Quantizes the batch's new keys and values into the cache.  For each block and head, with a the
  * largest magnitude among the block's new tokens:
- *   a block that starts with a new token takes scale s = a / 127 (1 if a = 0);
- *   one that holds older tokens takes s = max(its scale, a / 127), and where that grew the older
+ *   a block that starts with a new token, or whose older tokens are all zeros, takes scale
+ *   s = a / 127 (1 if a = 0);
+ *   one that holds other older tokens takes s = max(its scale, a / 127), and where that grew the older
  *   codes become round(c * (old scale / s));
  *   new codes are round(x / s).
  * Divisions are fp32; a block that takes a NaN or an infinity gets a NaN scale.  Writing the same

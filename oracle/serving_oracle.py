@@ -53,7 +53,10 @@ class Cache:
                 a = np.float32(np.abs(rows).max())
                 fresh = np.float32(a / np.float32(127.0)) if np.isfinite(a) else np.float32(np.nan)
                 was = self.scale[blk, h]
-                if old:
+                zeros = was == 0 or (was == 1 and not self.codes[blk, h, :old].any())    # nothing but zeros so far
+                if zeros:
+                    self.codes[blk, h, :old] = 0
+                if old and not zeros:
                     s = was if (was >= fresh or np.isnan(was)) else fresh
                     if s > was:
                         c = self.codes[blk, h, :old].astype(np.float32) * np.float32(was / s)

@@ -2,9 +2,9 @@
 //
 // A block holds `block` tokens of one key/value head as int8 codes with one fp32 scale s:
 // value = s c.  Writing new tokens x into a block whose first e tokens are older:
-//   a = max|x| over the block's new tokens;  s' = a / 127 (1 if a = 0) where e = 0, else
-//   max(s, a / 127);  new codes round(x / s');  where s' > s the e older codes become
-//   round(c (s / s')).
+//   a = max|x| over the block's new tokens;  s' = a / 127 (1 if a = 0) where e = 0 or the older
+//   tokens are all zeros, else max(s, a / 127);  new codes round(x / s');  where s' > s the e older
+//   codes become round(c (s / s')).
 // A thread block owns one (cache block, head, key or value), so nothing is shared between
 // thread blocks and the result does not depend on their order.  Everything is bound by memory: a
 // thread keeps its words of the new tokens in registers between the maximum and the codes.
@@ -79,10 +79,18 @@ __global__ void __launch_bounds__(kKvThreads) kv_write_kernel(KvArgs a, const ui
   // infinities and NaN leave a NaN scale: the block then reads back as NaN
   const float amax = top < 0x7F80u ? __uint_as_float(top << 16) : __int_as_float(0x7FFFFFFF);
   const float fresh = __fdiv_rn(amax, 127.0f);
-  const float s = p.old ? (was >= fresh || was != was ? was : fresh) : (amax == 0.0f ? 1.0f : fresh);
+  uint2* codes = reinterpret_cast<uint2*>((kv ? a.codes[1] : a.codes[0]) + (p.at << a.block_log2) * a.d);
+  // Older tokens that are all zeros (scale 1, the one a block of zeros takes, and codes 0; or scale 0) fix no scale: at
+  // scale 1 small new ones would be lost.  The whole thread block takes the same branch.
+  bool empty = p.old == 0 || was == 0.0f;
+  if (p.old && was == 1.0f) {
+    uint32_t any = 0;
+    for (int v = threadIdx.x; v < p.old << dlog; v += kKvThreads) any |= codes[v].x | codes[v].y;
+    empty = !__syncthreads_or(any != 0);
+  }
+  const float s = empty ? (amax == 0.0f ? 1.0f : fresh) : was >= fresh || was != was ? was : fresh;
   const float inv = __frcp_rn(s);
   if (threadIdx.x == 0) *scale = s;
-  uint2* codes = reinterpret_cast<uint2*>((kv ? a.codes[1] : a.codes[0]) + (p.at << a.block_log2) * a.d);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = threadIdx.x + kKvThreads * i, slot = v >> dlog;

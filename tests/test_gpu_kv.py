@@ -532,3 +532,61 @@ def test_value_scales_on_both_sides_of_the_first_one(seqs):
         z = 0.1 * np.abs(np.einsum("nhd,lhd->nhl", q[at].astype(np.float64), np.repeat(vals[b][0], 2, 1))).max()
         bound = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + (z + 100) * 2.0 ** -21 + seen[:, None, None] * 2.0 ** -18) * mass.max(2, keepdims=True)
         assert (np.abs(got[at] - ref) <= bound).all()
+
+
+@pytest.mark.parametrize("block,d", [(16, 64), (64, 128)])
+def test_tokens_behind_zeros_keep_their_values(block, d):
+    """A block whose tokens so far are all zeros takes the scale of the first ones that are not, in a later call as in the
+    same one; a block of scale 1 that holds anything else keeps it."""
+    t = torch()
+    p = Paged([(0, 0), (0, 0)], 2, d, block, seed=23, spare=6)
+    p.table = np.array([[1, 2], [4, 3]], np.int32)
+    p.blocks = [[1, 2], [4, 3]]
+    for c in p.codes:
+        c[:] = 85
+    oracle = [SO.Cache(p.cache.n_blocks, 2, block, d) for _ in range(2)]
+    for c in oracle:
+        c.codes[:] = 85
+    steps = [([(3, 3), (2, 2)], 0.0, 127.0), ([(4, 1), (3, 1)], 0.0, 1e-2), ([(5, 1), (4, 1)], 1e-3, 1e-2),
+             ([(6, 1), (6, 2)], 2e-3, 500.0), ([(7, 1), (7, 1)], 1e-4, 0.0)]
+    for seqs, *top in steps:
+        n0 = seqs[0][1]
+        rows = []
+        for _ in range(2):
+            x = p.rng.uniform(-1, 1, (n0 + seqs[1][1], 2, d)).astype(np.float32)
+            x[0, :, 0] = x[n0, :, 0] = 1.0                 # the largest magnitudes are `top`
+            x[:n0] *= top[0]
+            x[n0:] *= top[1]
+            bits = WL.bf16_bits(x)
+            rows.append((bits, WL.bf16_to_f32(bits)))
+        for _ in range(2):                                 # writing again changes nothing
+            LQ.kv_write(p.cache, p.batch(seqs), to_dev(rows[0][0]), to_dev(rows[1][0]))
+        LQ.get_device_status()
+        for kv in range(2):
+            for b, length, n, at in _seq_rows(seqs):
+                oracle[kv].write(rows[kv][1][at], length, p.blocks[b])
+            assert np.array_equal(p.scale[kv].cpu().numpy(), oracle[kv].scale, equal_nan=True)
+            assert np.array_equal(p.codes[kv].cpu().numpy(), oracle[kv].codes)
+    assert (p.scale[0][1] < 1e-4).all() and (p.scale[0][4] > 3).all()
+
+
+@pytest.mark.parametrize("top", [0.5, 0.0])
+def test_tokens_behind_a_block_of_scale_zero(top):
+    """Older tokens whose scale is 0 are zeros whatever their codes are, and stay zeros."""
+    t = torch()
+    p = Paged([(3, 1)], 2, 64, 16, seed=26)
+    bits, x = p.random_rows(2)
+    x = (x / np.abs(x).max() * top).astype(np.float32)
+    bits = WL.bf16_bits(x)
+    for c in p.scale:
+        c[p.blocks[0][0]] = 0.0
+    LQ.kv_write(p.cache, p.batch(), to_dev(bits), to_dev(bits))
+    LQ.get_device_status()
+    K, V = (t.full((3, 2, 64), 0x7FC0, dtype=t.int16, device="cuda") for _ in range(2))
+    LQ.kv_read(p.cache, p.batch([(3, 3)]), K, V)
+    scale = np.abs(WL.bf16_to_f32(bits)).max(2)[0] / np.float32(127)
+    for kv, got in enumerate((K, V)):
+        v = bits_to_f32(got)
+        assert (v[:2] == 0).all()
+        assert np.array_equal(p.scale[kv][p.blocks[0][0]].cpu().numpy(), scale if top else np.ones(2, np.float32))
+        assert (np.abs(v[2] - WL.bf16_to_f32(bits)[0]) <= 0.5001 * scale[:, None] + 2.0 ** -8 * np.abs(x[0])).all()

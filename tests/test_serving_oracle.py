@@ -66,3 +66,14 @@ def test_attention_rows_are_convex_combinations(window):
         assert np.allclose(o[2:], np.repeat(v, 2, 1))
     same, _, _ = SO.attention(q, k, np.ones_like(v), 7, 0.5, window)
     assert np.allclose(same[2:], 1.0)
+
+
+def test_cache_zeros_fix_no_scale():
+    c = SO.Cache(1, 1, 4, 2)
+    c.write([[[0.0, 0.0]]], 1, [0])
+    c.write([[[0.25, -0.5]]], 2, [0])                        # behind zeros: as if the block started here
+    assert c.scale[0, 0] == np.float32(0.5) / np.float32(127) and c.codes[0, 0].tolist()[:2] == [[0, 0], [64, -127]]
+    c.write([[[127.0, 0.0]]], 3, [0])                        # 64 and -127 steps of 0.5 / 127 are less than half of one of 1
+    assert c.scale[0, 0] == 1 and c.codes[0, 0].tolist()[:3] == [[0, 0], [0, 0], [127, 0]]
+    c.write([[[0.25, 0.0]]], 4, [0])                         # a scale of 1 that a token does need
+    assert c.scale[0, 0] == 1 and c.codes[0, 0].tolist()[3] == [0, 0]
