@@ -266,7 +266,8 @@ int lrqat_merge(const lrqat_layer* layer, const void* Phi0, const uint16_t* A, c
  * Residual addition, root-mean-square norm and the per-token 8-bit quantizer of the
  * weight-activation runs (act_per_token of lrqat_layer) in one pass, for rows of k:
  *   h = x + r,  y = gamma h / sqrt(mean(h^2) + eps),
- *   s = max|y| / 127 (1 for a row of zeros),  c = round(y / s),  y_hat = s c.
+ *   s = max|y| / 127 (1 for a row of zeros),  c = round(y / s) within -128 .. 127,
+ *   y_hat = s c.
  * Everything between the inputs and the rounded outputs is fp32 (y is not rounded to
  * bf16 before the quantizer, as it is where lrqat_act_quant reads a stored y).  A row
  * that holds a NaN or an infinity in h or in h gamma, or in which the sum of squares, h gamma

@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kKvThreads) kv_write_kernel(KvArgs a, const ui
     if (slot >= p.old && slot < p.end) {
       float xf[8], q[8];
       unpack8(x[i], xf);
-      round_div8(xf, s, inv, q);
+      round_div8<false>(xf, s, inv, q);
       codes[v] = pack_codes8(q);
     }
   }

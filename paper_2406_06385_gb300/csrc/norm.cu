@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsno
     float q[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) hg[i][e] *= rstd;
-    round_div8(hg[i], s, inv, q);
+    round_div8<true>(hg[i], s, inv, q);
     if (a.Y_q) reinterpret_cast<uint2*>(a.Y_q)[base + j] = pack_codes8(q);
     if (a.Y) {
 #pragma unroll

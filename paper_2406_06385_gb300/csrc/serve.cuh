@@ -41,7 +41,9 @@ __device__ __forceinline__ float max3_abs_nan(float a, float b, float c) {
 // t = round(fl32(x / s)) + kRoundMagic for 8 values with |x / s| < 2^10.  y = x r with r = fl32(1 / s) and
 // fl32(x / s) both lie within 2^-22 |y| of x / s, below 2^-12: where y is more than 2^-11 away from a
 // half-integer both round to the same integer; otherwise, and where r is infinite or a value is not a
-// number, the division decides.
+// number, the division decides.  A scale below 2^-142 has too few bits for max|x| / s <= 127 (up to 190), which
+// fp32 x can meet, bf16 x not (kFp32): r is infinite there, and the division's integers end at -128 and 127.
+template <bool kFp32>
 __device__ __forceinline__ void round_div8(const float (&x)[8], float s, float r, float (&t)[8]) {
   const float2 rr = make_float2(r, r), mm = make_float2(kRoundMagic, kRoundMagic);
   float off = 0.0f;
@@ -56,7 +58,10 @@ __device__ __forceinline__ void round_div8(const float (&x)[8], float s, float r
   }
   if (!(off < 0.49951171875f)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = rintf(__fdiv_rn(x[e], s)) + kRoundMagic;
+    for (int e = 0; e < 8; ++e) {
+      const float u = rintf(__fdiv_rn(x[e], s));
+      t[e] = (kFp32 ? fminf(fmaxf(u, -128.0f), 127.0f) : u) + kRoundMagic;
+    }
   }
 }
 // The codes of round_div8: the low bytes of whole numbers in [-128, 127] plus kRoundMagic.

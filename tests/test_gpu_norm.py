@@ -233,3 +233,19 @@ def test_a_weight_that_is_not_finite_poisons_every_row(T, k, bad):
     assert np.isnan(_fwd(bits, LQ.Norm(k, EPS, 8), T, k, True, "qs")[3].cpu().numpy()).all()
     plain = bits_to_f32(_fwd(bits, LQ.Norm(k, EPS, 0), T, k, True, "Y")[1])
     assert not np.isfinite(plain[:, j]).any() and np.isfinite(np.delete(plain, j, 1)).all()
+
+
+def test_codes_of_rows_whose_scale_is_subnormal_keep_their_sign():
+    """max|y| of 190 steps of the subnormal range: max|y| / 127 is one step, so y / s reaches 190 and the codes end at
+    the 8 bits' ends."""
+    k = 256
+    x = np.zeros((2, k), np.float32)
+    x[0, :4] = 2.0 ** -126 * np.array([1.0, -1.0, 0.5, -0.25])
+    x[1] = 1.0
+    eps = float(np.float32((2.0 ** 23 / 190) ** 2))          # y = x / sqrt(eps): 190, -190, 95, -47.5 steps of 2^-149
+    bits = {"X": WL.bf16_bits(x), "R": None, "gamma": WL.bf16_bits(np.ones(k, np.float32))}
+    _, Y, q, s = _fwd(bits, LQ.Norm(k, eps, 8), 2, k, False, "Yqs")
+    q, s = q.cpu().numpy(), s.cpu().numpy()
+    assert s[0] == np.float32(2.0 ** -149)
+    assert q[0, :3].tolist() == [127, -128, 95] and q[0, 3] in (-47, -48) and (q[0, 4:] == 0).all()
+    assert (q[1] == 127).all()
