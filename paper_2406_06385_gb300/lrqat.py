@@ -67,6 +67,18 @@ class Norm(ctypes.Structure):
     _fields_ = [("k", ctypes.c_int64), ("eps", ctypes.c_float), ("act_bits", ctypes.c_int32)]
 
 
+_types = None
+
+
+def _dtypes():
+    """(int8, float32, int32, types of a bf16 row array: bf16 or its bits as 16-bit whole numbers) of torch."""
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.int8, torch.float32, torch.int32, (torch.bfloat16, torch.int16, torch.uint16))
+    return _types
+
+
 class KVCache(ctypes.Structure):
     """Mirror of lrqat_kv_cache."""
     _fields_ = [("n_blocks", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
@@ -82,6 +94,11 @@ class KVCache(ctypes.Structure):
                 or not (k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
                         and v_scale.is_contiguous())):
             raise LrqatError(-1, "cache tensors must be dense and of matching shapes")
+        i8, f32 = _dtypes()[:2]
+        if not (k_codes.dtype is v_codes.dtype is i8 and k_scale.dtype is v_scale.dtype is f32):
+            raise LrqatError(-1, "cache codes must be int8 and scales float32")
+        if not k_codes.device == v_codes.device == k_scale.device == v_scale.device:
+            raise LrqatError(-1, "cache tensors must lie on one device")
         n_blocks, heads, block, d = shape
         cache = cls(n_blocks, heads, d, block, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(),
                     v_scale.data_ptr())
@@ -103,6 +120,10 @@ class KVBatch(ctypes.Structure):
         if (lens.shape != (n_seqs,) or row_start.shape != (n_seqs + 1,)
                 or not (lens.is_contiguous() and row_start.is_contiguous() and block_table.is_contiguous())):
             raise LrqatError(-1, "lens, row_start and block_table must be dense, of n_seqs, n_seqs + 1 and n_seqs rows")
+        if not lens.dtype is row_start.dtype is block_table.dtype is _dtypes()[2]:
+            raise LrqatError(-1, "lens, row_start and block_table must be int32")
+        if not lens.device == row_start.device == block_table.device:
+            raise LrqatError(-1, "lens, row_start and block_table must lie on one device")
         batch = cls(n_seqs, max_blocks, lens.data_ptr(), row_start.data_ptr(), block_table.data_ptr(), rows, max_rows,
                     max_len)
         batch.tensors = (lens, row_start, block_table)

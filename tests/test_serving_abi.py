@@ -124,3 +124,22 @@ def test_binding_checks_tensor_layouts():
     with pytest.raises(LQ.LrqatError):
         LQ._rows(torch.zeros(3, 2, 64).transpose(0, 1), 3, 64)
     assert LQ._rows(torch.zeros(3, 6, 64)[:, :2], 2, 64) == 384
+
+
+def test_binding_checks_types_and_devices_of_caches_and_batches():
+    """A whole number is int64 in torch unless asked otherwise: as a block table it would be read as id, 0, id, 0."""
+    torch = pytest.importorskip("torch")
+    k, s = torch.zeros(4, 2, 16, 64, dtype=torch.int8), torch.zeros(4, 2)
+    LQ.KVCache.of(k, k, s, s)
+    for bad in ((k.to(torch.uint8), k, s, s), (k, k.float(), s, s), (k, k.int(), s, s), (k, k, s.double(), s),
+                (k, k, s, s.half()), (k, k, s, s.int()), (k, k.to("meta"), s, s), (k, k, s, s.to("meta"))):
+        with pytest.raises(LQ.LrqatError) as e:
+            LQ.KVCache.of(*bad)
+        assert e.value.status == -1
+    arrays = [torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32), torch.zeros(3, 5, dtype=torch.int32)]
+    LQ.KVBatch.of(*arrays, 3, 1, 16)
+    for i in range(3):
+        for bad in (arrays[i].long(), arrays[i].float(), arrays[i].short(), arrays[i].to("meta")):
+            with pytest.raises(LQ.LrqatError) as e:
+                LQ.KVBatch.of(*arrays[:i], bad, *arrays[i + 1:], 3, 1, 16)
+            assert e.value.status == -1
