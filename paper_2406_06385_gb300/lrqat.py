@@ -75,7 +75,7 @@ def _dtypes():
     global _types
     if _types is None:
         import torch
-        _types = (torch.int8, torch.float32, torch.int32, (torch.bfloat16, torch.int16, torch.uint16))
+        _types = (torch.int8, torch.float32, torch.int32, frozenset((torch.bfloat16, torch.int16, torch.uint16)))
     return _types
 
 
@@ -84,6 +84,7 @@ class KVCache(ctypes.Structure):
     _fields_ = [("n_blocks", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("block", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+    device = None                      # get_device() of the tensors, where `of` has seen them
 
     @classmethod
     def of(cls, k_codes, v_codes, k_scale, v_scale) -> "KVCache":
@@ -94,7 +95,7 @@ class KVCache(ctypes.Structure):
                 or not (k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
                         and v_scale.is_contiguous())):
             raise LrqatError(-1, "cache tensors must be dense and of matching shapes")
-        i8, f32 = _dtypes()[:2]
+        i8, f32, _, _ = _types or _dtypes()
         if not (k_codes.dtype is v_codes.dtype is i8 and k_scale.dtype is v_scale.dtype is f32):
             raise LrqatError(-1, "cache codes must be int8 and scales float32")
         if not k_codes.device == v_codes.device == k_scale.device == v_scale.device:
@@ -103,6 +104,7 @@ class KVCache(ctypes.Structure):
         cache = cls(n_blocks, heads, d, block, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(),
                     v_scale.data_ptr())
         cache.tensors = (k_codes, v_codes, k_scale, v_scale)
+        cache.device = k_codes.get_device()
         return cache
 
 
@@ -111,6 +113,7 @@ class KVBatch(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("len", ctypes.c_void_p),
                 ("row_start", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("rows", ctypes.c_int64),
                 ("max_rows", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+    device = None                      # get_device() of the tensors, where `of` has seen them
 
     @classmethod
     def of(cls, lens, row_start, block_table, rows: int, max_rows: int, max_len: int) -> "KVBatch":
@@ -120,13 +123,14 @@ class KVBatch(ctypes.Structure):
         if (lens.shape != (n_seqs,) or row_start.shape != (n_seqs + 1,)
                 or not (lens.is_contiguous() and row_start.is_contiguous() and block_table.is_contiguous())):
             raise LrqatError(-1, "lens, row_start and block_table must be dense, of n_seqs, n_seqs + 1 and n_seqs rows")
-        if not lens.dtype is row_start.dtype is block_table.dtype is _dtypes()[2]:
+        if not lens.dtype is row_start.dtype is block_table.dtype is (_types or _dtypes())[2]:
             raise LrqatError(-1, "lens, row_start and block_table must be int32")
         if not lens.device == row_start.device == block_table.device:
             raise LrqatError(-1, "lens, row_start and block_table must lie on one device")
         batch = cls(n_seqs, max_blocks, lens.data_ptr(), row_start.data_ptr(), block_table.data_ptr(), rows, max_rows,
                     max_len)
         batch.tensors = (lens, row_start, block_table)
+        batch.device = lens.get_device()
         return batch
 
 
@@ -331,26 +335,48 @@ def act_dequant(norm: Norm, T: int, codes, s, X_hat, stream=None) -> None:
     _check(lib().lrqat_act_dequant(ctypes.byref(norm), T, _ptr(codes), _ptr(s), _ptr(X_hat), _stream(stream)))
 
 
-def _rows(t, heads: int, d: int) -> int:
-    """Distance in elements of consecutive rows of a [rows, heads, head_dim] tensor or view."""
+def _rows(t, heads: int, d: int, rows: int = 0) -> int:
+    """Distance in elements of consecutive rows of a [rows or more, heads, head_dim] tensor or view."""
     shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[1] != heads or shape[2] != d or stride[2] != 1 or (heads > 1 and stride[1] != d):
-        raise LrqatError(-1, f"rows of {heads} heads by {d} expected, dense within a row")
+    if (len(shape) != 3 or shape[1] != heads or shape[2] != d or shape[0] < rows or stride[2] != 1
+            or (heads > 1 and stride[1] != d)):
+        raise LrqatError(-1, f"{rows} rows of {heads} heads by {d} expected, dense within a row")
     return stride[0] if shape[0] > 1 else max(stride[0], heads * d)
+
+
+def _device(cache: KVCache, batch: KVBatch):
+    """The CUDA device of a cache and a batch, None where both were filled by hand."""
+    a, b = cache.device, batch.device
+    if a != b and a is not None and b is not None:
+        raise LrqatError(-1, "the cache and the batch must lie on one device")
+    if a is None:
+        a = b
+    if a == -1:
+        raise LrqatError(-1, "the cache and the batch must lie on a CUDA device")
+    return a
+
+
+def _row_array(t, heads: int, d: int, rows: int, device) -> int:
+    """Checks a row array of a call and returns its row distance (see _rows)."""
+    if t.dtype not in (_types or _dtypes())[3]:
+        raise LrqatError(-1, "row arrays must be bf16 (or its bits as 16-bit whole numbers)")
+    if t.get_device() != device and (device is not None or not t.is_cuda):
+        raise LrqatError(-1, "row arrays must lie on the device of the cache and the batch")
+    return _rows(t, heads, d, rows)
 
 
 def kv_write(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:
     """Quantizes the batch's new keys and values, bf16 [rows, n_kv_heads, head_dim], into the cache."""
-    h, d = cache.n_kv_heads, cache.head_dim
-    _check(lib().lrqat_kv_write(ctypes.byref(cache), ctypes.byref(batch), _ptr(K), _rows(K, h, d), _ptr(V),
-                                _rows(V, h, d), _stream(stream)))
+    h, d, rows, device = cache.n_kv_heads, cache.head_dim, batch.rows, _device(cache, batch)
+    ldk, ldv = _row_array(K, h, d, rows, device), _row_array(V, h, d, rows, device)
+    _check(lib().lrqat_kv_write(ctypes.byref(cache), ctypes.byref(batch), _ptr(K), ldk, _ptr(V), ldv, _stream(stream)))
 
 
 def kv_read(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:
     """Reads the batch's rows back into K and V, bf16 [rows, n_kv_heads, head_dim]."""
-    h, d = cache.n_kv_heads, cache.head_dim
-    _check(lib().lrqat_kv_read(ctypes.byref(cache), ctypes.byref(batch), _ptr(K), _rows(K, h, d), _ptr(V),
-                               _rows(V, h, d), _stream(stream)))
+    h, d, rows, device = cache.n_kv_heads, cache.head_dim, batch.rows, _device(cache, batch)
+    ldk, ldv = _row_array(K, h, d, rows, device), _row_array(V, h, d, rows, device)
+    _check(lib().lrqat_kv_read(ctypes.byref(cache), ctypes.byref(batch), _ptr(K), ldk, _ptr(V), ldv, _stream(stream)))
 
 
 def kv_attn_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window: int = 0) -> int:
@@ -359,12 +385,16 @@ def kv_attn_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window
 
 def kv_attn(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, O, workspace, stream=None) -> None:
     """Causal attention of the batch's rows Q over the cache into O, both bf16 [rows, n_heads, head_dim]."""
-    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    shape, d = Q.shape, cache.head_dim
+    nbytes, device = 0, _device(cache, batch)
+    if workspace is not None:
+        nbytes = workspace.numel() * workspace.element_size()
+        if not workspace.is_cuda:
+            raise LrqatError(-1, "the workspace must lie on the device")
+    shape, d, rows = Q.shape, cache.head_dim, batch.rows
     heads = shape[1] if len(shape) == 3 else 0
-    _check(lib().lrqat_kv_attn(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, _ptr(Q),
-                               _rows(Q, heads, d), _ptr(O), _rows(O, heads, d), _ptr(workspace), nbytes,
-                               _stream(stream)))
+    ldq, ldo = _row_array(Q, heads, d, rows, device), _row_array(O, heads, d, rows, device)
+    _check(lib().lrqat_kv_attn(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, _ptr(Q), ldq,
+                               _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
 
 
 def get_device_status(stream=None) -> None:

@@ -1,5 +1,6 @@
 """The norm, cache and attention entry points reject bad arguments on the host before any CUDA work."""
 import ctypes
+import types
 
 import pytest
 
@@ -143,3 +144,63 @@ def test_binding_checks_types_and_devices_of_caches_and_batches():
             with pytest.raises(LQ.LrqatError) as e:
                 LQ.KVBatch.of(*arrays[:i], bad, *arrays[i + 1:], 3, 1, 16)
             assert e.value.status == -1
+
+
+def _stand_in(torch, shape, dtype, device="cuda:0"):
+    """What the binding asks of a tensor, with an address that is never followed."""
+    t = torch.zeros(shape, dtype=dtype)
+    return types.SimpleNamespace(shape=t.shape, dtype=dtype, stride=t.stride, numel=t.numel, element_size=t.element_size,
+                                 is_contiguous=lambda: True, is_cuda=device != "cpu",
+                                 device=torch.device(device), data_ptr=lambda: OK,
+                                 get_device=lambda: -1 if device == "cpu" else int(device[5:]))
+
+
+def test_binding_checks_row_arrays(monkeypatch):
+    """Row arrays shorter than the batch (read or written out of range on the device), of another type, or elsewhere
+    than the cache are refused before the library is called."""
+    torch = pytest.importorskip("torch")
+    calls = []
+    record = lambda name: lambda *a: calls.append(name) or 0  # noqa: E731
+    monkeypatch.setattr(LQ, "lib", lambda: types.SimpleNamespace(
+        **{n: record(n) for n in ("lrqat_kv_write", "lrqat_kv_read", "lrqat_kv_attn")}))
+    fake = lambda shape, dtype, device="cuda:0": _stand_in(torch, shape, dtype, device)  # noqa: E731
+
+    def objects(device="cuda:0"):
+        codes, scale = fake((8, 2, 16, 128), torch.int8, device), fake((8, 2), torch.float32, device)
+        i32 = lambda *shape: fake(shape, torch.int32, device)  # noqa: E731
+        return LQ.KVCache.of(codes, codes, scale, scale), LQ.KVBatch.of(i32(2), i32(3), i32(2, 4), 6, 3, 64)
+
+    cache, batch = objects()
+    ws = fake((64,), torch.uint8)
+
+    def run(kv, kv2, q, o, ws=ws, cache=cache, batch=batch):
+        for f in (lambda: LQ.kv_write(cache, batch, kv, kv2, stream=0), lambda: LQ.kv_read(cache, batch, kv, kv2, stream=0),
+                  lambda: LQ.kv_attn(cache, batch, q, 1.0, 0, o, ws, stream=0)):
+            yield f
+
+    kv, q = fake((6, 2, 128), torch.bfloat16), fake((6, 4, 128), torch.int16)
+    for f in run(kv, kv, q, q):
+        f()
+    for f in run(fake((7, 2, 128), torch.int16), kv, q, fake((9, 4, 128), torch.bfloat16)):    # longer ones are fine
+        f()
+    for f in run(kv, kv, q, q, None, LQ.KVCache(8, 2, 128, 16, OK, OK, OK, OK), LQ.KVBatch(2, 4, OK, OK, OK, 6, 3, 64)):
+        f()
+    assert len(calls) == 9
+    bad = lambda **kw: (fake(**{**dict(shape=(6, 2, 128), dtype=torch.bfloat16), **kw}),  # noqa: E731
+                        fake(**{**dict(shape=(6, 4, 128), dtype=torch.bfloat16), **kw, **(
+                            {"shape": (kw["shape"][0], 4, 128)} if "shape" in kw else {})}))
+    for kw in (dict(shape=(5, 2, 128)), dict(shape=(0, 2, 128)), dict(dtype=torch.float16), dict(dtype=torch.float32),
+               dict(device="cpu"), dict(device="cuda:1")):
+        bkv, bq = bad(**kw)
+        for args in ((bkv, kv, bq, q), (kv, bkv, q, bq)):
+            for f in run(*args):
+                with pytest.raises(LQ.LrqatError) as e:
+                    f()
+                assert e.value.status == -1
+    with pytest.raises(LQ.LrqatError):
+        LQ.kv_attn(cache, batch, q, 1.0, 0, q, fake((64,), torch.uint8, "cpu"), stream=0)
+    for pair in ((objects("cpu")[0], batch), (cache, objects("cpu")[1])):
+        for f in run(kv, kv, q, q, None, *pair):
+            with pytest.raises(LQ.LrqatError):
+                f()
+    assert len(calls) == 9
