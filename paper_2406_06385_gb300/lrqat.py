@@ -341,7 +341,7 @@ def _rows(t, heads: int, d: int, rows: int = 0) -> int:
     if (len(shape) != 3 or shape[1] != heads or shape[2] != d or shape[0] < rows or stride[2] != 1
             or (heads > 1 and stride[1] != d)):
         raise LrqatError(-1, f"{rows} rows of {heads} heads by {d} expected, dense within a row")
-    return stride[0] if shape[0] > 1 else max(stride[0], heads * d)
+    return stride[0] if shape[0] > 1 else heads * d        # a single row's distance to the next one has no meaning
 
 
 def _device(cache: KVCache, batch: KVBatch):
