@@ -208,7 +208,8 @@ def test_binding_checks_row_arrays(monkeypatch):
 
 def test_binding_takes_a_single_row_of_any_stride():
     torch = pytest.importorskip("torch")
-    row = torch.zeros(3, 517)[1:2, :256].unflatten(1, (2, 128))
+    row = torch.zeros(3, 517)[:, :256].unflatten(1, (2, 128))[1:2]
+    assert row.stride()[0] == 517
     assert LQ._rows(row, 2, 128) == 256                       # 517 is no multiple of 8, and nothing lies at it
     assert LQ._rows(row.expand(1, 2, 128), 2, 128) == 256
     assert LQ._rows(torch.zeros(0, 2, 128), 2, 128) == 256
