@@ -213,16 +213,26 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-_torch_c = None
+_current_stream = None
+
+
+def _current_stream_source():
+    """The handle of torch's current stream.  torch's own raw accessors take a tenth of the time of
+    torch.cuda.current_stream(), but are not part of its public interface: without them the public one serves."""
+    import torch
+    device, raw = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if device is None or raw is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    return lambda: raw(device())
 
 
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    global _torch_c
-    if _torch_c is None:
-        from torch import _C as _torch_c
-    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())   # a tenth of current_stream()'s time
+    global _current_stream
+    if _current_stream is None:
+        _current_stream = _current_stream_source()
+    return _current_stream()
 
 
 def last_error() -> str:

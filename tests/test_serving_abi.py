@@ -213,3 +213,13 @@ def test_binding_takes_a_single_row_of_any_stride():
     assert LQ._rows(row, 2, 128) == 256                       # 517 is no multiple of 8, and nothing lies at it
     assert LQ._rows(row.expand(1, 2, 128), 2, 128) == 256
     assert LQ._rows(torch.zeros(0, 2, 128), 2, 128) == 256
+
+
+@pytest.mark.parametrize("missing", ["_cuda_getDevice", "_cuda_getCurrentRawStream"])
+def test_the_current_stream_does_not_hang_on_private_names(monkeypatch, missing):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(LQ, "_current_stream", None, raising=False)
+    monkeypatch.delattr(torch._C, missing)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=4096))
+    assert LQ._stream(None) == 4096
+    assert LQ._stream(types.SimpleNamespace(cuda_stream=32)) == 32 and LQ._stream(48) == 48
