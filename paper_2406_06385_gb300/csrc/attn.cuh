@@ -56,12 +56,17 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile
   t.pos_lo = t.seq.first + t.r0 / a.group;
   t.pos_hi = t.seq.first + last / a.group;
   t.hi = max(t.pos_hi + 1, 0);
-  t.lo = a.window > 0 ? max(t.pos_lo - a.window + 1, 0) & ~(kKeyAlign - 1) : 0;
+  const int64_t seen = static_cast<int64_t>(t.pos_lo) - a.window + 1;   // pos_lo is negative for padding rows
+  t.lo = a.window > 0 && seen > 0 ? static_cast<int>(seen) & ~(kKeyAlign - 1) : 0;
   return true;
 }
 
+// The end of the piece of a tile's keys that starts at k0.
+__device__ __forceinline__ int piece_end(const AttnArgs& a, const Tile& t, int k0) {
+  return t.hi - k0 > a.chunk ? k0 + a.chunk : t.hi;
+}
 __device__ __forceinline__ int tile_splits(const AttnArgs& a, const Tile& t) {
-  return t.hi > t.lo ? (t.hi - t.lo + a.chunk - 1) / a.chunk : 0;
+  return t.hi > t.lo ? (t.hi - t.lo - 1) / a.chunk + 1 : 0;   // lengths and a.chunk may be close to 2^31
 }
 
 }  // namespace lrqat

@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   if (last ? ns > 0 && ns < a.splits && (t.hi - t.lo) % a.chunk == 0
            : (split + 1) * static_cast<int64_t>(a.chunk) > t.hi - t.lo)
     return;
-  const int k0 = t.lo + split * a.chunk, k1 = min(t.hi, k0 + a.chunk);
+  const int k0 = t.lo + split * a.chunk, k1 = piece_end(a, t, k0);
 
   const uint32_t ring = smem_addr(smem) + warp * Sm::kWarpStage;
   const uint32_t scales = smem_addr(smem) + Sm::kScales + warp * 16;

@@ -31,8 +31,10 @@ __device__ __forceinline__ bool block_part(const KvArgs& a, int b, int j, int he
   SeqRows s;
   if (!seq_rows(a, b, s)) return false;
   const int first = s.first > 0 ? s.first : 0;
-  const int p0 = ((first >> a.block_log2) + j) << a.block_log2;
-  if (p0 >= s.len || s.n == 0) return false;
+  // the batch's bounds may allow many more blocks than are left below 2^31 tokens
+  const int64_t start = (static_cast<int64_t>(first >> a.block_log2) + j) << a.block_log2;
+  if (start >= s.len || s.n == 0) return false;
+  const int p0 = static_cast<int>(start);
   const int blk = seq_block(a, b, p0);
   if (blk < 0) return false;
   p.old = first > p0 ? first - p0 : 0;

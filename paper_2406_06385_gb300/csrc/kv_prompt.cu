@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   if (rt < 0 || !attn_tile(a, b, rt, t)) return;
   const int ns = tile_splits(a, t);
   if (split > 0 && split >= ns) return;
-  const int k0 = t.lo + split * a.chunk, k1 = min(t.hi, k0 + a.chunk);
+  const int k0 = t.lo + split * a.chunk, k1 = piece_end(a, t, k0);
   const int tiles = k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0;
   const int halves = t.rows - t.r0 > 128 ? 2 : 1;
 

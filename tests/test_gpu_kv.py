@@ -590,3 +590,68 @@ def test_tokens_behind_a_block_of_scale_zero(top):
         assert (v[:2] == 0).all()
         assert np.array_equal(p.scale[kv][p.blocks[0][0]].cpu().numpy(), scale if top else np.ones(2, np.float32))
         assert (np.abs(v[2] - WL.bf16_to_f32(bits)[0]) <= 0.5001 * scale[:, None] + 2.0 ** -8 * np.abs(x[0])).all()
+
+
+def _far(seqs_len, n, d, seed):
+    """A sequence of `seqs_len` tokens whose blocks are one and the same but for its last six, and the short sequence
+    of those six alone."""
+    t = torch()
+    width = -(-seqs_len // 128)
+    p = Paged([(6 * 128 - (width * 128 - seqs_len), n)], 1, d, 128, seed=seed)
+    table = t.full((1, width), p.blocks[0][0], dtype=t.int32, device="cuda")
+    table[0, -6:] = t.tensor(p.blocks[0], dtype=t.int32)
+    one = lambda v: t.tensor(v, dtype=t.int32, device="cuda")  # noqa: E731
+    batch = lambda rows, max_rows: LQ.KVBatch.of(one([seqs_len]), one([0, rows]), table, rows, max_rows, seqs_len)  # noqa: E731
+    return p, batch
+
+
+LONGEST = (2 ** 31 - 1 - 1024) // 128 * 128               # the most that the host admits
+
+
+@pytest.mark.parametrize("length,n,max_rows", [(LONGEST, 1, 1), (LONGEST - 3, 1, 2 ** 24), (LONGEST - 100, 200, 2 ** 20)])
+def test_writes_and_reads_at_the_longest_lengths(length, n, max_rows):
+    """The newest tokens of a sequence close to 2^31 tokens long, under bounds that allow many more rows than lie
+    behind the last block."""
+    t = torch()
+    p, far = _far(length, n, 64, seed=27)
+    _fill(p)
+    before = [x.clone() for x in p.codes + p.scale]
+    rows = [p.random_rows(1) for _ in range(2)]
+    out = [[t.zeros((n, 1, 64), dtype=t.int16, device="cuda") for _ in range(2)] for _ in range(2)]
+    after = []
+    for batch, back in ((p.batch(), out[0]), (far(n, max_rows), out[1])):
+        for x, start in zip(p.codes + p.scale, before):
+            x.copy_(start)
+        LQ.kv_write(p.cache, batch, to_dev(rows[0][0]), to_dev(rows[1][0]))
+        LQ.kv_read(p.cache, batch, *back)
+        LQ.get_device_status()
+        after.append([x.nan_to_num() for x in p.codes + p.scale] + back)
+    assert all(t.equal(a, b) for a, b in zip(*after)) and not t.equal(after[0][0], before[0])
+
+
+@pytest.mark.parametrize("n", [1, 12, 40])
+def test_windows_at_the_longest_lengths(n):
+    p, far = _far(LONGEST - 3, n, 64, seed=28)
+    vals = _fill(p)
+    bits, q = p.random_rows(1)
+    O = _attn(p, far(n, n), to_dev(bits), 0.2, 300, 1)
+    LQ.get_device_status()
+    _check(p, vals, O, q, 0.2, 300)
+
+
+def test_attention_over_the_longest_length():
+    """Every key of 2^31 - 1152 tokens, of which all but the last six blocks are one block over and over.  Bound: fp32
+    sums of about 28,000 steps a warp and lane, each rounding once (2^-25 of the sum), in numerator and denominator."""
+    p, far = _far(LONGEST - 3, 1, 64, seed=29)
+    vals = _fill(p)
+    bits, q = p.random_rows(1, scale=0.3)
+    O = _attn(p, far(1, 1), to_dev(bits), 0.1, 0, 1)
+    LQ.get_device_status()
+    k, v = (x[:, 0] for x in vals[0])
+    z = 0.1 * (k @ q[0, 0].astype(np.float64))
+    w = np.exp(z - z.max())
+    w[:128] *= LONGEST // 128 - 5                           # the repeated block stands at its own place too
+    w /= w.sum()
+    got, ref, mass = bits_to_f32(O)[0, 0], w @ v, w @ np.abs(v)
+    assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2 * 28000 * 2.0 ** -25) * mass).all()
+    assert np.abs(ref).max() > 4 * (2.0 ** -11 + 2 * 28000 * 2.0 ** -25) * mass.max()
