@@ -537,7 +537,8 @@ void plan_attn(AttnArgs& a, int sms) {
     chunk = (keys + at_once / tiles - 1) / (at_once / tiles);
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk < least) chunk = least;
-  if (prompt && tiles >= want) chunk = (keys + unit) / unit * unit;
+  const int64_t whole = (keys + unit) / unit * unit;         // with many tiles keys * tiles / want passes 32 bits
+  if (chunk > whole || (prompt && tiles >= want)) chunk = whole;
   a.chunk = static_cast<int>(chunk);
   const int64_t splits = (keys + chunk - 1) / chunk;
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);

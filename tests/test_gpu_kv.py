@@ -655,3 +655,19 @@ def test_attention_over_the_longest_length():
     got, ref, mass = bits_to_f32(O)[0, 0], w @ v, w @ np.abs(v)
     assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2 * 28000 * 2.0 ** -25) * mass).all()
     assert np.abs(ref).max() > 4 * (2.0 ** -11 + 2 * 28000 * 2.0 ** -25) * mass.max()
+
+
+def test_many_sequences_under_a_bound_far_above_their_lengths():
+    """Thousands of sequences and heads with a length bound in the millions: the keys of one piece number no more than
+    the bound, whatever the number of tiles."""
+    t = torch()
+    seqs, heads, width = 4096, 128, 78125
+    p = Paged([(100, 1)], heads, 64, 128, seed=30)
+    _fill(p)
+    lens = (t.arange(seqs, device="cuda") % 101).int()
+    start, table = t.arange(seqs + 1, device="cuda").int(), t.full((seqs, width), p.blocks[0][0], dtype=t.int32, device="cuda")
+    Q = (t.randn(seqs, heads, 64, device="cuda") * 2).bfloat16()
+    out = [_attn(p, LQ.KVBatch.of(lens, start, table, seqs, 1, bound), Q, 0.1, 0, heads, out=t.full_like(Q, float("nan")))
+           for bound in (100, width * 128)]
+    LQ.get_device_status()
+    assert t.equal(*out) and (out[0][0] == 0).all() and (out[0][1:101].abs().amax((1, 2)) > 0).all()
