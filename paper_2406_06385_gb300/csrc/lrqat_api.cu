@@ -1416,7 +1416,7 @@ int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int3
   AttnArgs a;
   LRQAT_TRY(attn_args(cache, batch, n_heads, window, &a));
   if (!std::isfinite(softmax_scale)) return fail(LRQAT_ERR_INVALID_ARG, "softmax_scale must be finite");
-  if (a.kv.rows == 0 || a.kv.max_rows == 0) return LRQAT_OK;
+  if (a.kv.rows == 0) return LRQAT_OK;
   LRQAT_TRY(check_rows(Q, ldq, static_cast<int64_t>(n_heads) * a.kv.d, "Q"));
   LRQAT_TRY(check_rows(O, ldo, static_cast<int64_t>(n_heads) * a.kv.d, "O"));
   const int64_t part_rows = attn_part_rows(a);

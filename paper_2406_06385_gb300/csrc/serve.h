@@ -62,11 +62,12 @@ struct KvArgs {
   int max_rows, max_len;
   int* status;
 };
-// Blocks that the last `max_rows` of `max_len` tokens can touch.
+// Blocks that the last `max_rows` of `max_len` tokens can touch; at least one, whose thread block then reports
+// sequences beyond a bound of zero.
 inline int kv_touched_blocks(const KvArgs& a) {
   const int64_t all = (static_cast<int64_t>(a.max_len) + (1 << a.block_log2) - 1) >> a.block_log2;
   const int64_t some = ((static_cast<int64_t>(a.max_rows) + (1 << a.block_log2) - 2) >> a.block_log2) + 1;
-  return static_cast<int>(all < some ? all : some);
+  return static_cast<int>(all < 1 ? 1 : all < some ? all : some);
 }
 cudaError_t launch_kv_write(const KvArgs& a, const uint16_t* K, int64_t ldk, const uint16_t* V, int64_t ldv,
                             cudaStream_t stream);

@@ -671,3 +671,27 @@ def test_many_sequences_under_a_bound_far_above_their_lengths():
            for bound in (100, width * 128)]
     LQ.get_device_status()
     assert t.equal(*out) and (out[0][0] == 0).all() and (out[0][1:101].abs().amax((1, 2)) > 0).all()
+
+
+@pytest.mark.parametrize("max_rows,max_len", [(0, 48), (2, 0), (0, 0)])
+def test_bounds_of_zero_are_bounds(max_rows, max_len):
+    """Sequences beyond bounds of zero rows or zero tokens are reported as beyond any other bound; what lies within
+    them is served."""
+    t = torch()
+    p = Paged([(40, 2), (0, 1)], 2, 128, 16, seed=31)
+    vals = _fill(p)
+    del vals
+    bits, _ = p.random_rows(2)
+    K = to_dev(bits)
+    batch = p.batch()
+    batch.max_rows, batch.max_len = max_rows, max_len
+    before = [c.clone() for c in p.codes]
+    O = t.full((3, 2, 128), 1, dtype=t.int16, device="cuda")
+    for call in (lambda: LQ.kv_write(p.cache, batch, K, K), lambda: LQ.kv_read(p.cache, batch, O, O),
+                 lambda: _attn(p, batch, K, 0.1, 0, 2, out=O)):
+        call()
+        with pytest.raises(LQ.LrqatError) as e:
+            LQ.get_device_status()
+        assert e.value.status == -7
+    assert all(t.equal(a, b) for a, b in zip(before, p.codes)) and (O[:2] == 1).all()
+    assert (O[2] == (1 if max_rows == 0 else 0)).all()     # an idle slot's row, within the bounds or not
