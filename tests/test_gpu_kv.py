@@ -695,3 +695,65 @@ def test_bounds_of_zero_are_bounds(max_rows, max_len):
         assert e.value.status == -7
     assert all(t.equal(a, b) for a, b in zip(before, p.codes)) and (O[:2] == 1).all()
     assert (O[2] == (1 if max_rows == 0 else 0)).all()     # an idle slot's row, within the bounds or not
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("how", ["argument", "current"])
+def test_calls_are_queued_behind_the_work_of_their_stream(how, new):
+    """On a side stream some milliseconds of other work and then the copies that fill the inputs: a call on any other
+    stream would read what the inputs or the cache held before."""
+    t = torch()
+    p = Paged([(90, new), (new, new)], 2, 128, 16, seed=32)
+    _fill(p)
+    src = [to_dev(p.random_rows(h)[0]) for h in (2, 2, 8)]
+    start = [x.clone() for x in p.codes + p.scale]
+    junk, side, batch = empty((1 << 28,), t.float32), t.cuda.Stream(), p.batch()
+
+    def run(stream):
+        for x, y in zip(p.codes + p.scale, start):
+            x.copy_(y)
+        K, V, Q = (t.zeros_like(x) for x in src)
+        K2, V2, O = (t.zeros_like(x) for x in src)
+        ws = empty((LQ.kv_attn_workspace_bytes(p.cache, batch, 8, 0),), t.uint8)
+        other = stream or t.cuda.current_stream()
+        other.wait_stream(t.cuda.current_stream())
+        with t.cuda.stream(other):
+            for i in range(20):
+                junk.fill_(float(i))
+            for x, y in zip((K, V, Q), src):
+                x.copy_(y)
+        with t.cuda.stream(stream if how == "current" else None):
+            at = stream if how == "argument" else None
+            LQ.kv_write(p.cache, batch, K, V, stream=at)
+            LQ.kv_read(p.cache, batch, K2, V2, stream=at)
+            LQ.kv_attn(p.cache, batch, Q, 0.1, 0, O, ws, stream=at)
+        t.cuda.synchronize()
+        return [x.nan_to_num() for x in p.codes + p.scale + [K2, V2, O]]
+
+    assert all(t.equal(a, b) for a, b in zip(run(None), run(side)))
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0, -0.0])
+@pytest.mark.parametrize("new", [1, 6, 100])
+def test_softmax_scales_that_are_not_positive(new, scale):
+    p = Paged([(333, new), (20, min(new, 20))], 2, 128, 16, seed=24)
+    vals = _fill(p)
+    bits, q = p.random_rows(4)
+    O = _attn(p, p.batch(), to_dev(bits), scale, 0, 4)
+    LQ.get_device_status()
+    _check(p, vals, O, q, scale, 0)
+
+
+def test_a_long_sequence_beside_a_prompt():
+    """One new token of a long sequence in the batch of a prompt, whose tiles fill the machine: nothing is cut."""
+    seqs = [(20000, 1), (1300, 1300)]
+    p = Paged(seqs, 8, 64, 64, seed=25)
+    vals = _fill(p)
+    bits, q = p.random_rows(32)
+    got = bits_to_f32(_attn(p, p.batch(), to_dev(bits), 0.1, 0, 32)).astype(np.float64)
+    LQ.get_device_status()
+    for b, rows, last in ((0, slice(0, 1), 20000), (1, slice(1, 4), 3), (1, slice(690, 700), 699), (1, slice(1297, 1301), 1300)):
+        k, v = vals[b]
+        ref, mass, seen = SO.attention(q[rows], k[:last], v[:last], last, 0.1)
+        bound = 2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * mass + (seen[:, None, None] * 2.0 ** -25) * np.abs(v).max()
+        assert (np.abs(got[rows] - ref) <= bound).all()

@@ -249,3 +249,41 @@ def test_codes_of_rows_whose_scale_is_subnormal_keep_their_sign():
     assert s[0] == np.float32(2.0 ** -149)
     assert q[0, :3].tolist() == [127, -128, 95] and q[0, 3] in (-47, -48) and (q[0, 4:] == 0).all()
     assert (q[1] == 127).all()
+
+
+@pytest.mark.parametrize("how", ["argument", "current"])
+def test_calls_are_queued_behind_the_work_of_their_stream(how):
+    """On a side stream some milliseconds of other work and then the copies that fill the inputs: a call on any other
+    stream would read what the inputs held before."""
+    t = torch()
+    T, k = 129, 4096
+    d = _inputs(T, k, 22, ["X", "R", "dY", "gamma"])
+    norm = LQ.Norm(k, EPS, 8)
+    src = {n: to_dev(v[0]) for n, v in d.items()}
+    junk, side = empty((1 << 28,), t.float32), t.cuda.Stream()
+
+    def run(dev, stream):
+        H, Y, q, s = empty((T, k), t.int16), empty((T, k), t.int16), empty((T, k), t.int8), empty((T,), t.float32)
+        dX, dgamma, back = empty((T, k), t.int16), empty((k,), t.float32), empty((T, k), t.int16)
+        ws = empty((LQ.add_rmsnorm_bwd_workspace_bytes(norm, T),), t.uint8)
+        out = [H, Y, q, s, dX, dgamma, back]
+        for o in out:
+            o.zero_()
+        if stream is not None:
+            stream.wait_stream(t.cuda.current_stream())
+            with t.cuda.stream(stream):
+                for i in range(20):
+                    junk.fill_(float(i))
+                for n in dev:
+                    dev[n].copy_(src[n])
+        with t.cuda.stream(stream if how == "current" else None):
+            at = stream if how == "argument" else None
+            LQ.add_rmsnorm_fwd(norm, T, dev["X"], dev["R"], dev["gamma"], H, Y, q, s, stream=at)
+            LQ.act_dequant(norm, T, q, s, back, stream=at)
+            LQ.add_rmsnorm_bwd(norm, T, dev["dY"], None, H, dev["gamma"], dX, dgamma, False, ws, stream=at)
+        t.cuda.synchronize()
+        return out
+
+    want = run(src, None)
+    got = run({n: t.zeros_like(v) for n, v in src.items()}, side)
+    assert all(t.equal(a, b) for a, b in zip(want, got))
