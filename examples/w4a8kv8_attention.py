@@ -1,7 +1,8 @@
 """An attention block with 4-bit weights, 8-bit activations and an 8-bit key / value cache (W4A8KV8), as a user
 of the library runs it.
 
-Serving, one call per step for a ragged batch of prompts, single tokens or both:
+Serving, one call per step for a ragged batch of prompts, single tokens or both (kv_attn is faster in two calls, one
+for the prompts and one for the single tokens, than over both at once):
 
     h, x = x + residual, quantized norm       add_rmsnorm_fwd (X_hat per token)
     q, k, v = x W_qkv^T                       linear_fwd_quantized, one fused projection
@@ -9,6 +10,9 @@ Serving, one call per step for a ragged batch of prompts, single tokens or both:
     a = attention(q, cache)                   kv_attn
     y = quantize(a) W_o^T                     act_quant, linear_fwd_quantized
     h, x = y + h, quantized norm              add_rmsnorm_fwd: what the block's MLP takes
+
+Positions: the block has none of its own.  A model with rotary positions rotates q and k between the projection and
+kv_write; the library has no operator for that.
 
 Training, a normed projection that keeps its activations as one byte each: the codes and scales of
 add_rmsnorm_fwd, from which act_dequant rebuilds X_hat for the backward of the projection, and

@@ -374,8 +374,10 @@ size_t lrqat_kv_attn_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv
  * query head h reads key/value head h / (n_heads / n_kv_heads).  A row that sees no key is 0.
  * n_heads: a multiple of n_kv_heads.  Q, O: bf16 [rows, n_heads, head_dim], consecutive rows
  * ldq / ldo elements apart (multiples of 8).
- * Scores, the softmax statistics and the sums are fp32; probabilities are rounded to 11
- * significant bits.  The result of a row does not depend on the order of thread blocks. */
+ * Scores, the softmax statistics and the sums are fp32.  A key's contribution e^z s_v (s_v the scale
+ * of its values) is rounded to half precision before it weights the codes, the denominator sums it
+ * unrounded: 11 significant bits down to 2^-14 of the row's largest contribution, fewer below, none
+ * below 2^-25.  The result of a row does not depend on the order of thread blocks. */
 int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
                   int32_t window, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo, void* workspace,
                   size_t workspace_bytes, lrqat_stream_t stream);

@@ -3,13 +3,15 @@
 // With s_k, s_v the scales of a cache block and c_k, c_v its codes, query row q at position p:
 //   z_j = scale s_k (q . c_k,j)   for the keys j <= p (and j > p - window),
 //   o = sum_j e^{z_j} s_v c_v,j / sum_j e^{z_j},   0 for a row that sees no key.
-// The kernels fold s_v into the exponent: with z'_j = z_j log2(e) + log2(s_v) and m their running
-// maximum, P_j = 2^{z'_j - m} lies in [0, 1] and is what a key contributes to o, whatever the scales
-// of the blocks are.  The denominator, the sum of P_j / s_v, is kept relative to a running
-// maximum n of its own, that of z_j log2(e): scales of one sequence may lie as far apart as fp32 reaches.
-// So P fits 11-bit half precision and the codes (|c| <= 128) are exact in it; a row of q is first divided
-// by the power of two of its largest magnitude, which half precision also holds (exact but for elements
-// below 2^-14 of the largest).
+// The kernels fold s_v into the exponent: with z'_j = z_j log2(e) + log2(s_v) and m their running maximum,
+// P_j = 2^{z'_j - m} lies in [0, 1] and is what a key contributes to o, whatever the scales of the blocks
+// are (the many-row kernel lets m stay below the maximum as long as half precision holds P, and scales
+// within 2^32 of the first one share m with the denominator).  The denominator, the sum of P_j / s_v, is
+// kept relative to a running maximum n of its own, that of z_j log2(e): scales of one sequence may lie as
+// far apart as fp32 reaches. So P fits half precision (11 bits, fewer below 2^-14, zero below 2^-25: a long
+// row loses at most its number of keys times 2^-25 of its largest contribution) and the codes (|c| <= 128)
+// are exact in it; a row of q is first divided by the power of two of its largest magnitude, which half
+// precision also holds (exact but for elements below 2^-14 of the largest).
 // Scores, maxima, sums and outputs are 32-bit.
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -501,7 +503,9 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 
 // Up to 16 rows per sequence and key/value head the keys' bytes bound the call, and 8- or 16-row tiles of
 // the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
-// all of them.  The keys of a tile are cut so that the tiles of the largest batch the bounds allow fill the
+// all of them.  Both sides of the limit, 32 / 8 heads, 4000 tokens: 12 and 16 rows, 16 sequences, 48 and 49 us (floor 19);
+// 20, 32 and 64 rows in 256-row tiles 91, 92 and 95 us, in 16-row tiles 74, 77 and 121; with 64 sequences 226, 226 and
+// 228 against 220, 222 and 414 (floor 78).  The keys of a tile are cut so that the tiles of the largest batch the bounds allow fill the
 // machine about twice, or four times where there are many tiles (many sequences, whose lengths differ), in
 // pieces of at least 128 keys (a step of each warp; prompt kernel: 512).  A piece costs about 3 us beside its
 // keys, the start and the join, so tiles that fill the machine by themselves are cut into 4096 keys or more
@@ -512,7 +516,8 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 // 64 of 1001 tokens 28 us (cut in four 36), 100 of 4001 tokens 137 us (whole 151), 200 of 2501 tokens 162 us
 // (cut in two 171); 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in two 48).  Where all pieces
 // are of one length they come in one wave: one sequence of 32001 tokens 20 us (two waves 24, 10 for its
-// bytes), 4 drafted tokens behind 32000 24 us (31), 12 windows of 1000 tokens 10.6 us (12).
+// bytes), 4 drafted tokens behind 32000 24 us (31), 12 windows of 1000 tokens 10.6 us (12).  The host knows bounds, not
+// lengths: that two sequences are about equally long is a guess (one of 32001 tokens beside one of 100: 25 us).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;

@@ -16,10 +16,12 @@
 // Scores and O live in tensor memory: 2 x 2 x 64 and 2 x d columns.
 //
 // Four prompts of up to 4000 tokens behind 500 older ones, 32 query and 8 key/value heads of 128: 524 us,
-// 971 TFLOP/s, 51% of the rate of a plain product.  Bound by the softmax warps: a tile of 256 rows and 128
-// keys takes about 3700 cycles, its matrix instructions 2033; without the softmax's arithmetic the call
-// would take 407 us, without the producers' stores 479, almost without matrix instructions still 505.  Start
-// and end of a block cost 17000 cycles of its about 90000.  Measured against it: two threads a row 686 (the
+// 971 TFLOP/s, 51% of the rate of a plain product.  A tile of 256 rows and 128 keys takes about 3700
+// cycles, its matrix instructions 2033; without the softmax's arithmetic the call would take 407 us,
+// without the producers' stores 479, without both 358, almost without matrix instructions still 505.  So
+// the softmax warps and the conversion share about two thirds of the distance to the matrix instructions'
+// 269 us; the rest is start and end of a block (17000 cycles of its about 90000) and the wait for the next
+// scores, which are asked for after P is handed over.  Measured against it: two threads a row 686 (the
 // exchange of their maxima), one 128-key score buffer 834, persistent blocks that load the next rows' q
 // early 709, eight producer warps with 136 softmax registers 574.
 #include <cuda.h>
@@ -315,6 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
             const float m1 = fmaxf(m, mx), alpha = ex2(m - finite_max(m1));
             if (!wild) l *= alpha;
             if (i > 0) {
+              // of the products' phases only step i - 1's can be open: this step's scores have arrived, and they were
+              // issued behind step i - 2's product
               ok = wait_bounded(bar(B_OFULL + half), (i - 1) & 1u, ctl, 3);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;

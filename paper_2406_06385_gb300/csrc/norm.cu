@@ -38,7 +38,7 @@ __device__ __forceinline__ float2 warp_sum_max(float2 v) {
 // max|h gamma|; rounding is monotone, so max|y| = fl(R max|h gamma|) exactly and no second
 // exchange is needed.  Bound by memory: what counts is loads in flight, so the fewest threads a row
 // (four words each) and as many rows at once as 64 registers a thread allow.  16384 rows of 5120 with
-// residual: 99.3 us, 6.76 TB/s; with two words a thread 115 us, with one 150 us.
+// residual: 99.5 us, 6.74 TB/s; with two words a thread 115 us, with one 150 us.
 template <int V>
 __global__ void __launch_bounds__(V == 1 ? 1024 : 512, V == 1 ? 1 : 2) add_rmsnorm_fwd_kernel(NormFwdArgs a, int wpr) {
   __shared__ float2 red[32];

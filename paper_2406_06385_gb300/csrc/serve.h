@@ -38,7 +38,7 @@ struct NormBwdArgs {
   float* part;              // [norm_bwd_parts][k] partial sums of dgamma
   int accumulate;
 };
-// Rows of the partial sums of dgamma (0 without dgamma).
+// Rows of the partial sums of dgamma that a call which writes dgamma needs.
 int64_t norm_bwd_parts(int64_t T, int64_t k, int sms);
 cudaError_t launch_add_rmsnorm_bwd(const NormBwdArgs& a, int sms, cudaStream_t stream);
 cudaError_t launch_act_dequant(const int8_t* codes, const float* scale, int64_t T, int64_t k, uint16_t* x_hat,
