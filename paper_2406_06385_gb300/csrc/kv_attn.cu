@@ -503,21 +503,22 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
 
 // Up to 16 rows per sequence and key/value head the keys' bytes bound the call, and 8- or 16-row tiles of
 // the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
-// all of them.  Both sides of the limit, 32 / 8 heads, 4000 tokens: 12 and 16 rows, 16 sequences, 48 and 49 us (floor 19);
-// 20, 32 and 64 rows in 256-row tiles 91, 92 and 95 us, in 16-row tiles 74, 77 and 121; with 64 sequences 226, 226 and
-// 228 against 220, 222 and 414 (floor 78).  The keys of a tile are cut so that the tiles of the largest batch the bounds allow fill the
-// machine about twice, or four times where there are many tiles (many sequences, whose lengths differ), in
-// pieces of at least 128 keys (a step of each warp; prompt kernel: 512).  A piece costs about 3 us beside its
-// keys, the start and the join, so tiles that fill the machine by themselves are cut into 4096 keys or more
-// (8-row tiles that fill it less than twice, whose last wave is far from full: 2304), and up to 1024 keys
-// stay whole where tiles fill half of it.  Measured, 8 key/value heads of 128: two sequences of 131002
-// tokens 88 us (79 for the bytes at the copy rate; cut twice as fine 92), 64 ragged sequences up to 8101
-// tokens 83 us (66; in five pieces at most, in two 90, whole 116, in sixteen 88), one of 1030 tokens 6.1 us,
-// 64 of 1001 tokens 28 us (cut in four 36), 100 of 4001 tokens 137 us (whole 151), 200 of 2501 tokens 162 us
-// (cut in two 171); 16 x 5 rows of 40 full heads, window 2048, 41 us (30; cut in two 48).  Where all pieces
-// are of one length they come in one wave: one sequence of 32001 tokens 20 us (two waves 24, 10 for its
-// bytes), 4 drafted tokens behind 32000 24 us (31), 12 windows of 1000 tokens 10.6 us (12).  The host knows bounds, not
-// lengths: that two sequences are about equally long is a guess (one of 32001 tokens beside one of 100: 25 us).
+// all of them.  Both sides of the limit, 32 / 8 heads, 4000 tokens: 12 and 16 rows, 16 sequences, 48 and 49
+// us (floor 19); 20, 32 and 64 rows in 256-row tiles 91, 92 and 95 us, in 16-row tiles 74, 77 and 121; with
+// 64 sequences 226, 226 and 228 against 220, 222 and 414 (floor 78).  The keys of a tile are cut so that
+// the tiles of the largest batch the bounds allow fill the machine about twice, or four times where there
+// are many tiles (many sequences, whose lengths differ), in pieces of at least 128 keys (a step of each
+// warp; prompt kernel: 512).  A piece costs about 3 us beside its keys, the start and the join, so tiles
+// that fill the machine by themselves are cut into 4096 keys or more (8-row tiles that fill it less than
+// twice, whose last wave is far from full: 2304), and up to 1024 keys stay whole where tiles fill half of
+// it.  Measured, 8 key/value heads of 128: two sequences of 131002 tokens 88 us (79 for the bytes at the
+// copy rate; cut twice as fine 92), 64 ragged sequences up to 8101 tokens 83 us (66; in five pieces at
+// most, in two 90, whole 116, in sixteen 88), one of 1030 tokens 6.1 us, 64 of 1001 tokens 28 us (cut in
+// four 36), 100 of 4001 tokens 137 us (whole 151), 200 of 2501 tokens 162 us (cut in two 171); 16 x 5 rows
+// of 40 full heads, window 2048, 41 us (30; cut in two 48).  Where all pieces are of one length they come
+// in one wave: one sequence of 32001 tokens 20 us (two waves 24, 10 for its bytes), 4 drafted tokens behind
+// 32000 24 us (31), 12 windows of 1000 tokens 10.6 us (12).  The host knows bounds, not lengths: that two
+// sequences are about equally long is a guess (one of 32001 tokens beside one of 100: 25 us).
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
