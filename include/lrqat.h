@@ -61,7 +61,7 @@ typedef enum {
   LRQAT_ERR_CUDA = -5,        /* a CUDA runtime/driver call or launch failed          */
   LRQAT_ERR_TIMEOUT = -6,     /* a kernel's bounded wait gave up (device status)      */
   LRQAT_ERR_RANGE = -7        /* device arrays of a batch contradict its bounds (device
-                                 status; lrqat_kv_write, _read and _attn)             */
+                                 status; the lrqat_kv_ calls)                         */
 } lrqat_status;
 
 /* Storage format of the frozen base Phi0 (Sec. 3, "Downcasting operator"). */
@@ -310,6 +310,51 @@ int lrqat_add_rmsnorm_bwd(const lrqat_norm* norm, int64_t T, const uint16_t* dY,
 int lrqat_act_dequant(const lrqat_norm* norm, int64_t T, const int8_t* codes, const float* s, uint16_t* X_hat,
                       lrqat_stream_t stream);
 
+/* ---- Norm of each head and rotation by position ------------------------------------
+ * Of the queries and keys behind a projection, for each head x of head_dim elements:
+ *   n = x / sqrt(mean(x^2) + eps) gamma                         (n = x where gamma is NULL),
+ * and of n's first rot_dim elements the pair (a, b) number i becomes
+ *   (a cos w - b sin w, a sin w + b cos w),  w = position freq_i;
+ * the elements behind rot_dim pass.  Everything between inputs and the rounded outputs is fp32, the sum of squares
+ * included; angles are exact to 2^-34 turns at any position. */
+typedef struct {
+  int32_t n_heads;      /* query heads, 0 .. 16384 (0: no queries)                        */
+  int32_t n_kv_heads;   /* key heads, 0 .. 16384 (0: no keys)                             */
+  int32_t head_dim;     /* a multiple of 16, at most 256                                  */
+  int32_t rot_dim;      /* a multiple of 16, at most head_dim; 0: no rotation             */
+  int32_t neighbours;   /* pair i: 0: elements i and i + rot_dim / 2; 1: 2 i and 2 i + 1  */
+  float eps;            /* >= 0                                                           */
+  const uint64_t* turns; /* device, [rot_dim / 2], 8-byte aligned: lrqat_rope_turns of the
+                           frequencies (NULL where rot_dim is 0)                          */
+} lrqat_qk_rope;
+
+/* turns[i] = freq[i] / (2 pi) modulo 1 as a 64-bit fraction, rounded to nearest.  Both are HOST arrays of n;
+ * freq in radians per position, finite, at most 2^20 in magnitude. */
+int lrqat_rope_turns(const double* freq, int32_t n, uint64_t* turns);
+
+/* Q, Q_out: bf16 [T, n_heads, head_dim], K, K_out: bf16 [T, n_kv_heads, head_dim], rows ldq, ldqo, ldk, ldko elements
+ * apart (multiples of 8), so that they may be parts of one projection's output; an output may be its input itself, but
+ * not overlap it otherwise.  pos: int32 [T], or NULL for row t at position t; a row at a negative position is padding and
+ * left as it is.  gamma_q, gamma_k: bf16 [head_dim] or NULL. */
+int lrqat_qk_rope_fwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* Q, int64_t ldq,
+                      const uint16_t* K, int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k,
+                      uint16_t* Q_out, int64_t ldqo, uint16_t* K_out, int64_t ldko, lrqat_stream_t stream);
+
+/* Bytes of workspace lrqat_qk_rope_bwd needs for T rows when it writes dgamma_q or dgamma_k (none without). */
+size_t lrqat_qk_rope_bwd_workspace_bytes(const lrqat_qk_rope* rope, int64_t T);
+
+/* Gradient at the inputs Q, K (read only where there is a gamma; else NULL allowed): with g the gradient of an output
+ * rotated back and r = 1 / sqrt(mean(x^2) + eps),
+ *   dx = r (g gamma - x r^2 mean(g gamma x))   (g where gamma is NULL),  dgamma = sum over rows and heads of g x r.
+ * dQ_out, dK_out, dQ, dK: bf16, laid out as the forward's arrays; dQ and dK may be one of dQ_out, dK_out, Q, K themselves.
+ * Rows at negative positions get a zero gradient and add nothing to dgamma.  dgamma_q, dgamma_k: fp32 [head_dim] or
+ * NULL; accumulate = 1 adds to them.  Sums run in a fixed order. */
+int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* dQ_out, int64_t lddqo,
+                      const uint16_t* dK_out, int64_t lddko, const uint16_t* Q, int64_t ldq, const uint16_t* K,
+                      int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k, uint16_t* dQ, int64_t lddq,
+                      uint16_t* dK, int64_t lddk, float* dgamma_q, float* dgamma_k, int accumulate, void* workspace,
+                      size_t workspace_bytes, lrqat_stream_t stream);
+
 /* ---- 8-bit key / value cache (the KV8 of the W4A8KV8 runs, Sec. 4) ----------------
  * A pool of blocks of `block` tokens.  Codes are int8 [n_blocks, n_kv_heads, block,
  * head_dim], with one fp32 scale per block and head, [n_blocks, n_kv_heads]:
@@ -345,6 +390,49 @@ typedef struct {
   int32_t max_rows;           /* bound on the rows of one sequence                    */
   int32_t max_len;            /* bound on len, at most max_blocks * block             */
 } lrqat_kv_batch;
+
+/* Block tables of running sequences and the list of free blocks, on the device: what makes a batch out of request
+ * lengths.  A sequence of n tokens holds ceil(n / block) columns of its row of block_table; the first `pinned` columns of
+ * every row are the caller's (such as a prefix that sequences share): never handed out, never taken back.  The first
+ * *free_count entries of free_ids are the free blocks; the rest of it, and table entries behind a sequence's columns,
+ * hold nothing. */
+typedef struct {
+  int32_t n_seqs;        /* 1 .. 65535                                   */
+  int32_t max_blocks;    /* columns of block_table                       */
+  int32_t block;         /* tokens of a block: 16, 32, 64 or 128         */
+  int32_t pinned;        /* 0 .. max_blocks                              */
+  int64_t capacity;      /* entries of free_ids, 1 .. 2^31 - 1           */
+  int32_t* block_table;  /* [n_seqs, max_blocks]                         */
+  int32_t* free_ids;     /* [capacity]                                   */
+} lrqat_kv_blocks;
+
+/* Bytes of workspace lrqat_kv_extend and lrqat_kv_truncate need. */
+size_t lrqat_kv_blocks_workspace_bytes(const lrqat_kv_blocks* blocks);
+
+/* Makes room for add[b] new tokens behind sequence b's len[b] (add[b] > 0), or for -add[b] rows of padding (such as the
+ * row of an idle slot), and lays the batch out:
+ *   row_start[b] = sum of |add| over the sequences before b (saturating), [n_seqs + 1];
+ *   new columns take blocks from the end of the list, sequence by sequence and column by column;
+ *   len_out[b]: the sequence's length with its new tokens;
+ *   batch_len[b]: the `len` of lrqat_kv_batch, len_out[b], or 0 for a sequence with padding;
+ *   pos, slot [rows]: position of a row (what lrqat_qk_rope_fwd takes) and its place in the cache, block id times block
+ *   plus the place within it; -1 for padding and for rows behind the last sequence's.  slot may be NULL.
+ *   *free_out: free blocks that are left.
+ * A sequence that does not fit its row of the table or whose rows do not fit `rows`, and from the first one on whose blocks
+ * the list cannot give all that ask for blocks, takes no tokens: its rows are padding, and lrqat_get_device_status reports
+ * LRQAT_ERR_RANGE.  len_out may be len and free_out free_count; the other arrays must not overlap.  rows: at most 2^31 - 1. */
+int lrqat_kv_extend(const lrqat_kv_blocks* blocks, const int32_t* len, const int32_t* add, const int32_t* free_count,
+                    int64_t rows, int32_t* len_out, int32_t* free_out, int32_t* batch_len, int32_t* row_start,
+                    int32_t* pos, int64_t* slot, void* workspace, size_t workspace_bytes, lrqat_stream_t stream);
+
+/* Shortens sequence b to keep[b] tokens (rejected drafts; 0 or less: the sequence is finished; len[b] or more: it stays)
+ * and appends the blocks it no longer needs to the list, in the order that hands the same ones out again.  len_out may be
+ * len and free_out free_count.  A length outside the table's row, or more blocks than the list has entries: the sequence
+ * stays as it is (with the list full, all behind it that would give blocks back), and lrqat_get_device_status reports
+ * LRQAT_ERR_RANGE. */
+int lrqat_kv_truncate(const lrqat_kv_blocks* blocks, const int32_t* len, const int32_t* keep, const int32_t* free_count,
+                      int32_t* len_out, int32_t* free_out, void* workspace, size_t workspace_bytes,
+                      lrqat_stream_t stream);
 
 /* Quantizes the batch's new keys and values into the cache.  For each block and head, with a the
  * largest magnitude among the block's new tokens:

@@ -99,3 +99,96 @@ def attention(q, k, v, length, softmax_scale, window=0):
             out[i, h] = p @ v[lo:pos + 1, h // group]
             mass[i, h] = p @ np.abs(v[lo:pos + 1, h // group])
     return out, mass, seen
+
+
+def rotate(x, pos, freq, neighbours=False, back=False):
+    """Rows x [n, heads, d] at positions pos [n]: pair i of the first 2 len(freq) elements of each head turned by the
+    angle pos freq[i] (by its negative where `back`)."""
+    x = np.array(x, F64)
+    rot = 2 * len(freq)
+    # the angle modulo a turn in extended precision: positions reach 2^31
+    w = np.asarray(pos, np.longdouble)[:, None] * np.asarray(freq, np.longdouble)[None]
+    w = np.remainder(w, 2 * np.longdouble("3.14159265358979323846264338327950288")).astype(F64)[:, None]
+    c, s = np.cos(w), np.sin(w) * (-1 if back else 1)
+    a, b = (x[..., 0:rot:2], x[..., 1:rot:2]) if neighbours else (x[..., :rot // 2], x[..., rot // 2:rot])
+    a, b = a * c - b * s, a * s + b * c
+    if neighbours:
+        x[..., 0:rot:2], x[..., 1:rot:2] = a, b
+    else:
+        x[..., :rot // 2], x[..., rot // 2:rot] = a, b
+    return x
+
+
+def head_norm_rope(x, gamma, pos, freq, eps, neighbours=False):
+    """Norm of each head of x [n, heads, d] (none where gamma is None), then its rotation."""
+    x = np.asarray(x, F64)
+    if gamma is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(gamma, F64)
+    return rotate(x, pos, freq, neighbours)
+
+
+def head_norm_rope_bwd(dy, x, gamma, pos, freq, eps, neighbours=False):
+    """(dx, dgamma) of head_norm_rope at x; dgamma is None where gamma is."""
+    g = rotate(dy, pos, freq, neighbours, back=True)
+    if gamma is None:
+        return g, None
+    x, gamma = np.asarray(x, F64), np.asarray(gamma, F64)
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    dx = r * (g * gamma - x * r * r * (g * gamma * x).mean(-1, keepdims=True))
+    return dx, (g * x * r).sum((0, 1))
+
+
+class Blocks:
+    """Tables [n_seqs][max_blocks] and the list of free blocks; `len` per sequence."""
+
+    def __init__(self, table, free_ids, free, length, block, pinned=0):
+        self.table, self.free_ids = np.array(table, np.int32), np.array(free_ids, np.int32)
+        self.free, self.len, self.block, self.pinned = int(free), [int(n) for n in length], block, pinned
+
+    def extend(self, add, rows):
+        """(batch lengths, row starts, positions, slots, whether a sequence was refused)."""
+        P, most = self.block, self.table.shape[1] * self.block
+        start, batch_len, pos, slot = [0], [], [-1] * rows, [-1] * rows
+        ok_all, dry, free = True, False, self.free if 0 <= self.free <= len(self.free_ids) else 0
+        ok_all = free == self.free
+        for b, a in enumerate(int(a) for a in add):
+            r0, n = start[-1], self.len[b]
+            start.append(r0 + abs(a))
+            ok = 0 <= n <= most and n + max(a, 0) <= most and start[-1] <= rows
+            new = [c for c in range(self.pinned, -(-(n + a) // P)) if c * P >= n] if ok and a > 0 else []
+            if new and (dry or len(new) > free):
+                ok, dry = False, True
+            ok_all &= ok
+            batch_len.append(n + a if ok and a >= 0 else 0)
+            if not ok or a <= 0:
+                continue
+            for c in new:
+                free -= 1
+                self.table[b, c] = self.free_ids[free]
+            for i in range(a):
+                pos[r0 + i] = n + i
+                slot[r0 + i] = int(self.table[b, (n + i) // P]) * P + (n + i) % P
+            self.len[b] = n + a
+        if 0 <= self.free <= len(self.free_ids):
+            self.free = free
+        return batch_len, [min(r, 2 ** 31 - 1) for r in start], pos, slot, not ok_all
+
+    def truncate(self, keep):
+        """Whether a sequence was refused."""
+        P, most, known = self.block, self.table.shape[1] * self.block, 0 <= self.free <= len(self.free_ids)
+        back, full, ok_all = [], False, known
+        for b, k in enumerate(int(k) for k in keep):
+            n = self.len[b]
+            k = min(n, max(k, 0))
+            if not 0 <= n <= most:
+                ok_all = False
+                continue
+            gone = [int(self.table[b, c]) for c in range(max(-(-k // P), self.pinned), -(-n // P))]
+            if gone and (full or not known or self.free + len(back) + len(gone) > len(self.free_ids)):
+                ok_all, full = False, True
+                continue
+            back += gone
+            self.len[b] = k
+        self.free_ids[self.free:self.free + len(back)] = back[::-1]
+        self.free += len(back)
+        return not ok_all

@@ -19,7 +19,7 @@ LIB_DIR = os.path.join(PKG, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "liblrqat.so")
 
 SOURCES = ["elementwise.cu", "fused_gemm.cu", "fused_pair.cu", "dw.cu", "dw_pair.cu", "merge.cu", "optim.cu", "norm.cu",
-           "kv_cache.cu", "kv_attn.cu", "kv_prompt.cu", "lrqat_api.cu"]
+           "rope.cu", "kv_blocks.cu", "kv_cache.cu", "kv_attn.cu", "kv_prompt.cu", "lrqat_api.cu"]
 HEADERS = ["kernels.h", "merge.h", "ptx.cuh", "quant.cuh", "serve.h", "serve.cuh",
            "attn.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

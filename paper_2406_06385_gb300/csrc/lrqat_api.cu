@@ -686,6 +686,92 @@ int attn_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t 
     return fail(LRQAT_ERR_UNSUPPORTED, "too many (token, head) rows in one sequence");
   return LRQAT_OK;
 }
+
+// ------------------------------------------------- head norm and rotation --
+constexpr int kMaxHeads = 16384, kMaxRopeDim = 256;
+
+int validate_rope(const lrqat_qk_rope* r, int64_t T) {
+  if (!r) return fail(LRQAT_ERR_INVALID_ARG, "rope is NULL");
+  if (T < 1) return fail(LRQAT_ERR_INVALID_ARG, "T must be positive (T=%lld)", (long long)T);
+  if (T > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "T too large (T=%lld)", (long long)T);
+  if (r->n_heads < 0 || r->n_kv_heads < 0 || r->n_heads + static_cast<int64_t>(r->n_kv_heads) < 1)
+    return fail(LRQAT_ERR_INVALID_ARG, "n_heads and n_kv_heads must be >= 0, one of them positive");
+  if (r->n_heads > kMaxHeads || r->n_kv_heads > kMaxHeads)
+    return fail(LRQAT_ERR_UNSUPPORTED, "more than %d heads", kMaxHeads);
+  if (r->head_dim < 1 || r->rot_dim < 0 || r->rot_dim > r->head_dim)
+    return fail(LRQAT_ERR_INVALID_ARG, "head_dim must be positive and rot_dim between 0 and head_dim (%d, %d)", r->head_dim,
+                r->rot_dim);
+  if (r->head_dim % 16 || r->head_dim > kMaxRopeDim || r->rot_dim % 16)
+    return fail(LRQAT_ERR_UNSUPPORTED, "head_dim (at most %d) and rot_dim must be multiples of 16 (got %d, %d)", kMaxRopeDim,
+                r->head_dim, r->rot_dim);
+  if (r->neighbours != 0 && r->neighbours != 1) return fail(LRQAT_ERR_INVALID_ARG, "neighbours must be 0 or 1");
+  if (!(r->eps >= 0.0f) || !std::isfinite(r->eps)) return fail(LRQAT_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (r->rot_dim > 0 && !r->turns) return fail(LRQAT_ERR_INVALID_ARG, "turns must be non-NULL where rot_dim is positive");
+  if (reinterpret_cast<uintptr_t>(r->turns) & 7u) return fail(LRQAT_ERR_ALIGNMENT, "turns must be 8-byte aligned");
+  return LRQAT_OK;
+}
+
+RopeArgs rope_args(const lrqat_qk_rope& r, int64_t T) {
+  RopeArgs a{};
+  a.T = T;
+  a.heads[0] = r.n_heads;
+  a.heads[1] = r.n_kv_heads;
+  a.d = r.head_dim;
+  a.rot = r.rot_dim;
+  a.eps = r.eps;
+  a.turns = r.turns;
+  return a;
+}
+
+// ------------------------------------------------------- blocks of the cache --
+int blocks_args(const lrqat_kv_blocks* b, BlocksArgs* a) {
+  if (!b) return fail(LRQAT_ERR_INVALID_ARG, "blocks is NULL");
+  if (b->n_seqs < 1 || b->max_blocks < 1 || b->capacity < 1 || b->pinned < 0 || b->pinned > b->max_blocks)
+    return fail(LRQAT_ERR_INVALID_ARG, "n_seqs, max_blocks and capacity must be positive, pinned within 0 .. max_blocks");
+  if (b->n_seqs > 65535) return fail(LRQAT_ERR_UNSUPPORTED, "n_seqs %d > 65535", b->n_seqs);
+  if (b->capacity > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "capacity too large");
+  if (b->block != 16 && b->block != 32 && b->block != 64 && b->block != 128)
+    return fail(LRQAT_ERR_UNSUPPORTED, "block must be 16, 32, 64 or 128 (got %d)", b->block);
+  if (static_cast<int64_t>(b->max_blocks) * b->block > INT32_MAX - 1024)
+    return fail(LRQAT_ERR_UNSUPPORTED, "max_blocks * block does not fit 32 bits");
+  if (!b->block_table || !b->free_ids) return fail(LRQAT_ERR_INVALID_ARG, "block_table and free_ids must be non-NULL");
+  if ((reinterpret_cast<uintptr_t>(b->block_table) | reinterpret_cast<uintptr_t>(b->free_ids)) & 3u)
+    return fail(LRQAT_ERR_ALIGNMENT, "block_table and free_ids must be 4-byte aligned");
+  *a = BlocksArgs{};
+  a->n_seqs = b->n_seqs;
+  a->max_blocks = b->max_blocks;
+  a->block_log2 = b->block == 16 ? 4 : b->block == 32 ? 5 : b->block == 64 ? 6 : 7;
+  a->pinned = b->pinned;
+  a->capacity = b->capacity;
+  a->table = b->block_table;
+  a->free_ids = b->free_ids;
+  return LRQAT_OK;
+}
+size_t blocks_workspace(const BlocksArgs& a) { return (static_cast<size_t>(a.n_seqs) + 1) * sizeof(int4); }
+
+// The arrays that extending and shortening share, and the workspace.
+int blocks_state(BlocksArgs* a, const int32_t* len, const int32_t* change, const int32_t* free_count, int32_t* len_out,
+                 int32_t* free_out, void* workspace, size_t workspace_bytes) {
+  if (!len || !change || !free_count || !len_out || !free_out)
+    return fail(LRQAT_ERR_INVALID_ARG, "len, the requests, free_count, len_out and free_out must be non-NULL");
+  if ((reinterpret_cast<uintptr_t>(len) | reinterpret_cast<uintptr_t>(change) | reinterpret_cast<uintptr_t>(free_count) |
+       reinterpret_cast<uintptr_t>(len_out) | reinterpret_cast<uintptr_t>(free_out)) & 3u)
+    return fail(LRQAT_ERR_ALIGNMENT, "len, the requests, free_count, len_out and free_out must be 4-byte aligned");
+  const size_t need = blocks_workspace(*a);
+  if (!workspace || workspace_bytes < need)
+    return fail(LRQAT_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
+  if (!aligned16(workspace)) return fail(LRQAT_ERR_ALIGNMENT, "workspace is not 16-byte aligned");
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  a->status = dev->status;
+  a->len = len;
+  a->free_count = free_count;
+  a->len_out = len_out;
+  a->free_out = free_out;
+  a->info = static_cast<int4*>(workspace);
+  return LRQAT_OK;
+}
+
 }  // namespace
 }  // namespace lrqat
 
@@ -1372,6 +1458,152 @@ int lrqat_act_dequant(const lrqat_norm* norm, int64_t T, const int8_t* codes, co
   LRQAT_CHECK_PTR(s, "s");
   LRQAT_CHECK_PTR(X_hat, "X_hat");
   LRQAT_LAUNCH("act_dequant", 1, stream, launch_act_dequant(codes, s, T, norm->k, X_hat, stream), "dequantizer launch");
+  return LRQAT_OK;
+}
+
+int lrqat_rope_turns(const double* freq, int32_t n, uint64_t* turns) {
+  if (n < 0 || (n > 0 && (!freq || !turns))) return fail(LRQAT_ERR_INVALID_ARG, "freq and turns must be non-NULL, n >= 0");
+  // 1 / (2 pi) in 192 fractional bits, from the top
+  static const uint64_t inv[3] = {0x28be60db9391054aull, 0x7f09d5f47d4d3770ull, 0x36d8a5664f10e410ull};
+  for (int32_t i = 0; i < n; ++i) {
+    if (!std::isfinite(freq[i]) || std::fabs(freq[i]) > 0x1p20)
+      return fail(LRQAT_ERR_INVALID_ARG, "freq[%d] must be finite and at most 2^20 in magnitude", i);
+    int e = 0;
+    const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(freq[i]), &e), 53));
+    // |freq| = m 2^(e - 53); p = m times the fraction is |freq| / (2 pi) in units of 2^(e - 53 - 192)
+    uint64_t p[4] = {0, 0, 0, 0};                          // from the bottom
+    for (int w = 0; w < 3; ++w) {
+      const unsigned __int128 v = static_cast<unsigned __int128>(m) * inv[2 - w] + p[w];
+      p[w] = static_cast<uint64_t>(v);
+      p[w + 1] = static_cast<uint64_t>(v >> 64);
+    }
+    const int shift = 192 + 53 - e - 64;                   // from units of 2^(e - 245) to 2^-64: at least 160
+    auto bits = [&](int from) {                            // 64 bits of p from bit `from` on
+      if (from >= 256) return uint64_t{0};
+      const int w = from / 64, b = from % 64;
+      uint64_t v = p[w] >> b;
+      if (b && w + 1 < 4) v |= p[w + 1] << (64 - b);
+      return v;
+    };
+    const uint64_t t = bits(shift) + (bits(shift - 1) & 1u);
+    turns[i] = freq[i] < 0.0 ? 0u - t : t;
+  }
+  return LRQAT_OK;
+}
+
+int lrqat_qk_rope_fwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* Q, int64_t ldq,
+                      const uint16_t* K, int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k,
+                      uint16_t* Q_out, int64_t ldqo, uint16_t* K_out, int64_t ldko, lrqat_stream_t stream) {
+  LRQAT_TRY(validate_rope(rope, T));
+  RopeArgs a = rope_args(*rope, T);
+  if (reinterpret_cast<uintptr_t>(pos) & 3u) return fail(LRQAT_ERR_ALIGNMENT, "pos must be 4-byte aligned");
+  a.pos = pos;
+  const uint16_t* in[2] = {Q, K};
+  const uint16_t* gamma[2] = {gamma_q, gamma_k};
+  uint16_t* out[2] = {Q_out, K_out};
+  const int64_t ld[2] = {ldq, ldk}, ldo[2] = {ldqo, ldko};
+  for (int i = 0; i < 2; ++i) {
+    if (a.heads[i] == 0) continue;
+    const int64_t width = static_cast<int64_t>(a.heads[i]) * a.d;
+    LRQAT_TRY(check_rows(in[i], ld[i], width, i ? "K" : "Q"));
+    LRQAT_TRY(check_rows(out[i], ldo[i], width, i ? "K_out" : "Q_out"));
+    if (!aligned16(gamma[i])) return fail(LRQAT_ERR_ALIGNMENT, "gamma is not 16-byte aligned");
+    a.X[i] = in[i], a.ldx[i] = ld[i], a.gamma[i] = gamma[i], a.Y[i] = out[i], a.ldy[i] = ldo[i];
+  }
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  LRQAT_LAUNCH("qk_rope_fwd", 1, stream, launch_rope_fwd(a, rope->neighbours != 0, dev->sms, stream), "rotation launch");
+  return LRQAT_OK;
+}
+
+size_t lrqat_qk_rope_bwd_workspace_bytes(const lrqat_qk_rope* rope, int64_t T) {
+  if (validate_rope(rope, T) != LRQAT_OK) return 0;
+  return static_cast<size_t>(rope_bwd_parts(rope_args(*rope, T), sm_count())) * 2 * rope->head_dim * sizeof(float);
+}
+
+int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* dQ_out, int64_t lddqo,
+                      const uint16_t* dK_out, int64_t lddko, const uint16_t* Q, int64_t ldq, const uint16_t* K,
+                      int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k, uint16_t* dQ, int64_t lddq,
+                      uint16_t* dK, int64_t lddk, float* dgamma_q, float* dgamma_k, int accumulate, void* workspace,
+                      size_t workspace_bytes, lrqat_stream_t stream) {
+  LRQAT_TRY(validate_rope(rope, T));
+  RopeBwdArgs a{};
+  a.f = rope_args(*rope, T);
+  if (reinterpret_cast<uintptr_t>(pos) & 3u) return fail(LRQAT_ERR_ALIGNMENT, "pos must be 4-byte aligned");
+  a.f.pos = pos;
+  const uint16_t* dy[2] = {dQ_out, dK_out};
+  const uint16_t* x[2] = {Q, K};
+  const uint16_t* gamma[2] = {gamma_q, gamma_k};
+  uint16_t* dx[2] = {dQ, dK};
+  float* dgamma[2] = {dgamma_q, dgamma_k};
+  const int64_t lddy[2] = {lddqo, lddko}, ldx[2] = {ldq, ldk}, lddx[2] = {lddq, lddk};
+  for (int i = 0; i < 2; ++i) {
+    if (dgamma[i] && (!gamma[i] || a.f.heads[i] == 0))
+      return fail(LRQAT_ERR_INVALID_ARG, "the gradient of a gamma that is not there");
+    if (a.f.heads[i] == 0) continue;
+    const int64_t width = static_cast<int64_t>(a.f.heads[i]) * a.f.d;
+    LRQAT_TRY(check_rows(dy[i], lddy[i], width, i ? "dK_out" : "dQ_out"));
+    LRQAT_TRY(check_rows(dx[i], lddx[i], width, i ? "dK" : "dQ"));
+    if (gamma[i]) LRQAT_TRY(check_rows(x[i], ldx[i], width, i ? "K" : "Q"));
+    if (!aligned16(gamma[i]) || !aligned16(dgamma[i])) return fail(LRQAT_ERR_ALIGNMENT, "gamma or dgamma is not 16-byte aligned");
+    a.dY[i] = dy[i], a.lddy[i] = lddy[i], a.f.gamma[i] = gamma[i], a.f.Y[i] = dx[i], a.f.ldy[i] = lddx[i];
+    a.f.X[i] = gamma[i] ? x[i] : nullptr, a.f.ldx[i] = gamma[i] ? ldx[i] : 0, a.dgamma[i] = dgamma[i];
+  }
+  const bool sums = dgamma_q || dgamma_k;
+  if (sums) {
+    const size_t need = lrqat_qk_rope_bwd_workspace_bytes(rope, T);
+    if (!workspace || workspace_bytes < need)
+      return fail(LRQAT_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
+    if (!aligned16(workspace)) return fail(LRQAT_ERR_ALIGNMENT, "workspace is not 16-byte aligned");
+    a.part = static_cast<float*>(workspace);
+  }
+  a.accumulate = accumulate;
+  DeviceInfo* dev = nullptr;
+  LRQAT_TRY(device_info(&dev));
+  LRQAT_LAUNCH("qk_rope_bwd", sums ? 2 : 1, stream, launch_rope_bwd(a, rope->neighbours != 0, dev->sms, stream),
+               "rotation backward launch");
+  return LRQAT_OK;
+}
+
+size_t lrqat_kv_blocks_workspace_bytes(const lrqat_kv_blocks* blocks) {
+  BlocksArgs a;
+  return blocks_args(blocks, &a) == LRQAT_OK ? blocks_workspace(a) : 0;
+}
+
+int lrqat_kv_extend(const lrqat_kv_blocks* blocks, const int32_t* len, const int32_t* add, const int32_t* free_count,
+                    int64_t rows, int32_t* len_out, int32_t* free_out, int32_t* batch_len, int32_t* row_start,
+                    int32_t* pos, int64_t* slot, void* workspace, size_t workspace_bytes, lrqat_stream_t stream) {
+  ExtendArgs a{};
+  LRQAT_TRY(blocks_args(blocks, &a.b));
+  if (rows < 0) return fail(LRQAT_ERR_INVALID_ARG, "rows must be >= 0");
+  if (rows > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "rows too large");
+  if (!batch_len || !row_start || (rows > 0 && !pos))
+    return fail(LRQAT_ERR_INVALID_ARG, "batch_len, row_start and pos must be non-NULL");
+  if (batch_len == len || batch_len == len_out || batch_len == add)
+    return fail(LRQAT_ERR_INVALID_ARG, "batch_len must not be one of the other arrays");
+  if (((reinterpret_cast<uintptr_t>(batch_len) | reinterpret_cast<uintptr_t>(row_start) | reinterpret_cast<uintptr_t>(pos)) & 3u) ||
+      (reinterpret_cast<uintptr_t>(slot) & 7u))
+    return fail(LRQAT_ERR_ALIGNMENT, "batch_len, row_start and pos must be 4-byte aligned, slot 8-byte aligned");
+  LRQAT_TRY(blocks_state(&a.b, len, add, free_count, len_out, free_out, workspace, workspace_bytes));
+  a.add = add;
+  a.rows = rows;
+  a.batch_len = batch_len;
+  a.row_start = row_start;
+  a.pos = pos;
+  a.slot = slot;
+  LRQAT_LAUNCH("kv_extend", kv_extend_launches(rows), stream, launch_kv_extend(a, stream), "block table launch");
+  return LRQAT_OK;
+}
+
+int lrqat_kv_truncate(const lrqat_kv_blocks* blocks, const int32_t* len, const int32_t* keep, const int32_t* free_count,
+                      int32_t* len_out, int32_t* free_out, void* workspace, size_t workspace_bytes,
+                      lrqat_stream_t stream) {
+  TruncateArgs a{};
+  LRQAT_TRY(blocks_args(blocks, &a.b));
+  LRQAT_TRY(blocks_state(&a.b, len, keep, free_count, len_out, free_out, workspace, workspace_bytes));
+  a.keep = keep;
+  LRQAT_LAUNCH("kv_truncate", kv_truncate_launches(a.b.n_seqs), stream, launch_kv_truncate(a, stream),
+               "block table launch");
   return LRQAT_OK;
 }
 

@@ -44,6 +44,66 @@ cudaError_t launch_add_rmsnorm_bwd(const NormBwdArgs& a, int sms, cudaStream_t s
 cudaError_t launch_act_dequant(const int8_t* codes, const float* scale, int64_t T, int64_t k, uint16_t* x_hat,
                                cudaStream_t stream);
 
+// ---- rope.cu -----------------------------------------------------------------
+// [0]: queries, [1]: keys.
+struct RopeArgs {
+  int64_t T;
+  int heads[2];             // 0: none
+  int d, rot;
+  float eps;
+  const uint64_t* turns;    // [rot / 2] freq / (2 pi) as 64-bit fractions
+  const int32_t* pos;       // [T] or nullptr: row t at position t
+  const uint16_t* X[2];
+  int64_t ldx[2];
+  const uint16_t* gamma[2]; // or nullptr: no norm
+  uint16_t* Y[2];           // backward: the gradient of X
+  int64_t ldy[2];
+};
+struct RopeBwdArgs {
+  RopeArgs f;
+  const uint16_t* dY[2];
+  int64_t lddy[2];
+  float* dgamma[2];         // [d] or nullptr
+  float* part;              // [rope_bwd_parts][2][d], nullptr without dgamma
+  int accumulate;
+};
+// Rows of the partial sums of dgamma.
+int64_t rope_bwd_parts(const RopeArgs& a, int sms);
+// neighbours: pairs (2 i, 2 i + 1), else (i, i + rot / 2).
+cudaError_t launch_rope_fwd(const RopeArgs& a, bool neighbours, int sms, cudaStream_t stream);
+cudaError_t launch_rope_bwd(const RopeBwdArgs& a, bool neighbours, int sms, cudaStream_t stream);
+
+// ---- kv_blocks.cu ------------------------------------------------------------
+struct BlocksArgs {
+  int n_seqs, max_blocks, block_log2, pinned;
+  int64_t capacity;         // entries of free_ids
+  int32_t* table;           // [n_seqs][max_blocks]
+  int32_t* free_ids;
+  const int32_t* len;       // [n_seqs]
+  const int32_t* free_count;
+  int32_t* len_out;         // may be len
+  int32_t* free_out;        // may be free_count
+  int4* info;               // [n_seqs + 1]
+  int* status;
+};
+struct ExtendArgs {
+  BlocksArgs b;
+  const int32_t* add;
+  int64_t rows;
+  int32_t* batch_len;       // [n_seqs]
+  int32_t* row_start;       // [n_seqs + 1]
+  int32_t* pos;             // [rows]
+  int64_t* slot;            // [rows] or nullptr
+};
+struct TruncateArgs {
+  BlocksArgs b;
+  const int32_t* keep;
+};
+int kv_extend_launches(int64_t rows);
+int kv_truncate_launches(int64_t n_seqs);
+cudaError_t launch_kv_extend(const ExtendArgs& a, cudaStream_t stream);
+cudaError_t launch_kv_truncate(const TruncateArgs& a, cudaStream_t stream);
+
 // ---- kv_cache.cu, kv_attn.cu ---------------------------------------------------
 // A paged cache and a ragged batch of its sequences (lrqat_kv_cache, lrqat_kv_batch).
 struct KvArgs {

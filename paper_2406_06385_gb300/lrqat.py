@@ -134,6 +134,52 @@ class KVBatch(ctypes.Structure):
         return batch
 
 
+class QKRope(ctypes.Structure):
+    """Mirror of lrqat_qk_rope."""
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("neighbours", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("turns", ctypes.c_void_p)]
+
+    @classmethod
+    def of(cls, n_heads: int, n_kv_heads: int, head_dim: int, turns, neighbours: bool = False,
+           eps: float = 1e-6) -> "QKRope":
+        """`turns`: rope_turns of the frequencies on the device (int64, one for each pair that rotates), or None; it is
+        kept alive."""
+        if turns is not None:
+            import torch
+            if turns.dtype is not torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or not turns.is_cuda:
+                raise LrqatError(-1, "turns must be a dense int64 vector on the device")
+        rope = cls(n_heads, n_kv_heads, head_dim, 0 if turns is None else 2 * turns.numel(), int(neighbours), eps,
+                   _ptr(turns))
+        rope.turns_tensor = turns
+        return rope
+
+
+class KVBlocks(ctypes.Structure):
+    """Mirror of lrqat_kv_blocks."""
+    _fields_ = [("n_seqs", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("pinned", ctypes.c_int32), ("capacity", ctypes.c_int64), ("block_table", ctypes.c_void_p),
+                ("free_ids", ctypes.c_void_p)]
+    device = None                      # get_device() of the tensors, where `of` has seen them
+
+    @classmethod
+    def of(cls, block_table, free_ids, block: int, pinned: int = 0) -> "KVBlocks":
+        """`block_table` int32 [n_seqs, max_blocks], `free_ids` int32 [capacity], dense device tensors, which are kept
+        alive."""
+        i32 = (_types or _dtypes())[2]
+        if block_table.dim() != 2 or free_ids.dim() != 1 or not (block_table.is_contiguous() and free_ids.is_contiguous()):
+            raise LrqatError(-1, "block_table and free_ids must be dense, of two and one dimensions")
+        if not block_table.dtype is free_ids.dtype is i32:
+            raise LrqatError(-1, "block_table and free_ids must be int32")
+        if block_table.device != free_ids.device or not block_table.is_cuda:
+            raise LrqatError(-1, "block_table and free_ids must lie on one device")
+        n_seqs, max_blocks = block_table.shape
+        blocks = cls(n_seqs, max_blocks, block, pinned, free_ids.shape[0], block_table.data_ptr(), free_ids.data_ptr())
+        blocks.tensors = (block_table, free_ids)
+        blocks.device = block_table.get_device()
+        return blocks
+
+
 _lib = None
 
 
@@ -165,11 +211,18 @@ def lib() -> ctypes.CDLL:
                                  vp],
         }
         np_, cp, bp = ctypes.POINTER(Norm), ctypes.POINTER(KVCache), ctypes.POINTER(KVBatch)
+        rp, tp = ctypes.POINTER(QKRope), ctypes.POINTER(KVBlocks)
         i32, f32 = ctypes.c_int32, ctypes.c_float
         sigs.update({
             "lrqat_add_rmsnorm_fwd": [np_, i64, vp, vp, vp, vp, vp, vp, vp, vp],
             "lrqat_add_rmsnorm_bwd": [np_, i64, vp, vp, vp, vp, vp, vp, ip, vp, sz, vp],
             "lrqat_act_dequant": [np_, i64, vp, vp, vp, vp],
+            "lrqat_rope_turns": [vp, i32, vp],
+            "lrqat_qk_rope_fwd": [rp, i64, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp],
+            "lrqat_qk_rope_bwd": [rp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, ip,
+                                  vp, sz, vp],
+            "lrqat_kv_extend": [tp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+            "lrqat_kv_truncate": [tp, vp, vp, vp, vp, vp, vp, sz, vp],
             "lrqat_kv_write": [cp, bp, vp, i64, vp, i64, vp],
             "lrqat_kv_read": [cp, bp, vp, i64, vp, i64, vp],
             "lrqat_kv_attn": [cp, bp, i32, f32, i32, vp, i64, vp, i64, vp, sz, vp],
@@ -198,6 +251,10 @@ def lib() -> ctypes.CDLL:
             fn.restype = ctypes.c_size_t
         L.lrqat_add_rmsnorm_bwd_workspace_bytes.argtypes = [np_, i64]
         L.lrqat_add_rmsnorm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.lrqat_qk_rope_bwd_workspace_bytes.argtypes = [rp, i64]
+        L.lrqat_qk_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.lrqat_kv_blocks_workspace_bytes.argtypes = [tp]
+        L.lrqat_kv_blocks_workspace_bytes.restype = ctypes.c_size_t
         L.lrqat_kv_attn_workspace_bytes.argtypes = [cp, bp, i32, i32]
         L.lrqat_kv_attn_workspace_bytes.restype = ctypes.c_size_t
         _lib = L
@@ -233,6 +290,19 @@ def _stream(stream) -> Optional[int]:
     if _current_stream is None:
         _current_stream = _current_stream_source()
     return _current_stream()
+
+
+_current_device = None
+
+
+def _on_current(device: int) -> None:
+    """Refuses tensors of another device than the current one, on which the library launches."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if device != _current_device():
+        raise LrqatError(-1, f"the tensors lie on device {device}, which is not the current one")
 
 
 def last_error() -> str:
@@ -373,6 +443,147 @@ def _row_array(t, heads: int, d: int, rows: int, device) -> int:
     if t.get_device() != device and (device is not None or not t.is_cuda):
         raise LrqatError(-1, "row arrays must lie on the device of the cache and the batch")
     return _rows(t, heads, d, rows)
+
+
+def rope_turns(freq):
+    """The frequencies `freq` (radians a position: base ** (-2 i / rot_dim), or a scaled variant) as the fractions of a turn
+    that QKRope takes: an int64 host tensor."""
+    import torch
+    freq = torch.as_tensor(freq, dtype=torch.float64, device="cpu").contiguous()
+    turns = torch.empty(freq.shape, dtype=torch.int64)
+    _check(lib().lrqat_rope_turns(freq.data_ptr(), freq.numel(), turns.data_ptr()))
+    return turns
+
+
+def _vector(t, n: int, dtype, device, name: str) -> Optional[int]:
+    """Address of a dense vector of at least n elements on the call's device (None: none)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise LrqatError(-1, f"{name} must be dense, {dtype}, of at least {n} elements")
+    if t.get_device() != device or not t.is_cuda:
+        raise LrqatError(-1, f"{name} must lie on the device of the call's other arrays")
+    return t.data_ptr()
+
+
+def _rope_rows(rope: QKRope, q, k, name: str):
+    """(addresses and row distances of a pair of row arrays, rows, device)."""
+    d, out, rows, device = rope.head_dim, [], None, None
+    for t, heads, what in ((q, rope.n_heads, "queries"), (k, rope.n_kv_heads, "keys")):
+        if heads == 0:
+            out += [None, 0]
+            continue
+        if t is None or not t.is_cuda or (device is not None and t.get_device() != device):
+            raise LrqatError(-1, f"{name} of {what} must lie on the device of the other ones")
+        device = t.get_device()
+        ld = _row_array(t, heads, d, 0, device)
+        if rows is not None and t.shape[0] != rows:
+            raise LrqatError(-1, f"{name} of queries and keys must have one number of rows")
+        rows = t.shape[0]
+        out += [_ptr(t), ld]
+    if device is None:
+        raise LrqatError(-1, "n_heads and n_kv_heads are both 0")
+    _on_current(device)
+    return out, rows, device
+
+
+def _gamma(t, d: int, device) -> Optional[int]:
+    if t is not None and t.dtype not in (_types or _dtypes())[3]:
+        raise LrqatError(-1, "gamma must be bf16 (or its bits as 16-bit whole numbers)")
+    return None if t is None else _vector(t, d, t.dtype, device, "gamma")
+
+
+def qk_rope_fwd(rope: QKRope, pos, Q, K, gamma_q, gamma_k, Q_out, K_out, stream=None) -> None:
+    """Norm of each head (where its gamma is not None) and rotation by position of Q, bf16 [T, n_heads, head_dim], and
+    K, bf16 [T, n_kv_heads, head_dim], into Q_out and K_out (which may be Q and K).  pos: int32 [T], or None for row t at
+    position t; rows at negative positions are left as they are."""
+    src, rows, device = _rope_rows(rope, Q, K, "inputs")
+    dst, rows_out, device_out = _rope_rows(rope, Q_out, K_out, "outputs")
+    if rows != rows_out or device != device_out:
+        raise LrqatError(-1, "inputs and outputs must have one number of rows and lie on one device")
+    _check(lib().lrqat_qk_rope_fwd(ctypes.byref(rope), rows, _vector(pos, rows, (_types or _dtypes())[2], device, "pos"),
+                                   *src, _gamma(gamma_q, rope.head_dim, device), _gamma(gamma_k, rope.head_dim, device),
+                                   *dst, _stream(stream)))
+
+
+def qk_rope_bwd_workspace_bytes(rope: QKRope, T: int) -> int:
+    return int(lib().lrqat_qk_rope_bwd_workspace_bytes(ctypes.byref(rope), T))
+
+
+def qk_rope_bwd(rope: QKRope, pos, dQ_out, dK_out, Q, K, gamma_q, gamma_k, dQ, dK, dgamma_q, dgamma_k, accumulate: bool,
+                workspace, stream=None) -> None:
+    """Gradient of qk_rope_fwd at its inputs Q and K (None where there is no gamma).  dgamma_q, dgamma_k: fp32 [head_dim] or
+    None (without both the workspace may be None)."""
+    d, f32 = rope.head_dim, (_types or _dtypes())[1]
+    up, rows, device = _rope_rows(rope, dQ_out, dK_out, "output gradients")
+    down, rows_in, device_in = _rope_rows(rope, dQ, dK, "input gradients")
+    if rows != rows_in or device != device_in:
+        raise LrqatError(-1, "the gradients must have one number of rows and lie on one device")
+    x = []
+    for t, heads, gamma in ((Q, rope.n_heads, gamma_q), (K, rope.n_kv_heads, gamma_k)):
+        if heads == 0 or gamma is None:
+            x += [None, 0]
+        elif t is None:
+            raise LrqatError(-1, "the gradient of a norm needs its input")
+        else:
+            x += [_ptr(t), _row_array(t, heads, d, rows, device)]
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    if workspace is not None and workspace.get_device() != device:
+        raise LrqatError(-1, "the workspace must lie on the device of the call's other arrays")
+    _check(lib().lrqat_qk_rope_bwd(ctypes.byref(rope), rows, _vector(pos, rows, (_types or _dtypes())[2], device, "pos"),
+                                   *up, *x, _gamma(gamma_q, d, device), _gamma(gamma_k, d, device), *down,
+                                   _vector(dgamma_q, d, f32, device, "dgamma_q"),
+                                   _vector(dgamma_k, d, f32, device, "dgamma_k"), 1 if accumulate else 0,
+                                   _ptr(workspace), nbytes, _stream(stream)))
+
+
+def kv_blocks_workspace_bytes(blocks: KVBlocks) -> int:
+    return int(lib().lrqat_kv_blocks_workspace_bytes(ctypes.byref(blocks)))
+
+
+def _blocks_arrays(blocks: KVBlocks, arrays):
+    """Addresses of (name, tensor, elements) int32 arrays on the blocks' device."""
+    i32 = (_types or _dtypes())[2]
+    for name, t, _ in arrays:
+        if t is None:
+            raise LrqatError(-1, f"{name} must be given")
+    device = arrays[0][1].get_device() if blocks.device is None else blocks.device
+    _on_current(device)
+    return [_vector(t, n, i32, device, name) for name, t, n in arrays], device
+
+
+def _scratch(workspace, device):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        raise LrqatError(-1, "the workspace must lie on the device of the call's other arrays")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def kv_extend(blocks: KVBlocks, lens, add, free_count, lens_out, free_out, batch_lens, row_start, pos, slot, workspace,
+              stream=None) -> None:
+    """Room for add[b] > 0 new tokens behind sequence b's lens[b], or -add[b] rows of padding: blocks from the free list into
+    the tables, and the batch's layout.  lens, add, lens_out, batch_lens: int32 [n_seqs]; free_count, free_out: int32 [1];
+    row_start: int32 [n_seqs + 1]; pos: int32 [rows]; slot: int64 [rows] or None.  lens_out may be lens, free_out
+    free_count."""
+    n, rows = blocks.n_seqs, 0 if pos is None else pos.numel()
+    p, device = _blocks_arrays(blocks, [("lens", lens, n), ("add", add, n), ("free_count", free_count, 1),
+                                        ("lens_out", lens_out, n), ("free_out", free_out, 1),
+                                        ("batch_lens", batch_lens, n), ("row_start", row_start, n + 1), ("pos", pos, rows)])
+    if slot is not None:
+        import torch
+        slot = _vector(slot, rows, torch.int64, device, "slot")
+    _check(lib().lrqat_kv_extend(ctypes.byref(blocks), *p[:3], rows, *p[3:], slot, *_scratch(workspace, device),
+                                 _stream(stream)))
+
+
+def kv_truncate(blocks: KVBlocks, lens, keep, free_count, lens_out, free_out, workspace, stream=None) -> None:
+    """Shortens sequence b to keep[b] tokens and appends the blocks it no longer needs to the free list.  lens, keep,
+    lens_out: int32 [n_seqs]; free_count, free_out: int32 [1]; lens_out may be lens, free_out free_count."""
+    n = blocks.n_seqs
+    p, device = _blocks_arrays(blocks, [("lens", lens, n), ("keep", keep, n), ("free_count", free_count, 1),
+                                        ("lens_out", lens_out, n), ("free_out", free_out, 1)])
+    _check(lib().lrqat_kv_truncate(ctypes.byref(blocks), *p, *_scratch(workspace, device), _stream(stream)))
 
 
 def kv_write(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:

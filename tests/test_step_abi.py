@@ -1,0 +1,227 @@
+"""The block table and head rotation entry points reject bad arguments on the host before any CUDA work."""
+import ctypes
+import math
+import types
+
+import pytest
+
+from paper_2406_06385_gb300 import lrqat as LQ
+from paper_2406_06385_gb300.build import build
+
+OK = 16   # a 16-byte aligned address that is never followed
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build()
+    return LQ.lib()
+
+
+def _rope(**kw):
+    return LQ.QKRope(**dict(dict(n_heads=4, n_kv_heads=2, head_dim=128, rot_dim=128, neighbours=0, eps=1e-6, turns=OK), **kw))
+
+
+def _fwd(lib, rope, T=4, pos=OK, Q=OK, ldq=512, K=OK, ldk=256, gq=OK, gk=OK, Qo=OK, ldqo=512, Ko=OK, ldko=256):
+    return lib.lrqat_qk_rope_fwd(ctypes.byref(rope), T, pos, Q, ldq, K, ldk, gq, gk, Qo, ldqo, Ko, ldko, None)
+
+
+def _bwd(lib, rope, T=4, pos=OK, dQo=OK, lddqo=512, dKo=OK, lddko=256, Q=OK, ldq=512, K=OK, ldk=256, gq=OK, gk=OK, dQ=OK,
+         lddq=512, dK=OK, lddk=256, dgq=OK, dgk=OK, ws=OK, size=1 << 30):
+    return lib.lrqat_qk_rope_bwd(ctypes.byref(rope), T, pos, dQo, lddqo, dKo, lddko, Q, ldq, K, ldk, gq, gk, dQ, lddq, dK,
+                                 lddk, dgq, dgk, 0, ws, size, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_heads=-1), -1), (dict(n_heads=0, n_kv_heads=0), -1), (dict(n_kv_heads=16385), -2), (dict(head_dim=0), -1),
+    (dict(head_dim=72, rot_dim=0), -2), (dict(head_dim=272), -2), (dict(rot_dim=136), -1), (dict(rot_dim=-16), -1),
+    (dict(rot_dim=8), -2), (dict(neighbours=2), -1), (dict(eps=-1.0), -1), (dict(eps=float("inf")), -1),
+    (dict(eps=float("nan")), -1), (dict(turns=None), -1), (dict(turns=20), -3)])
+def test_rope_settings(lib, kw, status):
+    assert _fwd(lib, _rope(**kw)) == status and LQ.last_error()
+    assert _bwd(lib, _rope(**kw)) == status
+    assert lib.lrqat_qk_rope_bwd_workspace_bytes(ctypes.byref(_rope(**kw)), 4) == 0
+
+
+def test_rope_arrays(lib):
+    r = _rope()
+    for call in (_fwd, _bwd):
+        assert call(lib, r, T=0) == -1 and call(lib, r, T=1 << 31) == -2 and call(lib, r, pos=18) == -3
+        for name in ("Q", "K"):
+            assert call(lib, r, **{name: None}) == -1 and call(lib, r, **{name: 24}) == -3
+        for name, row in (("ldq", 512), ("ldk", 256)):
+            assert call(lib, r, **{name: row - 8}) == -1 and call(lib, r, **{name: row + 4}) == -3
+        for name in ("gq", "gk"):
+            assert call(lib, r, **{name: 24}) == -3
+    for name in ("Qo", "Ko"):
+        assert _fwd(lib, r, **{name: None}) == -1 and _fwd(lib, r, **{name: 24}) == -3
+    for name in ("dQo", "dKo", "dQ", "dK"):
+        assert _bwd(lib, r, **{name: None}) == -1 and _bwd(lib, r, **{name: 24}) == -3
+    for name, row in (("lddqo", 512), ("lddko", 256), ("lddq", 512), ("lddk", 256)):
+        assert _bwd(lib, r, **{name: row - 8}) == -1 and _bwd(lib, r, **{name: row + 4}) == -3
+    need = lib.lrqat_qk_rope_bwd_workspace_bytes(ctypes.byref(r), 4)
+    assert need > 0 and _bwd(lib, r, ws=None) == -4 and _bwd(lib, r, size=need - 1) == -4 and _bwd(lib, r, ws=24) == -3
+    assert _bwd(lib, r, dgq=24) == -3 and _bwd(lib, r, gq=None) == -1           # dgamma without gamma
+    assert _bwd(lib, _rope(n_kv_heads=0), dgk=OK) == -1
+
+
+def test_turns_of_frequencies(lib):
+    """Exact to half a unit of 2^-64 turns (pi to 87 digits), wrapped around, for either sign."""
+    from fractions import Fraction
+    turn = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803")
+    freq = [1.0, 0.5, 10000.0 ** (-2 / 128), 500000.0 ** -0.9, 1e-300, 5e-324, 0.0, -0.3, 2.0 ** 20, -2.0 ** 20, 2 * math.pi, 1e-15]
+    for f, t in zip(freq, LQ.rope_turns(freq).tolist()):
+        assert abs(Fraction(t) - (x := Fraction(f) / turn * 2 ** 64) + 2 ** 64 * round((x - t) / 2 ** 64)) <= Fraction(51, 100)
+    for bad in (float("nan"), float("inf"), 2.0 ** 20 + 1, -1e9):
+        with pytest.raises(LQ.LrqatError) as e:
+            LQ.rope_turns([1.0, bad])
+        assert e.value.status == -1
+    assert lib.lrqat_rope_turns(None, 0, None) == 0 and lib.lrqat_rope_turns(None, 1, None) == -1
+    assert lib.lrqat_rope_turns(None, -1, None) == -1
+
+
+def _blocks(**kw):
+    return LQ.KVBlocks(**dict(dict(n_seqs=3, max_blocks=4, block=16, pinned=0, capacity=64, block_table=OK, free_ids=OK), **kw))
+
+
+def _extend(lib, b, n=OK, add=32, count=OK, rows=5, n_out=OK, count_out=OK, seen=48, start=64, pos=80, slot=96, ws=OK, size=1 << 20):
+    return lib.lrqat_kv_extend(ctypes.byref(b), n, add, count, rows, n_out, count_out, seen, start, pos, slot, ws, size, None)
+
+
+def _truncate(lib, b, n=OK, keep=OK, count=OK, n_out=OK, count_out=OK, ws=OK, size=1 << 20):
+    return lib.lrqat_kv_truncate(ctypes.byref(b), n, keep, count, n_out, count_out, ws, size, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_seqs=0), -1), (dict(n_seqs=65536), -2), (dict(max_blocks=0), -1), (dict(max_blocks=1 << 27), -2),
+    (dict(block=8), -2), (dict(block=24), -2), (dict(pinned=-1), -1), (dict(pinned=5), -1), (dict(capacity=0), -1),
+    (dict(capacity=1 << 31), -2), (dict(block_table=None), -1), (dict(free_ids=None), -1), (dict(free_ids=18), -3)])
+def test_block_settings(lib, kw, status):
+    assert _extend(lib, _blocks(**kw)) == status and LQ.last_error()
+    assert _truncate(lib, _blocks(**kw)) == status
+    assert lib.lrqat_kv_blocks_workspace_bytes(ctypes.byref(_blocks(**kw))) == 0
+
+
+def test_block_arrays(lib):
+    b = _blocks()
+    for call, change in ((_extend, "add"), (_truncate, "keep")):
+        for name in ("n", change, "count", "n_out", "count_out"):
+            assert call(lib, b, **{name: None}) == -1 and call(lib, b, **{name: 18}) == -3
+        need = lib.lrqat_kv_blocks_workspace_bytes(ctypes.byref(b))
+        assert need > 0 and call(lib, b, ws=None) == -4 and call(lib, b, size=need - 1) == -4 and call(lib, b, ws=24) == -3
+    for name in ("seen", "start", "pos"):
+        assert _extend(lib, b, **{name: None}) == -1 and _extend(lib, b, **{name: 18}) == -3
+    assert _extend(lib, b, slot=20) == -3 and _extend(lib, b, rows=-1) == -1 and _extend(lib, b, rows=1 << 31) == -2
+    assert _extend(lib, b, seen=OK) == -1                     # the batch's lengths over the sequences'
+
+
+def _stand_in(torch, shape, dtype, device="cuda:0"):
+    """What the binding asks of a tensor, with an address that is never followed."""
+    t = torch.zeros(shape, dtype=dtype)
+    return types.SimpleNamespace(shape=t.shape, dtype=dtype, stride=t.stride, numel=t.numel, element_size=t.element_size,
+                                 dim=t.dim, is_contiguous=t.is_contiguous, is_cuda=device != "cpu",
+                                 device=torch.device(device), data_ptr=lambda: OK,
+                                 get_device=lambda: -1 if device == "cpu" else int(device[5:]))
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    """The binding with a library that only notes its calls; device 0 is the current one."""
+    torch = pytest.importorskip("torch")
+    calls = []
+    record = lambda name: lambda *a: calls.append((name, a)) or 0  # noqa: E731
+    monkeypatch.setattr(LQ, "lib", lambda: types.SimpleNamespace(**{n: record(n) for n in (
+        "lrqat_qk_rope_fwd", "lrqat_qk_rope_bwd", "lrqat_kv_extend", "lrqat_kv_truncate")}))
+    monkeypatch.setattr(LQ, "_current_device", lambda: 0)
+    return torch, calls, lambda shape, dtype, device="cuda:0": _stand_in(torch, shape, dtype, device)
+
+
+def test_binding_checks_rope_arrays(recorded):
+    torch, calls, fake = recorded
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    turns = fake((64,), torch.int64)
+    rope = LQ.QKRope.of(4, 2, 128, turns)
+    assert rope.rot_dim == 128 and LQ.QKRope.of(4, 2, 128, None).rot_dim == 0
+    for bad in (fake((64,), torch.float64), fake((64, 2), torch.int64), fake((64,), torch.int64, "cpu")):
+        with pytest.raises(LQ.LrqatError):
+            LQ.QKRope.of(4, 2, 128, bad)
+    good = dict(pos=fake((6,), i32), Q=fake((6, 4, 128), bf), K=fake((6, 2, 128), bf), gq=fake((128,), bf),
+                gk=fake((128,), torch.int16), Qo=fake((6, 4, 128), bf), Ko=fake((6, 2, 128), torch.int16),
+                dgq=fake((128,), f32), dgk=fake((128,), f32), ws=fake((4096,), torch.uint8))
+
+    def fwd(**kw):
+        a = {**good, **kw}
+        LQ.qk_rope_fwd(rope, a["pos"], a["Q"], a["K"], a["gq"], a["gk"], a["Qo"], a["Ko"], stream=0)
+
+    def bwd(**kw):
+        a = {**good, **kw}
+        LQ.qk_rope_bwd(rope, a["pos"], a["Qo"], a["Ko"], a["Q"], a["K"], a["gq"], a["gk"], a["Qo"], a["Ko"], a["dgq"],
+                       a["dgk"], False, a["ws"], stream=0)
+
+    for call in (fwd, bwd):
+        call()
+        call(pos=None)
+        call(gq=None, dgq=None, gk=fake((200,), bf))
+        for name, shape, dtype in (("Q", (6, 4, 128), bf), ("K", (6, 2, 128), bf), ("Qo", (6, 4, 128), bf), ("Ko", (6, 2, 128), bf)):
+            for bad in (fake(shape, f32), fake(shape, dtype, "cpu"), fake(shape, dtype, "cuda:1"), fake((5,) + shape[1:], dtype),
+                        fake((6, 3, 128), dtype), None):
+                with pytest.raises(LQ.LrqatError):
+                    call(**{name: bad})
+        for bad in (fake((5,), i32), fake((6,), torch.int64), fake((6,), i32, "cpu"), fake((6,), i32, "cuda:1")):
+            with pytest.raises(LQ.LrqatError):
+                call(pos=bad)
+        for bad in (fake((127,), bf), fake((128,), f32), fake((128,), bf, "cpu")):
+            with pytest.raises(LQ.LrqatError):
+                call(gk=bad)
+        for device in ("cuda:1",):                            # all on another device than the current one
+            with pytest.raises(LQ.LrqatError):
+                call(**{n: fake(t.shape, t.dtype, device) for n, t in good.items()})
+    for kw in (dict(dgq=fake((127,), f32)), dict(dgk=fake((128,), bf)), dict(ws=fake((64,), torch.uint8, "cpu"))):
+        with pytest.raises(LQ.LrqatError):
+            bwd(**kw)
+    assert len(calls) == 6
+
+
+def test_binding_checks_block_arrays(recorded):
+    torch, calls, fake = recorded
+    i32 = torch.int32
+    table, free = fake((3, 4), i32), fake((64,), i32)
+    blocks = LQ.KVBlocks.of(table, free, 16, 1)
+    assert (blocks.n_seqs, blocks.max_blocks, blocks.capacity, blocks.pinned) == (3, 4, 64, 1)
+    for bad in ((fake((3, 4), torch.int64), free), (table, fake((64,), torch.int64)), (fake((12,), i32), free),
+                (table, fake((8, 8), i32)), (fake((3, 4), i32, "cpu"), fake((64,), i32, "cpu")), (table, fake((64,), i32, "cuda:1"))):
+        with pytest.raises(LQ.LrqatError):
+            LQ.KVBlocks.of(*bad, 16)
+    n = lambda k, dtype=i32, device="cuda:0": fake((k,), dtype, device)  # noqa: E731
+    names = ["lens", "add", "free_count", "lens_out", "free_out", "batch_lens", "row_start", "pos", "slot", "workspace"]
+    good = dict(zip(names, [n(3), n(3), n(1), n(3), n(1), n(3), n(4), n(7), n(7, torch.int64), n(64, torch.uint8)]))
+    LQ.kv_extend(blocks, **good, stream=0)
+    LQ.kv_extend(blocks, **{**good, "slot": None}, stream=0)
+    assert calls[0][1][4] == 7 and calls[1][1][10] is None
+    keep = [good[k] for k in ("lens", "add", "free_count", "lens_out", "free_out", "workspace")]
+    LQ.kv_truncate(blocks, *keep, stream=0)
+    for name, size in zip(names[:9], (3, 3, 1, 3, 1, 3, 4, 7, 7)):
+        dtype = torch.int64 if name == "slot" else i32
+        bad = [n(size, torch.int16), n(size, dtype, "cpu"), n(size, dtype, "cuda:1")] + ([n(size - 1, dtype)] if name != "pos" else [])
+        for t in bad + ([None] if name != "slot" else []):
+            with pytest.raises(LQ.LrqatError):
+                LQ.kv_extend(blocks, **{**good, name: t}, stream=0)
+            if names.index(name) < 5:
+                with pytest.raises(LQ.LrqatError):
+                    LQ.kv_truncate(blocks, *[t if i == names.index(name) else v for i, v in enumerate(keep)], stream=0)
+    with pytest.raises(LQ.LrqatError):
+        LQ.kv_extend(blocks, **{**good, "workspace": n(64, torch.uint8, "cpu")}, stream=0)
+    assert len(calls) == 3
+
+
+def test_binding_refuses_another_device_than_the_current_one(recorded, monkeypatch):
+    torch, calls, fake = recorded
+    monkeypatch.setattr(LQ, "_current_device", lambda: 1)
+    i32 = torch.int32
+    blocks = LQ.KVBlocks.of(fake((3, 4), i32), fake((64,), i32), 16)
+    n = lambda k: fake((k,), i32)  # noqa: E731
+    with pytest.raises(LQ.LrqatError):
+        LQ.kv_truncate(blocks, n(3), n(3), n(1), n(3), n(1), fake((64,), torch.uint8), stream=0)
+    q = fake((2, 1, 16), torch.bfloat16)
+    with pytest.raises(LQ.LrqatError):
+        LQ.qk_rope_fwd(LQ.QKRope.of(1, 0, 16, None), None, q, None, None, None, q, None, stream=0)
+    assert not calls
