@@ -470,6 +470,28 @@ int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int3
                   int32_t window, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo, void* workspace,
                   size_t workspace_bytes, lrqat_stream_t stream);
 
+/* lrqat_kv_attn through a window that leaves the first tokens visible: a row at position p sees the keys j <= p with
+ * j > p - window or j < sinks (window 0: all j <= p).  Blocks none of whose keys a row of the call sees are not followed:
+ * those between the sinks and the oldest window may have been given away.  sinks >= 0; the rest as for lrqat_kv_attn, of
+ * which the results are, bit for bit, those with sinks = 0. */
+size_t lrqat_kv_attn_sinks_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                                           int32_t window, int32_t sinks);
+int lrqat_kv_attn_sinks(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
+                        int32_t window, int32_t sinks, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo,
+                        void* workspace, size_t workspace_bytes, lrqat_stream_t stream);
+
+/* Causal attention of a batch whose sequences start with the same `prefix` tokens: position p < prefix of every sequence
+ * lies in cache block prefix_table[p / block] (int32 [prefix / block], on the device), p >= prefix in
+ * block_table[b, p / block]; the first prefix / block columns of block_table are not followed.  len and positions count the
+ * prefix; a row at a position inside it sees its part up to there.  Keys and values of the prefix are read once for all rows
+ * of the batch, or once for each sequence where its own rows keep the machine busy.  prefix: a multiple of block, 0 for
+ * none; the rest as for lrqat_kv_attn without a window, of which the results are, bit for bit, those with prefix = 0. */
+size_t lrqat_kv_attn_shared_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                                            int32_t prefix);
+int lrqat_kv_attn_shared(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, const int32_t* prefix_table,
+                         int32_t prefix, int32_t n_heads, float softmax_scale, const uint16_t* Q, int64_t ldq, uint16_t* O,
+                         int64_t ldo, void* workspace, size_t workspace_bytes, lrqat_stream_t stream);
+
 /* ---- Optimizer step on A, B, s (App. B, Table B1) ------------------------------
  * AdamW with decoupled weight decay, bias-corrected moments, separate learning rates
  * for the adapters and the scales, after clipping the global L2 norm of all

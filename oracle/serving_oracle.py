@@ -78,26 +78,27 @@ class Cache:
         return np.stack(out) if out else np.zeros((0,) + self.codes.shape[1::2], F64)
 
 
-def attention(q, k, v, length, softmax_scale, window=0):
-    """Rows q [n, heads, d] at positions length - n .. length - 1 over k, v [length, kv heads, d].  Returns the
-    outputs, sum_j p_j |v_j| (what rounding errors of the probabilities p_j scale with) and the number of keys
-    each row sees."""
+def attention(q, k, v, length, softmax_scale, window=0, sinks=0):
+    """Rows q [n, heads, d] at positions length - n .. length - 1 over k, v [length, kv heads, d], through a window that
+    leaves the first `sinks` keys visible.  Returns the outputs, sum_j p_j |v_j| (what rounding errors of the
+    probabilities p_j scale with) and the number of keys each row sees."""
     q = np.asarray(q, F64)
     n, heads, d = q.shape
     out, mass, seen = np.zeros((n, heads, d)), np.zeros((n, heads, d)), np.zeros(n, int)
     group = heads // max(1, k.shape[1])
     for i in range(n):
         pos = length - n + i
-        lo = max(0, pos - window + 1) if window else 0
         if pos < 0:
             continue
-        seen[i] = pos + 1 - lo
+        lo = max(0, pos - window + 1) if window else 0
+        keys = np.r_[0:min(lo, sinks), lo:pos + 1]
+        seen[i] = len(keys)
         for h in range(heads):
-            z = softmax_scale * (k[lo:pos + 1, h // group] @ q[i, h])
+            z = softmax_scale * (k[keys, h // group] @ q[i, h])
             p = np.exp(z - z.max())
             p /= p.sum()
-            out[i, h] = p @ v[lo:pos + 1, h // group]
-            mass[i, h] = p @ np.abs(v[lo:pos + 1, h // group])
+            out[i, h] = p @ v[keys, h // group]
+            mass[i, h] = p @ np.abs(v[keys, h // group])
     return out, mass, seen
 
 

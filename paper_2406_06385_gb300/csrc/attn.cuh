@@ -39,15 +39,30 @@ __device__ __forceinline__ float out_factor(float l, float up) {
 
 // The tile of `tile_rows` rows `rt` of (sequence, key/value head): row i is token
 // (tile_rows rt + i) / group of the sequence's rows and query head (tile_rows rt + i) % group of the
-// head's group.
+// head's group.  Its keys are numbered without the gap between the sinks and the window: number x is key x before
+// sink_pad and key x + gap from there on.
 struct Tile {
   SeqRows seq;
   int rows;            // rows of the sequence and head, all tiles
   int r0;              // first row of this tile
   int pos_lo, pos_hi;  // positions of the tile's first and last row
-  int lo, hi;          // keys [lo, hi) that some row may see; lo a multiple of kKeyAlign
+  int lo, hi;          // keys [lo, hi) that some row may see; lo a multiple of 16
+  int gap, seen;       // general variants only; `seen`: the first key of the first row's window
 };
+template <bool kGeneral>
 __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile& t) {
+  t.gap = t.seen = 0;
+  if (kGeneral && a.across) {
+    t.seq.row0 = 0;
+    t.seq.n = static_cast<int>(a.kv.rows);
+    t.seq.len = t.seq.first = 0;
+    t.rows = t.seq.n * a.group;
+    t.r0 = rt * a.tile_rows;
+    t.pos_lo = t.pos_hi = 0;
+    t.lo = 0;
+    t.hi = a.prefix;
+    return t.r0 < t.rows;
+  }
   if (!seq_rows(a.kv, b, t.seq)) return false;
   t.rows = t.seq.n * a.group;
   t.r0 = rt * a.tile_rows;
@@ -58,7 +73,58 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile
   t.hi = max(t.pos_hi + 1, 0);
   const int64_t seen = static_cast<int64_t>(t.pos_lo) - a.window + 1;   // pos_lo is negative for padding rows
   t.lo = a.window > 0 && seen > 0 ? static_cast<int>(seen) & ~(kKeyAlign - 1) : 0;
+  if (kGeneral) {
+    if (a.sinks > 0) {
+      t.seen = a.window > 0 && seen > 0 ? static_cast<int>(seen) : 0;
+      if (t.lo > a.sink_pad) t.gap = t.lo - a.sink_pad;
+      t.hi -= t.gap;
+      t.lo = 0;
+    }
+    if (a.first > 0) t.lo = a.first;
+  }
   return true;
+}
+// The key that number x stands for.
+template <bool kGeneral>
+__device__ __forceinline__ int key_at(const AttnArgs& a, const Tile& t, int x) {
+  return kGeneral && x >= a.sink_pad ? x + t.gap : x;
+}
+// The entry of a block table that holds `key` of the sequence whose row of the table is given.
+template <bool kGeneral>
+__device__ __forceinline__ int table_entry(const AttnArgs& a, const int32_t* table, int key) {
+  return __ldg((kGeneral && key < a.prefix ? a.prefix_table : table) + (key >> a.kv.block_log2));
+}
+// The block of the 16 keys from number x on; -2 where no row of the tile sees one of them: the blocks between the sinks
+// and the window may be anybody's.
+template <bool kGeneral>
+__device__ __forceinline__ int group_block(const AttnArgs& a, const Tile& t, const int32_t* table, int x) {
+  const int key = key_at<kGeneral>(a, t, x);
+  if (kGeneral && key + 16 <= t.seen && key >= a.sinks) return -2;
+  return table_entry<kGeneral>(a, table, key);
+}
+
+// The position of a row of the batch, -1 for padding, rows behind the last sequence and rows of sequences that contradict
+// the bounds.  Row starts are bisected; where the one found does not hold the row the arrays contradict
+// themselves, and the row may still belong to a sequence that does not.
+__device__ __forceinline__ int row_position(const KvArgs& a, int64_t row) {
+  int lo = 0, hi = a.n_seqs;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(a.row_start + mid) <= row) lo = mid;
+    else hi = mid;
+  }
+  auto holds = [&](int b) { return __ldg(a.row_start + b) <= row && row < __ldg(a.row_start + b + 1); };
+  if (!holds(lo)) {
+    const int end = __ldg(a.row_start + lo + 1);
+    if (lo == a.n_seqs - 1 && __ldg(a.row_start + lo) <= end && end <= row) return -1;
+    for (lo = 0; lo < a.n_seqs && !holds(lo); ++lo) {
+    }
+    if (lo == a.n_seqs) return -1;
+  }
+  const int64_t r0 = __ldg(a.row_start + lo), r1 = __ldg(a.row_start + lo + 1);
+  const int len = __ldg(a.len + lo);
+  if (r0 < 0 || r1 > a.rows || r1 - r0 > a.max_rows || len < 0 || len > a.max_len) return -1;
+  return max(static_cast<int>(len - (r1 - row)), -1);
 }
 
 // The end of the piece of a tile's keys that starts at k0.

@@ -81,7 +81,7 @@ struct SplitSmem {
 // through a ring in shared memory filled by the warp that reads it: warps never wait for one another.
 // Bound by the copies in flight (48 KB a block, four blocks an SM) and, close behind, by issue slots (58%
 // in use, half of them for turning codes into halves): 64 ragged sequences at 72% of the memory's rate.
-template <int D, int NT>
+template <int D, int NT, bool kGeneral>
 __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv_attn_split_kernel(AttnArgs a) {
   using Sm = SplitSmem<D, NT>;
   constexpr int kC = D / 64;         // 64-dimension pieces of a token
@@ -91,11 +91,12 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Tile t;
-  if (!attn_tile(a, b, rt, t)) return;
+  if (!attn_tile<kGeneral>(a, b, rt, t)) return;
   // Whole pieces first, every tile's shorter one (or its piece number a.splits - 1) in the end, where it fills
   // gaps: 20 ragged sequences of up to 5000 tokens with 40 heads 103 -> 97 us, 90 of up to 3000 with 8 heads
   // 65 -> 60, 64 of up to 8100 no faster (82 -> 83).
   const int ns = tile_splits(a, t);
+  if (kGeneral && a.keep_parts && ns == 0) return;
   const bool last = blockIdx.z + 1 == gridDim.z;
   const int split = last ? max(ns - 1, 0) : static_cast<int>(blockIdx.z);
   if (last ? ns > 0 && ns < a.splits && (t.hi - t.lo) % a.chunk == 0
@@ -111,7 +112,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   const int32_t* table = a.kv.table + static_cast<int64_t>(b) * a.kv.max_blocks;
   const uint32_t in_block = (1u << a.kv.block_log2) - 1;
   // 16 keys from `key` on; the second half of a step may lie past the tile's keys, and then past the table
-  auto block_of = [&](int key) { return key < k1 ? __ldg(table + (key >> a.kv.block_log2)) : -2; };
+  auto block_of = [&](int key) { return key < k1 ? group_block<kGeneral>(a, t, table, key) : -2; };
   int next_blk[2] = {block_of(first_key), block_of(first_key + 16)};
   uint32_t skipped = 0;              // bit 2 s + u: half u of the step in stage s has no valid block
   const uint32_t piece = lane % (D / 16), tok = lane / (D / 16);            // a copy instruction covers 512 / D tokens
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
         if (static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks)) {
           skipped &= ~bit;
           const int64_t at = static_cast<int64_t>(blk) * a.kv.heads + h;
-          off[u] = ((at << a.kv.block_log2) + ((key + 16 * u) & in_block)) * D + lane * 16;
+          off[u] = ((at << a.kv.block_log2) + (key_at<kGeneral>(a, t, key + 16 * u) & in_block)) * D + lane * 16;
           const int8_t* p = a.kv.codes[0] + off[u];
           const uint32_t dst = ring + stage * kStageBytes + u * Sm::kHalf;
 #pragma unroll
@@ -209,7 +210,17 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
       qs[nt][j] = __shfl_sync(0xffffffffu, __uint_as_float(e << 23), 4 * (2 * t4 + j));
       const int rr = t.r0 + 8 * nt + 2 * t4 + j;
       pos[nt][j] = rr < t.rows ? t.seq.first + rr / a.group : -1;
+      if (kGeneral && a.across && rr < t.rows) pos[nt][j] = row_position(a.kv, rr / a.group);
     }
+  }
+  if (kGeneral && a.across) {                // padding does not count: nobody reads its parts
+    int least = INT32_MAX;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (pos[nt][j] >= 0) least = min(least, pos[nt][j]);
+    t.pos_lo = __reduce_min_sync(0xffffffffu, least);
   }
 
   float acc[NT][D / 16][4];
@@ -229,7 +240,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   for (int i = 0; i < steps; ++i) {
     copy_wait<2>();                  // in flight: this step's values and the next one's keys
     __syncwarp();                    // every lane's copies of this step's keys are here
-    const int key = first_key + i * kStep * kWarps, stage = i % kStages;
+    const int key = key_at<kGeneral>(a, t, first_key + i * kStep * kWarps), stage = i % kStages;
     const uint32_t src = ring + stage * kStageBytes;
     const uint32_t skip = skipped >> (2 * stage) & 3u;   // before the stage takes another step's keys
 
@@ -254,7 +265,8 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
     const uint4 sc = lds128(scales + stage * kStageScales);
     const float coef[2] = {a.scale_log2 * __uint_as_float(sc.x), a.scale_log2 * __uint_as_float(sc.z)};
     const float lsv[2] = {lg2(__uint_as_float(sc.y)), lg2(__uint_as_float(sc.w))};
-    const bool all = skip == 0 && key + kStep - 1 <= t.pos_lo && (a.window == 0 || key > t.pos_hi - a.window);
+    const bool all = skip == 0 && key + kStep - 1 <= t.pos_lo &&
+                     (a.window == 0 || key > t.pos_hi - a.window || (kGeneral && key + kStep <= a.sinks));
     uint32_t p[2][NT][2];
     float alpha[NT][2];
     bool moved = false;
@@ -279,7 +291,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int k = key + 16 * u + 8 * e + g;
-              if (k > pos[nt][j] || (a.window > 0 && k <= pos[nt][j] - a.window) || (skip >> u & 1))
+              if (k > pos[nt][j] || (a.window > 0 && k <= pos[nt][j] - a.window && !(kGeneral && k < a.sinks)) || (skip >> u & 1))
                 z[u][e] = x[u][e] = -INFINITY;
             }
         }
@@ -401,7 +413,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
       o[e + 2] = fmaf(v.z, f, o[e + 2]), o[e + 3] = fmaf(v.w, f, o[e + 3]);
     }
   }
-  if (ns <= 1) {
+  if (ns <= 1 && !(kGeneral && a.keep_parts)) {
     const float inv = out_factor(ll, mm - nbase);
     uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D + d0;
 #pragma unroll
@@ -418,31 +430,40 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
 }
 
 // Joins the splits of one row per thread block: the warps take interleaved splits, each relative to its own
-// maxima, and are then added in order.
+// maxima, and are then added in order.  kShared: the parts of the row's own keys, then those of the prefix `p`.
 constexpr int kJoinWarps = 8;
-template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs a) {
+template <int D, bool kGeneral, bool kShared>
+__device__ __forceinline__ void join_row(const AttnArgs& a, const AttnArgs& p, int b, int h, int rt, int row) {
   constexpr int kPer = D / 32;
-  const int h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z, row = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   Tile t;
-  const bool in = attn_tile(a, b, rt, t);
+  const bool in = attn_tile<kGeneral>(a, b, rt, t);
   asm volatile("griddepcontrol.wait;" ::: "memory");         // the parts are there
-  const int ns = in ? tile_splits(a, t) : 0, r = t.r0 + row;
-  if (ns <= 1 || r >= t.rows) return;
+  const int own = in ? tile_splits(a, t) : 0, r = t.r0 + row;
+  if ((kShared ? !in : own <= 1) || r >= t.rows) return;
   const int64_t slot0 = (((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits) * a.tile_rows + row;
+  int ns = own;
+  int64_t slot1 = 0;
+  if constexpr (kShared) {
+    // rows of padding see nothing
+    if (t.seq.first + r / a.group < 0) ns = 0;
+    else ns += (p.prefix - 1) / p.chunk + 1;
+    const int64_t rr = t.seq.row0 * a.group + r, prt = rr / p.tile_rows;
+    slot1 = ((static_cast<int64_t>(h) * p.row_tiles + prt) * p.splits) * p.tile_rows + rr % p.tile_rows;
+  }
   float m = -INFINITY, n = -INFINITY, acc[kPer] = {}, l = 0.0f;
 #pragma unroll 4
   for (int s = warp; s < ns; s += warps) {
-    const int64_t slot = slot0 + static_cast<int64_t>(s) * a.tile_rows;
-    const float4 v = *reinterpret_cast<const float4*>(a.part_stat + 4 * slot);
-    const float* p = a.part + slot * D + lane * kPer;
+    const bool mine = !kShared || s < own;
+    const int64_t slot = mine ? slot0 + static_cast<int64_t>(s) * a.tile_rows : slot1 + static_cast<int64_t>(s - own) * p.tile_rows;
+    const float4 v = *reinterpret_cast<const float4*>((mine ? a.part_stat : p.part_stat) + 4 * slot);
+    const float* o = (mine ? a.part : p.part) + slot * D + lane * kPer;
     const float m1 = fmaxf(m, v.x), n1 = fmaxf(n, v.y);
     const float keep = ex2(m - finite_max(m1)), f = ex2(v.x - finite_max(m1));
     l = fmaf(l, ex2(n - finite_max(n1)), v.z * ex2(v.y - finite_max(n1)));
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) {
-      const float2 x = *reinterpret_cast<const float2*>(p + e);
+      const float2 x = *reinterpret_cast<const float2*>(o + e);
       acc[e] = fmaf(acc[e], keep, x.x * f), acc[e + 1] = fmaf(acc[e + 1], keep, x.y * f);
     }
     m = m1;
@@ -469,34 +490,64 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
   uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
   reinterpret_cast<uint32_t*>(out)[threadIdx.x] = pack_bf16(o0 * inv, o1 * inv);
 }
+template <int D, bool kGeneral>
+__global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs a) {
+  join_row<D, kGeneral, false>(a, a, blockIdx.z, blockIdx.y % a.kv.heads, blockIdx.y / a.kv.heads, blockIdx.x);
+}
+// One thread block per (row of a sequence and head, key/value head, sequence).
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_shared_kernel(AttnArgs a, AttnArgs p) {
+  join_row<D, true, true>(a, p, blockIdx.z, blockIdx.y, blockIdx.x / a.tile_rows, blockIdx.x % a.tile_rows);
+}
 
-template <int D, int NT>
+template <int D, int NT, bool kGeneral>
 cudaError_t launch_split(const AttnArgs& a, cudaStream_t stream) {
   using Sm = SplitSmem<D, NT>;
-  const dim3 grid(a.kv.heads * a.row_tiles, a.kv.n_seqs, a.splits);
+  const dim3 grid(a.kv.heads * a.row_tiles, attn_grid_seqs(a), a.splits);
   static bool smem_set[kMaxDevices];
-  const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT>), Sm::kBytes, smem_set);
+  const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT, kGeneral>), Sm::kBytes, smem_set);
   if (e != cudaSuccess) return e;
-  kv_attn_split_kernel<D, NT><<<grid, 32 * kWarps, Sm::kBytes, stream>>>(a);
+  kv_attn_split_kernel<D, NT, kGeneral><<<grid, 32 * kWarps, Sm::kBytes, stream>>>(a);
   return cudaGetLastError();
 }
 
-template <int D>
-cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
-  const cudaError_t e = a.tile_rows == kPromptRows ? launch_kv_prompt(a, stream)
-                        : a.tile_rows == 8         ? launch_split<D, 1>(a, stream)
-                                                   : launch_split<D, 2>(a, stream);
-  if (e != cudaSuccess || a.splits <= 1) return e;
+template <int D, bool kGeneral>
+cudaError_t launch_parts(const AttnArgs& a, cudaStream_t stream) {
+  return a.tile_rows == kPromptRows ? launch_kv_prompt(a, stream)
+         : a.tile_rows == 8         ? launch_split<D, 1, kGeneral>(a, stream)
+                                    : launch_split<D, 2, kGeneral>(a, stream);
+}
+
+// `kernel` behind the launch before it, whose last blocks it lines up behind.
+template <typename... Args>
+cudaError_t launch_join(void (*kernel)(Args...), dim3 grid, int parts, cudaStream_t stream, const Args&... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs);
-  cfg.blockDim = dim3(32 * (a.splits > 32 ? kJoinWarps : a.splits > 8 ? kJoinWarps / 2 : 2));   // at least D / 2 threads
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(32 * (parts > 32 ? kJoinWarps : parts > 8 ? kJoinWarps / 2 : 2));   // at least D / 2 threads
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its blocks line up behind the last splits
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kv_attn_join_kernel<D>, a);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D, bool kGeneral>
+cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
+  const cudaError_t e = launch_parts<D, kGeneral>(a, stream);
+  if (e != cudaSuccess || a.splits <= 1) return e;
+  return launch_join(kv_attn_join_kernel<D, kGeneral>, dim3(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs), a.splits,
+                     stream, a);
+}
+
+template <int D>
+cudaError_t launch_shared(const AttnArgs& p, const AttnArgs& a, cudaStream_t stream) {
+  cudaError_t e = launch_parts<D, true>(p, stream);
+  if (e == cudaSuccess) e = launch_parts<D, true>(a, stream);
+  if (e != cudaSuccess) return e;
+  const int rows = a.kv.max_rows > 0 ? a.kv.max_rows * a.group : 1;
+  return launch_join(kv_attn_join_shared_kernel<D>, dim3(rows, a.kv.heads, a.kv.n_seqs), a.splits + p.splits, stream, a, p);
 }
 
 }  // namespace
@@ -525,9 +576,12 @@ void plan_attn(AttnArgs& a, int sms) {
   const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;
-  int64_t keys = a.kv.max_len;
+  // the sinks' steps: of 32 keys, of 64 in the prompt kernel
+  const int step = prompt ? 64 : kKeyAlign;
+  a.sink_pad = static_cast<int>((static_cast<int64_t>(a.sinks) + step - 1) / step * step);
+  int64_t keys = a.kv.max_len > a.first ? a.kv.max_len - a.first : 0;
   if (a.window > 0) {
-    const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kKeyAlign;
+    const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kKeyAlign + a.sink_pad;
     keys = keys < w ? keys : w;
   }
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
@@ -550,8 +604,32 @@ void plan_attn(AttnArgs& a, int sms) {
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);
 }
 
+bool shared_together(const AttnArgs& a) {
+  return a.kv.n_seqs > 1 && static_cast<int64_t>(a.kv.max_rows) * a.group <= 128;
+}
+
+// One wave of pieces: a piece costs its start and its join whatever its length.
+void plan_prefix(AttnArgs& a, int sms) {
+  const int64_t rows = a.kv.rows * a.group;
+  a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
+  const bool prompt = a.tile_rows == kPromptRows;
+  a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
+  const int64_t tiles = static_cast<int64_t>(a.kv.heads) * a.row_tiles;
+  const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
+  const int64_t pieces = tiles < at_once ? at_once / tiles : 1, unit = 128;
+  int64_t chunk = (a.prefix + pieces - 1) / pieces;
+  chunk = (chunk + unit - 1) / unit * unit;
+  a.chunk = static_cast<int>(chunk);
+  a.splits = static_cast<int>((a.prefix + chunk - 1) / chunk);
+}
+
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream) {
-  return a.kv.d == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+  if (attn_general(a)) return a.kv.d == 128 ? launch<128, true>(a, stream) : launch<64, true>(a, stream);
+  return a.kv.d == 128 ? launch<128, false>(a, stream) : launch<64, false>(a, stream);
+}
+
+cudaError_t launch_kv_attn_shared(const AttnArgs& prefix, const AttnArgs& own, cudaStream_t stream) {
+  return own.kv.d == 128 ? launch_shared<128>(prefix, own, stream) : launch_shared<64>(prefix, own, stream);
 }
 
 }  // namespace lrqat

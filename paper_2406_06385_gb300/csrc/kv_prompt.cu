@@ -137,7 +137,7 @@ __device__ __forceinline__ void store_codes(uint32_t at0, uint32_t at1, const ui
   st_shared_v4(at1, half_codes<0x4140>(x2), half_codes<0x4342>(x2), half_codes<0x4140>(x3), half_codes<0x4342>(x3));
 }
 
-template <int D>
+template <int D, bool kGeneral>
 __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   using Sm = PromptSmem<D>;
   constexpr uint32_t kBoxes = D / 64;
@@ -152,11 +152,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   // the longest rows first: the last tile of every sequence and head, then the one before, ...
   const int split = blockIdx.x % a.splits, hb = blockIdx.x / a.splits, h = hb % a.kv.heads, b = hb / a.kv.heads;
   Tile t;
-  if (!seq_rows(a.kv, b, t.seq)) return;
-  const int rt = (t.seq.n * a.group + a.tile_rows - 1) / a.tile_rows - 1 - static_cast<int>(blockIdx.y);
-  if (rt < 0 || !attn_tile(a, b, rt, t)) return;
+  int rt = blockIdx.y;
+  if (!(kGeneral && a.across)) {
+    if (!seq_rows(a.kv, b, t.seq)) return;
+    rt = (t.seq.n * a.group + a.tile_rows - 1) / a.tile_rows - 1 - static_cast<int>(blockIdx.y);
+  }
+  if (rt < 0 || !attn_tile<kGeneral>(a, b, rt, t)) return;
   const int ns = tile_splits(a, t);
-  if (split > 0 && split >= ns) return;
+  if ((split > 0 || (kGeneral && a.keep_parts)) && split >= ns) return;
   const int k0 = t.lo + split * a.chunk, k1 = piece_end(a, t, k0);
   const int tiles = k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0;
   const int halves = t.rows - t.r0 > 128 ? 2 : 1;
@@ -192,10 +195,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
     const int half = warp >> 2;
     if (half < halves) {
       const int r_in = threadIdx.x & 127, r = t.r0 + 128 * half + r_in, tok = r / a.group;
-      const bool in = r < t.rows;
-      const int pos = in ? t.seq.first + tok : -1;
+      bool in = r < t.rows;
+      int pos = in ? t.seq.first + tok : -1;
       // rows of the two halves this one's keys are masked against
-      const int h_lo = t.seq.first + (t.r0 + 128 * half) / a.group;
+      int h_lo = t.seq.first + (t.r0 + 128 * half) / a.group;
+      if (kGeneral && a.across) {            // padding has no part
+        if (in) pos = row_position(a.kv, tok);
+        in = pos >= 0;
+        h_lo = __reduce_min_sync(0xffffffffu, in ? pos : INT32_MAX);
+      }
       const int h_hi = t.seq.first + (min(t.r0 + 128 * half + 128, t.rows) - 1) / a.group;
       float qs;
       {
@@ -262,14 +270,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       for (int i = 0; i < 2 * tiles && ok; ++i) {
         const int sub = i & 1;
         const uint32_t t_p = t_s + kStepKeys * sub;      // this step's scores and, over them, its P
-        const int key = k0 + i * kStepKeys;
-        const bool all = key + kStepKeys - 1 <= h_lo && (a.window == 0 || key > h_hi - a.window);
+        const int key = key_at<kGeneral>(a, t, k0 + i * kStepKeys);
+        const bool all = key + kStepKeys - 1 <= h_lo &&
+                         (a.window == 0 || key > h_hi - a.window || (kGeneral && key + kStepKeys <= a.sinks));
         const int c_hi = pos - key;                      // columns c_lo .. c_hi of this row are visible
         const int c_lo = a.window > 0 ? c_hi - a.window + 1 : 0;
+        const int c_sink = kGeneral ? a.sinks - key : 0;  // and those before c_sink
         if (!all) {
 #pragma unroll
           for (int c = 0; c < kStepKeys; ++c)
-            if (c > c_hi || c < c_lo) s[c / 32][c % 32] = -INFINITY;
+            if (c > c_hi || (c < c_lo && !(kGeneral && c < c_sink))) s[c / 32][c % 32] = -INFINITY;
         }
         if (fminf(fminf(weight[0], weight[1]), fminf(weight[2], weight[3])) < 0.0f || wild) {
           const uint32_t slot = smem + Sm::kScale + ((i >> 1) % kScaleSlots) * Sm::kSlot + 16 * sub;
@@ -287,7 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
               tmem_ld_wait();
 #pragma unroll
               for (int e = 0; e < 16; ++e) {             // hidden keys and groups without a block add nothing
-                const bool seen = block && (all || (16 * u + e <= c_hi && 16 * u + e >= c_lo));
+                const bool seen =
+                    block && (all || (16 * u + e <= c_hi && (16 * u + e >= c_lo || (kGeneral && 16 * u + e < c_sink))));
                 if (turn == 0) n1 = seen ? fmaxf(n1, x[e] * cu) : n1;
                 else l += seen ? ex2(fmaf(x[e], cu, -n)) : 0.0f;
               }
@@ -385,7 +396,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       if (ok) {
         const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) +
                              128 * half + r_in;
-        const float f = ns <= 1 ? out_factor(l, m - n) : 1.0f;
+        const bool whole = ns <= 1 && !(kGeneral && a.keep_parts);
+        const float f = whole ? out_factor(l, m - n) : 1.0f;
         uint16_t* out = a.O + (t.seq.row0 + tok) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
@@ -398,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
             for (int e = 0; e < 32; ++e) o[e] = 0.0f;
           }
           if (!in) continue;
-          if (ns <= 1) {
+          if (whole) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
               float v[8];
@@ -412,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
               *reinterpret_cast<float4*>(a.part + slot * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
-        if (ns > 1 && in)
+        if (!whole && in)
           *reinterpret_cast<float4*>(a.part_stat + slot * 4) = make_float4(m, l == 0.0f ? -INFINITY : n, l, 0.0f);
       }
     }
@@ -429,7 +441,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
     auto block_of = [&](int j) {
       const int key = k0 + j * kTileKeys + 32 * w + 16 * (lane & 1);
       if (j >= tiles || key >= k1) return -2;
-      const int blk = __ldg(table + (key >> a.kv.block_log2));
+      const int blk = group_block<kGeneral>(a, t, table, key);
+      if (kGeneral && blk == -2) return -2;
       return static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks) ? blk : -1;
     };
     uint4 kr[4 * kBoxes], vr[4 * kBoxes];
@@ -437,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int bu = __shfl_sync(0xffffffffu, blk, u);
-        const int key = k0 + j * kTileKeys + 32 * w + 16 * u;
+        const int key = key_at<kGeneral>(a, t, k0 + j * kTileKeys + 32 * w + 16 * u);
         const int64_t at = static_cast<int64_t>(bu) * a.kv.heads + h;
         const int8_t* p = codes + ((at << a.kv.block_log2) + (key & in_block) + row) * D + 16 * piece;
 #pragma unroll
@@ -468,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
     // log2 of the value scale of the first key's block, 0 where that has none
     float ref = 0.0f;
     if (tiles > 0) {
-      const int first = __ldg(table + (k0 >> a.kv.block_log2));
+      const int first = table_entry<kGeneral>(a, table, key_at<kGeneral>(a, t, k0));
       const float v = scale_of(a.kv.scale[1], static_cast<uint32_t>(first) < static_cast<uint64_t>(a.kv.n_blocks) ? first : -1);
       ref = v > 0.0f && v < INFINITY ? lg2(v) : 0.0f;
     }
@@ -570,21 +583,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   }
 }
 
-template <int D>
+template <int D, bool kGeneral>
 cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
   static bool smem_set[kMaxDevices];
   constexpr int bytes = PromptSmem<D>::kBytes + 1024;
-  const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_prompt_kernel<D>), bytes, smem_set);
+  const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_prompt_kernel<D, kGeneral>), bytes, smem_set);
   if (e != cudaSuccess) return e;
-  const dim3 grid(static_cast<unsigned>(a.splits) * a.kv.heads * a.kv.n_seqs, a.row_tiles);
-  kv_prompt_kernel<D><<<grid, kThreads, bytes, stream>>>(a);
+  const dim3 grid(static_cast<unsigned>(a.splits) * a.kv.heads * attn_grid_seqs(a), a.row_tiles);
+  kv_prompt_kernel<D, kGeneral><<<grid, kThreads, bytes, stream>>>(a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_kv_prompt(const AttnArgs& a, cudaStream_t stream) {
-  return a.kv.d == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+  if (attn_general(a)) return a.kv.d == 128 ? launch<128, true>(a, stream) : launch<64, true>(a, stream);
+  return a.kv.d == 128 ? launch<128, false>(a, stream) : launch<64, false>(a, stream);
 }
 
 }  // namespace lrqat

@@ -670,20 +670,66 @@ int check_rows(const void* p, int64_t ld, int64_t width, const char* name) {
   return LRQAT_OK;
 }
 
-int attn_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, int32_t window, AttnArgs* a) {
+// Limits of a planned call's grids.
+int attn_fits(const AttnArgs& a) {
+  if (static_cast<int64_t>(a.kv.max_rows) * a.group > (1 << 24) ||
+      static_cast<int64_t>(a.kv.heads) * a.row_tiles > 65535 ||
+      static_cast<int64_t>(a.splits) * a.kv.heads * attn_grid_seqs(a) > INT32_MAX)
+    return fail(LRQAT_ERR_UNSUPPORTED, "too many (token, head) rows in one sequence");
+  return LRQAT_OK;
+}
+
+int attn_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, int32_t window, int32_t sinks,
+              AttnArgs* a) {
   *a = AttnArgs{};
   LRQAT_TRY(kv_args(cache, batch, &a->kv));
   if (n_heads < 1 || n_heads % cache->n_kv_heads)
     return fail(LRQAT_ERR_INVALID_ARG, "n_heads %d is not a positive multiple of n_kv_heads %d", n_heads,
                 cache->n_kv_heads);
   if (window < 0) return fail(LRQAT_ERR_INVALID_ARG, "window must be >= 0");
+  if (sinks < 0) return fail(LRQAT_ERR_INVALID_ARG, "sinks must be >= 0");
   a->group = n_heads / cache->n_kv_heads;
-  a->window = window < a->kv.max_len ? window : 0;   // a window as long as the sequences hides nothing
+  // a window that reaches from the newest token to the sinks hides nothing
+  a->window = static_cast<int64_t>(window) + sinks < a->kv.max_len ? window : 0;
+  a->sinks = a->window ? sinks : 0;
   plan_attn(*a, sm_count());
-  if (static_cast<int64_t>(a->kv.max_rows) * a->group > (1 << 24) ||
-      static_cast<int64_t>(a->kv.heads) * a->row_tiles > 65535 ||
-      static_cast<int64_t>(a->splits) * a->kv.heads * a->kv.n_seqs > INT32_MAX)
-    return fail(LRQAT_ERR_UNSUPPORTED, "too many (token, head) rows in one sequence");
+  return attn_fits(*a);
+}
+
+// A call whose sequences start with the same `prefix` tokens.  together: the batch's rows go over the prefix as one
+// sequence's (`p`), and each sequence's over its own keys (`a`); otherwise each goes over both (`a` alone).
+struct SharedArgs {
+  AttnArgs a, p;
+  bool together;
+  size_t bytes() const {
+    const int64_t rows = attn_part_rows(a) + (together ? attn_part_rows(p) : 0);
+    return static_cast<size_t>(rows) * (a.kv.d + 4) * sizeof(float);
+  }
+};
+int shared_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, int32_t prefix, SharedArgs* s) {
+  LRQAT_TRY(attn_args(cache, batch, n_heads, 0, 0, &s->a));
+  AttnArgs& a = s->a;
+  s->together = false;
+  if (prefix < 0 || prefix % cache->block)
+    return fail(LRQAT_ERR_INVALID_ARG, "prefix must be a multiple of block, >= 0 (got %d)", prefix);
+  if (prefix > static_cast<int64_t>(a.kv.max_blocks) << a.kv.block_log2)
+    return fail(LRQAT_ERR_INVALID_ARG, "prefix %d exceeds max_blocks * block", prefix);
+  a.prefix = prefix;
+  if (prefix == 0 || !shared_together(a)) return LRQAT_OK;
+  AttnArgs p = a;
+  p.across = p.keep_parts = 1;
+  plan_prefix(p, sm_count());
+  if (a.kv.rows * a.group > (1 << 24) || static_cast<int64_t>(p.kv.heads) * p.row_tiles > 65535 ||
+      static_cast<int64_t>(p.splits) * p.kv.heads > INT32_MAX)
+    return LRQAT_OK;
+  AttnArgs own = a;
+  own.first = prefix;
+  own.keep_parts = 1;
+  plan_attn(own, sm_count());
+  if (attn_fits(own) != LRQAT_OK) return LRQAT_OK;
+  s->a = own;
+  s->p = p;
+  s->together = true;
   return LRQAT_OK;
 }
 
@@ -1637,22 +1683,22 @@ int lrqat_kv_read(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, uint
 
 size_t lrqat_kv_attn_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
                                      int32_t window) {
+  return lrqat_kv_attn_sinks_workspace_bytes(cache, batch, n_heads, window, 0);
+}
+
+size_t lrqat_kv_attn_sinks_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                                           int32_t window, int32_t sinks) {
   AttnArgs a;
-  if (attn_args(cache, batch, n_heads, window, &a) != LRQAT_OK) return 0;
+  if (attn_args(cache, batch, n_heads, window, sinks, &a) != LRQAT_OK) return 0;
   return static_cast<size_t>(attn_part_rows(a)) * (a.kv.d + 4) * sizeof(float);
 }
 
-int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
-                  int32_t window, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo, void* workspace,
-                  size_t workspace_bytes, lrqat_stream_t stream) {
-  AttnArgs a;
-  LRQAT_TRY(attn_args(cache, batch, n_heads, window, &a));
-  if (!std::isfinite(softmax_scale)) return fail(LRQAT_ERR_INVALID_ARG, "softmax_scale must be finite");
-  if (a.kv.rows == 0) return LRQAT_OK;
-  LRQAT_TRY(check_rows(Q, ldq, static_cast<int64_t>(n_heads) * a.kv.d, "Q"));
-  LRQAT_TRY(check_rows(O, ldo, static_cast<int64_t>(n_heads) * a.kv.d, "O"));
-  const int64_t part_rows = attn_part_rows(a);
-  const size_t need = static_cast<size_t>(part_rows) * (a.kv.d + 4) * sizeof(float);
+// What the attention calls have in common behind their plans.
+static int attn_arrays(AttnArgs* a, float softmax_scale, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo,
+                       void* workspace, size_t workspace_bytes, size_t need) {
+  const int64_t width = static_cast<int64_t>(a->kv.heads) * a->group * a->kv.d;
+  LRQAT_TRY(check_rows(Q, ldq, width, "Q"));
+  LRQAT_TRY(check_rows(O, ldo, width, "O"));
   if (need > 0) {
     if (!workspace || workspace_bytes < need)
       return fail(LRQAT_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
@@ -1660,16 +1706,70 @@ int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int3
   }
   DeviceInfo* dev = nullptr;
   LRQAT_TRY(device_info(&dev));
-  a.kv.status = dev->status;
-  a.timeout_ns = kWaitTimeoutNs;
-  a.Q = Q;
-  a.ldq = ldq;
-  a.O = O;
-  a.ldo = ldo;
-  a.scale_log2 = softmax_scale * 1.4426950408889634f;
-  a.part = static_cast<float*>(workspace);
-  a.part_stat = a.part + part_rows * a.kv.d;
-  LRQAT_LAUNCH("kv_attn", a.splits > 1 ? 2 : 1, stream, launch_kv_attn(a, stream), "cache attention launch");
+  a->kv.status = dev->status;
+  a->timeout_ns = kWaitTimeoutNs;
+  a->Q = Q;
+  a->ldq = ldq;
+  a->O = O;
+  a->ldo = ldo;
+  a->scale_log2 = softmax_scale * 1.4426950408889634f;
+  a->part = static_cast<float*>(workspace);
+  a->part_stat = a->part + attn_part_rows(*a) * a->kv.d;
+  return LRQAT_OK;
+}
+
+static int attn_call(const char* name, const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                     float softmax_scale, int32_t window, int32_t sinks, const uint16_t* Q, int64_t ldq, uint16_t* O,
+                     int64_t ldo, void* workspace, size_t workspace_bytes, lrqat_stream_t stream) {
+  AttnArgs a;
+  LRQAT_TRY(attn_args(cache, batch, n_heads, window, sinks, &a));
+  if (!std::isfinite(softmax_scale)) return fail(LRQAT_ERR_INVALID_ARG, "softmax_scale must be finite");
+  if (a.kv.rows == 0) return LRQAT_OK;
+  const size_t need = static_cast<size_t>(attn_part_rows(a)) * (a.kv.d + 4) * sizeof(float);
+  LRQAT_TRY(attn_arrays(&a, softmax_scale, Q, ldq, O, ldo, workspace, workspace_bytes, need));
+  LRQAT_LAUNCH(name, a.splits > 1 ? 2 : 1, stream, launch_kv_attn(a, stream), "cache attention launch");
+  return LRQAT_OK;
+}
+
+int lrqat_kv_attn(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
+                  int32_t window, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo, void* workspace,
+                  size_t workspace_bytes, lrqat_stream_t stream) {
+  return attn_call("kv_attn", cache, batch, n_heads, softmax_scale, window, 0, Q, ldq, O, ldo, workspace, workspace_bytes,
+                   stream);
+}
+
+int lrqat_kv_attn_sinks(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads, float softmax_scale,
+                        int32_t window, int32_t sinks, const uint16_t* Q, int64_t ldq, uint16_t* O, int64_t ldo,
+                        void* workspace, size_t workspace_bytes, lrqat_stream_t stream) {
+  return attn_call("kv_attn_sinks", cache, batch, n_heads, softmax_scale, window, sinks, Q, ldq, O, ldo, workspace,
+                   workspace_bytes, stream);
+}
+
+size_t lrqat_kv_attn_shared_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
+                                            int32_t prefix) {
+  SharedArgs s;
+  return shared_args(cache, batch, n_heads, prefix, &s) == LRQAT_OK ? s.bytes() : 0;
+}
+
+int lrqat_kv_attn_shared(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, const int32_t* prefix_table,
+                         int32_t prefix, int32_t n_heads, float softmax_scale, const uint16_t* Q, int64_t ldq, uint16_t* O,
+                         int64_t ldo, void* workspace, size_t workspace_bytes, lrqat_stream_t stream) {
+  SharedArgs s;
+  LRQAT_TRY(shared_args(cache, batch, n_heads, prefix, &s));
+  if (!std::isfinite(softmax_scale)) return fail(LRQAT_ERR_INVALID_ARG, "softmax_scale must be finite");
+  if (prefix > 0 && !prefix_table) return fail(LRQAT_ERR_INVALID_ARG, "prefix_table must be non-NULL");
+  if (reinterpret_cast<uintptr_t>(prefix_table) & 3u) return fail(LRQAT_ERR_ALIGNMENT, "prefix_table must be 4-byte aligned");
+  if (s.a.kv.rows == 0) return LRQAT_OK;
+  s.a.prefix_table = prefix_table;
+  LRQAT_TRY(attn_arrays(&s.a, softmax_scale, Q, ldq, O, ldo, workspace, workspace_bytes, s.bytes()));
+  if (!s.together) {
+    LRQAT_LAUNCH("kv_attn_shared", s.a.splits > 1 ? 2 : 1, stream, launch_kv_attn(s.a, stream), "cache attention launch");
+    return LRQAT_OK;
+  }
+  s.p.prefix_table = prefix_table;
+  float* rest = s.a.part_stat + attn_part_rows(s.a) * 4;
+  LRQAT_TRY(attn_arrays(&s.p, softmax_scale, Q, ldq, O, ldo, rest, 0, 0));
+  LRQAT_LAUNCH("kv_attn_shared", 3, stream, launch_kv_attn_shared(s.p, s.a, stream), "cache attention launch");
   return LRQAT_OK;
 }
 

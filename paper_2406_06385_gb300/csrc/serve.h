@@ -149,15 +149,32 @@ struct AttnArgs {
   float* part;              // [seq][head][tile][split][tile_rows][d] unnormalised outputs (splits > 1)
   uint64_t timeout_ns;      // limit of one wait inside a kernel
   float* part_stat;         // [seq][head][tile][split][tile_rows][4] maxima m and n, denominator
+  // What the kernels' general variants add; all 0 for kv_attn itself.
+  int sinks;                // the first keys that a window leaves visible
+  int sink_pad;             // and the steps they come in: a multiple of a step, at most a step more
+  const int32_t* prefix_table;
+  int prefix;               // keys before it lie in the prefix table's blocks, whatever the sequence
+  int first;                // the first key of every tile: 0 or prefix
+  int across;               // 1: the rows of all sequences are one sequence's, over the prefix alone
+  int keep_parts;           // 1: outputs stay parts, even of tiles that are not cut
 };
-// Sets chunk, splits, tile_rows and row_tiles for the batch's bounds.
+inline bool attn_general(const AttnArgs& a) { return a.sinks || a.prefix; }
+inline int attn_grid_seqs(const AttnArgs& a) { return a.across ? 1 : a.kv.n_seqs; }
+// Sets chunk, splits, tile_rows, row_tiles and sink_pad for the batch's bounds.
 void plan_attn(AttnArgs& a, int sms);
+// The same for the pass of all rows over the prefix.
+void plan_prefix(AttnArgs& a, int sms);
+// Whether the batch's rows go over a shared prefix together.
+bool shared_together(const AttnArgs& a);
 inline int64_t attn_part_rows(const AttnArgs& a) {
-  return a.splits > 1 ? static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles * a.splits * a.tile_rows
-                      : 0;
+  return a.splits > 1 || a.keep_parts
+             ? static_cast<int64_t>(attn_grid_seqs(a)) * a.kv.heads * a.row_tiles * a.splits * a.tile_rows
+             : 0;
 }
 constexpr int kPromptRows = 256;   // tile_rows of the prompt kernel (kv_prompt.cu)
 cudaError_t launch_kv_prompt(const AttnArgs& a, cudaStream_t stream);
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream);
+// Attention whose rows go over the prefix together (`prefix`) and over their own keys (`own`), and the join of both.
+cudaError_t launch_kv_attn_shared(const AttnArgs& prefix, const AttnArgs& own, cudaStream_t stream);
 
 }  // namespace lrqat

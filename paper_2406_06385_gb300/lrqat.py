@@ -226,6 +226,8 @@ def lib() -> ctypes.CDLL:
             "lrqat_kv_write": [cp, bp, vp, i64, vp, i64, vp],
             "lrqat_kv_read": [cp, bp, vp, i64, vp, i64, vp],
             "lrqat_kv_attn": [cp, bp, i32, f32, i32, vp, i64, vp, i64, vp, sz, vp],
+            "lrqat_kv_attn_sinks": [cp, bp, i32, f32, i32, i32, vp, i64, vp, i64, vp, sz, vp],
+            "lrqat_kv_attn_shared": [cp, bp, vp, i32, i32, f32, vp, i64, vp, i64, vp, sz, vp],
         })
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -257,6 +259,10 @@ def lib() -> ctypes.CDLL:
         L.lrqat_kv_blocks_workspace_bytes.restype = ctypes.c_size_t
         L.lrqat_kv_attn_workspace_bytes.argtypes = [cp, bp, i32, i32]
         L.lrqat_kv_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.lrqat_kv_attn_sinks_workspace_bytes.argtypes = [cp, bp, i32, i32, i32]
+        L.lrqat_kv_attn_sinks_workspace_bytes.restype = ctypes.c_size_t
+        L.lrqat_kv_attn_shared_workspace_bytes.argtypes = [cp, bp, i32, i32]
+        L.lrqat_kv_attn_shared_workspace_bytes.restype = ctypes.c_size_t
         _lib = L
     return _lib
 
@@ -616,6 +622,51 @@ def kv_attn(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int
     ldq, ldo = _row_array(Q, heads, d, rows, device), _row_array(O, heads, d, rows, device)
     _check(lib().lrqat_kv_attn(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, _ptr(Q), ldq,
                                _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
+
+
+def _attn_rows(cache: KVCache, batch: KVBatch, Q, O, workspace):
+    """(query heads, row distances of Q and O, bytes of the workspace, device) of an attention call, checked."""
+    nbytes, device = 0, _device(cache, batch)
+    if workspace is not None:
+        nbytes = workspace.numel() * workspace.element_size()
+        if not workspace.is_cuda:
+            raise LrqatError(-1, "the workspace must lie on the device")
+    if device is not None:
+        _on_current(device)
+    heads = Q.shape[1] if len(Q.shape) == 3 else 0
+    return (heads, _row_array(Q, heads, cache.head_dim, batch.rows, device),
+            _row_array(O, heads, cache.head_dim, batch.rows, device), nbytes, device)
+
+
+def kv_attn_sinks_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window: int, sinks: int) -> int:
+    return int(lib().lrqat_kv_attn_sinks_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, window, sinks))
+
+
+def kv_attn_sinks(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, sinks: int, O, workspace,
+                  stream=None) -> None:
+    """kv_attn through a window that leaves the first `sinks` tokens visible."""
+    heads, ldq, ldo, nbytes, _ = _attn_rows(cache, batch, Q, O, workspace)
+    _check(lib().lrqat_kv_attn_sinks(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, sinks, _ptr(Q),
+                                     ldq, _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
+
+
+def kv_attn_shared_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, prefix: int) -> int:
+    return int(lib().lrqat_kv_attn_shared_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, prefix))
+
+
+def kv_attn_shared(cache: KVCache, batch: KVBatch, prefix_table, prefix: int, Q, softmax_scale: float, O, workspace,
+                   stream=None) -> None:
+    """Causal attention of a batch whose sequences start with the same `prefix` tokens (a multiple of the block), which lie
+    in the cache blocks prefix_table, int32 [prefix / block]."""
+    heads, ldq, ldo, nbytes, device = _attn_rows(cache, batch, Q, O, workspace)
+    columns = -(-prefix // cache.block) if prefix > 0 and cache.block > 0 else 0
+    if columns and prefix_table is None:
+        raise LrqatError(-1, "prefix_table must be given")
+    if prefix_table is not None and device is None:
+        device = prefix_table.get_device()
+    table = _vector(prefix_table, columns, (_types or _dtypes())[2], device, "prefix_table")
+    _check(lib().lrqat_kv_attn_shared(ctypes.byref(cache), ctypes.byref(batch), table, prefix, heads, softmax_scale,
+                                      _ptr(Q), ldq, _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
 
 
 def get_device_status(stream=None) -> None:

@@ -225,3 +225,90 @@ def test_binding_refuses_another_device_than_the_current_one(recorded, monkeypat
     with pytest.raises(LQ.LrqatError):
         LQ.qk_rope_fwd(LQ.QKRope.of(1, 0, 16, None), None, q, None, None, None, q, None, stream=0)
     assert not calls
+
+
+def _cache(**kw):
+    return LQ.KVCache(**dict(dict(n_blocks=8, n_kv_heads=2, head_dim=128, block=16, k_codes=OK, v_codes=OK,
+                                  k_scale=OK, v_scale=OK), **kw))
+
+
+def _batch(**kw):
+    return LQ.KVBatch(**dict(dict(n_seqs=2, max_blocks=4, len=OK, row_start=OK, block_table=OK, rows=6, max_rows=3,
+                                  max_len=64), **kw))
+
+
+def _sinks(lib, c=None, b=None, heads=4, scale=1.0, window=8, sinks=4, x=OK, ld=512, o=OK, ldo=512, ws=OK, size=1 << 30):
+    return lib.lrqat_kv_attn_sinks(ctypes.byref(c or _cache()), ctypes.byref(b or _batch()), heads, scale, window, sinks, x, ld,
+                                   o, ldo, ws, size, None)
+
+
+def _shared(lib, c=None, b=None, table=OK, prefix=32, heads=4, scale=1.0, x=OK, ld=512, o=OK, ldo=512, ws=OK, size=1 << 30):
+    return lib.lrqat_kv_attn_shared(ctypes.byref(c or _cache()), ctypes.byref(b or _batch()), table, prefix, heads, scale, x,
+                                    ld, o, ldo, ws, size, None)
+
+
+def test_attention_calls(lib):
+    for call in (_sinks, _shared):
+        assert call(lib, heads=0) == -1 and call(lib, heads=3) == -1
+        assert call(lib, scale=float("inf")) == -1 and call(lib, scale=float("nan")) == -1
+        assert call(lib, x=None) == -1 and call(lib, x=24) == -3 and call(lib, ld=504) == -1 and call(lib, ld=513) == -3
+        assert call(lib, o=None) == -1 and call(lib, o=24) == -3 and call(lib, ldo=504) == -1 and call(lib, ldo=513) == -3
+        assert call(lib, b=_batch(rows=0)) == 0
+        for c, status in ((_cache(head_dim=96), -2), (_cache(block=8), -2), (_cache(k_codes=None), -1)):
+            assert call(lib, c=c) == status
+        for b, status in ((_batch(n_seqs=0), -1), (_batch(max_len=65), -1), (_batch(len=None), -1), (_batch(rows=1 << 31), -2)):
+            assert call(lib, b=b) == status
+    assert _sinks(lib, window=-1) == -1 and _sinks(lib, sinks=-1) == -1
+    assert _shared(lib, prefix=-16) == -1 and _shared(lib, prefix=24) == -1 and _shared(lib, prefix=80) == -1
+    assert _shared(lib, table=None) == -1 and _shared(lib, table=18) == -3
+    long = _batch(max_blocks=4096, max_len=65536)
+    c, b = ctypes.byref(_cache()), ctypes.byref(long)
+    need = lib.lrqat_kv_attn_sinks_workspace_bytes(c, b, 4, 9000, 4)
+    assert need > 0
+    assert _sinks(lib, b=long, window=9000, ws=None, size=need) == -4 and _sinks(lib, b=long, window=9000, size=need - 1) == -4
+    assert _sinks(lib, b=long, window=9000, ws=24, size=need) == -3
+    need = lib.lrqat_kv_attn_shared_workspace_bytes(c, b, 4, 16000)
+    assert need > 0
+    assert _shared(lib, b=long, prefix=16000, ws=None, size=need) == -4
+    assert _shared(lib, b=long, prefix=16000, size=need - 1) == -4 and _shared(lib, b=long, prefix=16000, ws=24, size=need) == -3
+    assert lib.lrqat_kv_attn_sinks_workspace_bytes(c, b, 4, 9000, -1) == 0
+    assert lib.lrqat_kv_attn_shared_workspace_bytes(c, b, 4, 16001) == 0
+    # without sinks, and without a prefix, the plain call's workspace
+    for window in (0, 9000):
+        plain = lib.lrqat_kv_attn_workspace_bytes(c, b, 4, window)
+        assert plain > 0 and plain == lib.lrqat_kv_attn_sinks_workspace_bytes(c, b, 4, window, 0)
+    assert lib.lrqat_kv_attn_workspace_bytes(c, b, 4, 0) == lib.lrqat_kv_attn_shared_workspace_bytes(c, b, 4, 0)
+
+
+def test_binding_checks_attention_arrays(recorded, monkeypatch):
+    torch, _, fake = recorded
+    calls = []
+    record = lambda *a: calls.append(a) or 0  # noqa: E731
+    monkeypatch.setattr(LQ, "lib", lambda: types.SimpleNamespace(lrqat_kv_attn_sinks=record, lrqat_kv_attn_shared=record))
+    i32, bf = torch.int32, torch.bfloat16
+    codes, scale = fake((8, 2, 16, 128), torch.int8), fake((8, 2), torch.float32)
+    cache = LQ.KVCache.of(codes, codes, scale, scale)
+    batch = LQ.KVBatch.of(fake((2,), i32), fake((3,), i32), fake((2, 4), i32), 6, 3, 64)
+    ws, q, table = fake((64,), torch.uint8), fake((6, 4, 128), bf), fake((2,), i32)
+    sinks = lambda q=q, o=q, ws=ws: LQ.kv_attn_sinks(cache, batch, q, 1.0, 8, 4, o, ws, stream=0)  # noqa: E731
+    shared = lambda q=q, o=q, ws=ws, table=table: LQ.kv_attn_shared(cache, batch, table, 32, q, 1.0, o, ws, stream=0)  # noqa: E731
+    for call in (sinks, shared):
+        call()
+        call(ws=None)
+        for bad in (fake((5, 4, 128), bf), fake((6, 4, 64), bf), fake((6, 4, 128), torch.float32), fake((6, 4, 128), bf, "cpu"),
+                    fake((6, 4, 128), bf, "cuda:1"), fake((6, 512), bf)):
+            for kw in (dict(q=bad), dict(o=bad)):
+                with pytest.raises(LQ.LrqatError) as e:
+                    call(**kw)
+                assert e.value.status == -1
+        with pytest.raises(LQ.LrqatError):
+            call(ws=fake((64,), torch.uint8, "cpu"))
+        monkeypatch.setattr(LQ, "_current_device", lambda: 1)
+        with pytest.raises(LQ.LrqatError):
+            call()
+        monkeypatch.setattr(LQ, "_current_device", lambda: 0)
+    for bad in (None, fake((1,), i32), fake((2,), torch.int64), fake((2,), i32, "cpu"), fake((2,), i32, "cuda:1")):
+        with pytest.raises(LQ.LrqatError):
+            shared(table=bad)
+    LQ.kv_attn_shared(cache, batch, None, 0, q, 1.0, q, ws, stream=0)
+    assert len(calls) == 5
