@@ -614,6 +614,7 @@ void plan_prefix(AttnArgs& a, int sms) {
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
   const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
+  if (a.row_tiles < 1) a.row_tiles = 1;
   const int64_t tiles = static_cast<int64_t>(a.kv.heads) * a.row_tiles;
   const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
   const int64_t pieces = tiles < at_once ? at_once / tiles : 1, unit = 128;
