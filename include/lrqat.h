@@ -401,7 +401,7 @@ typedef struct {
   int32_t max_blocks;    /* columns of block_table                       */
   int32_t block;         /* tokens of a block: 16, 32, 64 or 128         */
   int32_t pinned;        /* 0 .. max_blocks                              */
-  int64_t capacity;      /* entries of free_ids, 1 .. 2^31 - 1           */
+  int64_t capacity;      /* entries of free_ids, 1 .. 2^31 - 2           */
   int32_t* block_table;  /* [n_seqs, max_blocks]                         */
   int32_t* free_ids;     /* [capacity]                                   */
 } lrqat_kv_blocks;
@@ -420,7 +420,7 @@ size_t lrqat_kv_blocks_workspace_bytes(const lrqat_kv_blocks* blocks);
  *   *free_out: free blocks that are left.
  * A sequence that does not fit its row of the table or whose rows do not fit `rows`, and from the first one on whose blocks
  * the list cannot give all that ask for blocks, takes no tokens: its rows are padding, and lrqat_get_device_status reports
- * LRQAT_ERR_RANGE.  len_out may be len and free_out free_count; the other arrays must not overlap.  rows: at most 2^31 - 1. */
+ * LRQAT_ERR_RANGE.  len_out may be len and free_out free_count; the other arrays must not overlap.  rows: at most 2^31 - 2. */
 int lrqat_kv_extend(const lrqat_kv_blocks* blocks, const int32_t* len, const int32_t* add, const int32_t* free_count,
                     int64_t rows, int32_t* len_out, int32_t* free_out, int32_t* batch_len, int32_t* row_start,
                     int32_t* pos, int64_t* slot, void* workspace, size_t workspace_bytes, lrqat_stream_t stream);

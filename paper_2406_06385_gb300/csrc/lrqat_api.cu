@@ -775,7 +775,7 @@ int blocks_args(const lrqat_kv_blocks* b, BlocksArgs* a) {
   if (b->n_seqs < 1 || b->max_blocks < 1 || b->capacity < 1 || b->pinned < 0 || b->pinned > b->max_blocks)
     return fail(LRQAT_ERR_INVALID_ARG, "n_seqs, max_blocks and capacity must be positive, pinned within 0 .. max_blocks");
   if (b->n_seqs > 65535) return fail(LRQAT_ERR_UNSUPPORTED, "n_seqs %d > 65535", b->n_seqs);
-  if (b->capacity > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "capacity too large");
+  if (b->capacity >= INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "capacity too large");   // sums end at INT32_MAX
   if (b->block != 16 && b->block != 32 && b->block != 64 && b->block != 128)
     return fail(LRQAT_ERR_UNSUPPORTED, "block must be 16, 32, 64 or 128 (got %d)", b->block);
   if (static_cast<int64_t>(b->max_blocks) * b->block > INT32_MAX - 1024)
@@ -1622,7 +1622,7 @@ int lrqat_kv_extend(const lrqat_kv_blocks* blocks, const int32_t* len, const int
   ExtendArgs a{};
   LRQAT_TRY(blocks_args(blocks, &a.b));
   if (rows < 0) return fail(LRQAT_ERR_INVALID_ARG, "rows must be >= 0");
-  if (rows > INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "rows too large");
+  if (rows >= INT32_MAX) return fail(LRQAT_ERR_UNSUPPORTED, "rows too large");
   if (!batch_len || !row_start || (rows > 0 && !pos))
     return fail(LRQAT_ERR_INVALID_ARG, "batch_len, row_start and pos must be non-NULL");
   if (batch_len == len || batch_len == len_out || batch_len == add)
@@ -1637,7 +1637,7 @@ int lrqat_kv_extend(const lrqat_kv_blocks* blocks, const int32_t* len, const int
   a.row_start = row_start;
   a.pos = pos;
   a.slot = slot;
-  LRQAT_LAUNCH("kv_extend", kv_extend_launches(rows), stream, launch_kv_extend(a, stream), "block table launch");
+  LRQAT_LAUNCH("kv_extend", kv_extend_launches(a), stream, launch_kv_extend(a, stream), "block table launch");
   return LRQAT_OK;
 }
 
@@ -1648,7 +1648,7 @@ int lrqat_kv_truncate(const lrqat_kv_blocks* blocks, const int32_t* len, const i
   LRQAT_TRY(blocks_args(blocks, &a.b));
   LRQAT_TRY(blocks_state(&a.b, len, keep, free_count, len_out, free_out, workspace, workspace_bytes));
   a.keep = keep;
-  LRQAT_LAUNCH("kv_truncate", kv_truncate_launches(a.b.n_seqs), stream, launch_kv_truncate(a, stream),
+  LRQAT_LAUNCH("kv_truncate", kv_truncate_launches(a), stream, launch_kv_truncate(a, stream),
                "block table launch");
   return LRQAT_OK;
 }

@@ -99,8 +99,8 @@ struct TruncateArgs {
   BlocksArgs b;
   const int32_t* keep;
 };
-int kv_extend_launches(int64_t rows);
-int kv_truncate_launches(int64_t n_seqs);
+int kv_extend_launches(const ExtendArgs& a);
+int kv_truncate_launches(const TruncateArgs& a);
 cudaError_t launch_kv_extend(const ExtendArgs& a, cudaStream_t stream);
 cudaError_t launch_kv_truncate(const TruncateArgs& a, cudaStream_t stream);
 

@@ -472,44 +472,44 @@ def _vector(t, n: int, dtype, device, name: str) -> Optional[int]:
     return t.data_ptr()
 
 
-def _rope_rows(rope: QKRope, q, k, name: str):
-    """(addresses and row distances of a pair of row arrays, rows, device)."""
-    d, out, rows, device = rope.head_dim, [], None, None
-    for t, heads, what in ((q, rope.n_heads, "queries"), (k, rope.n_kv_heads, "keys")):
-        if heads == 0:
-            out += [None, 0]
-            continue
-        if t is None or not t.is_cuda or (device is not None and t.get_device() != device):
-            raise LrqatError(-1, f"{name} of {what} must lie on the device of the other ones")
-        device = t.get_device()
-        ld = _row_array(t, heads, d, 0, device)
-        if rows is not None and t.shape[0] != rows:
-            raise LrqatError(-1, f"{name} of queries and keys must have one number of rows")
-        rows = t.shape[0]
-        out += [_ptr(t), ld]
-    if device is None:
-        raise LrqatError(-1, "n_heads and n_kv_heads are both 0")
-    _on_current(device)
-    return out, rows, device
+def _head_rows(t, heads: int, d: int, rows, device, name: str):
+    """(address, row distance, rows, device) of a row array [rows, heads, head_dim] of a call whose rows and device
+    are given, or None; no heads: no array."""
+    if heads == 0:
+        return None, 0, rows, device
+    if t is None:
+        raise LrqatError(-1, f"{name} must be given")
+    at = t.get_device()
+    if t.dtype not in (_types or _dtypes())[3] or at < 0 or (device is not None and at != device):
+        raise LrqatError(-1, f"{name} must be bf16 (or its bits as 16-bit whole numbers), on the device of the other arrays")
+    n = t.shape[0]
+    if rows is not None and n != rows:
+        raise LrqatError(-1, f"{name} must have as many rows as the other arrays ({rows})")
+    return t.data_ptr(), _rows(t, heads, d), n, at
 
 
 def _gamma(t, d: int, device) -> Optional[int]:
-    if t is not None and t.dtype not in (_types or _dtypes())[3]:
+    if t is None:
+        return None
+    if t.dtype not in (_types or _dtypes())[3]:
         raise LrqatError(-1, "gamma must be bf16 (or its bits as 16-bit whole numbers)")
-    return None if t is None else _vector(t, d, t.dtype, device, "gamma")
+    return _vector(t, d, t.dtype, device, "gamma")
 
 
 def qk_rope_fwd(rope: QKRope, pos, Q, K, gamma_q, gamma_k, Q_out, K_out, stream=None) -> None:
     """Norm of each head (where its gamma is not None) and rotation by position of Q, bf16 [T, n_heads, head_dim], and
     K, bf16 [T, n_kv_heads, head_dim], into Q_out and K_out (which may be Q and K).  pos: int32 [T], or None for row t at
     position t; rows at negative positions are left as they are."""
-    src, rows, device = _rope_rows(rope, Q, K, "inputs")
-    dst, rows_out, device_out = _rope_rows(rope, Q_out, K_out, "outputs")
-    if rows != rows_out or device != device_out:
-        raise LrqatError(-1, "inputs and outputs must have one number of rows and lie on one device")
-    _check(lib().lrqat_qk_rope_fwd(ctypes.byref(rope), rows, _vector(pos, rows, (_types or _dtypes())[2], device, "pos"),
-                                   *src, _gamma(gamma_q, rope.head_dim, device), _gamma(gamma_k, rope.head_dim, device),
-                                   *dst, _stream(stream)))
+    hq, hk, d = rope.n_heads, rope.n_kv_heads, rope.head_dim
+    q, ldq, rows, device = _head_rows(Q, hq, d, None, None, "Q")
+    k, ldk, rows, device = _head_rows(K, hk, d, rows, device, "K")
+    qo, ldqo, _, _ = _head_rows(Q_out, hq, d, rows, device, "Q_out")
+    ko, ldko, _, _ = _head_rows(K_out, hk, d, rows, device, "K_out")
+    _on_current(device)
+    if pos is not None:
+        pos = _vector(pos, rows, (_types or _dtypes())[2], device, "pos")
+    _check(lib().lrqat_qk_rope_fwd(ctypes.byref(rope), rows, pos, q, ldq, k, ldk, _gamma(gamma_q, d, device),
+                                   _gamma(gamma_k, d, device), qo, ldqo, ko, ldko, _stream(stream)))
 
 
 def qk_rope_bwd_workspace_bytes(rope: QKRope, T: int) -> int:
@@ -520,42 +520,41 @@ def qk_rope_bwd(rope: QKRope, pos, dQ_out, dK_out, Q, K, gamma_q, gamma_k, dQ, d
                 workspace, stream=None) -> None:
     """Gradient of qk_rope_fwd at its inputs Q and K (None where there is no gamma).  dgamma_q, dgamma_k: fp32 [head_dim] or
     None (without both the workspace may be None)."""
-    d, f32 = rope.head_dim, (_types or _dtypes())[1]
-    up, rows, device = _rope_rows(rope, dQ_out, dK_out, "output gradients")
-    down, rows_in, device_in = _rope_rows(rope, dQ, dK, "input gradients")
-    if rows != rows_in or device != device_in:
-        raise LrqatError(-1, "the gradients must have one number of rows and lie on one device")
-    x = []
-    for t, heads, gamma in ((Q, rope.n_heads, gamma_q), (K, rope.n_kv_heads, gamma_k)):
-        if heads == 0 or gamma is None:
-            x += [None, 0]
-        elif t is None:
-            raise LrqatError(-1, "the gradient of a norm needs its input")
-        else:
-            x += [_ptr(t), _row_array(t, heads, d, rows, device)]
-    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    if workspace is not None and workspace.get_device() != device:
-        raise LrqatError(-1, "the workspace must lie on the device of the call's other arrays")
-    _check(lib().lrqat_qk_rope_bwd(ctypes.byref(rope), rows, _vector(pos, rows, (_types or _dtypes())[2], device, "pos"),
-                                   *up, *x, _gamma(gamma_q, d, device), _gamma(gamma_k, d, device), *down,
-                                   _vector(dgamma_q, d, f32, device, "dgamma_q"),
+    hq, hk, d = rope.n_heads, rope.n_kv_heads, rope.head_dim
+    _, f32, i32, _ = _types or _dtypes()
+    gq, ldgq, rows, device = _head_rows(dQ_out, hq, d, None, None, "dQ_out")
+    gk, ldgk, rows, device = _head_rows(dK_out, hk, d, rows, device, "dK_out")
+    _on_current(device)
+    # the inputs of heads without a norm are not read
+    q, ldq, _, _ = _head_rows(Q, 0 if gamma_q is None else hq, d, rows, device, "Q")
+    k, ldk, _, _ = _head_rows(K, 0 if gamma_k is None else hk, d, rows, device, "K")
+    dq, lddq, _, _ = _head_rows(dQ, hq, d, rows, device, "dQ")
+    dk, lddk, _, _ = _head_rows(dK, hk, d, rows, device, "dK")
+    _check(lib().lrqat_qk_rope_bwd(ctypes.byref(rope), rows, _vector(pos, rows, i32, device, "pos"), gq, ldgq, gk, ldgk,
+                                   q, ldq, k, ldk, _gamma(gamma_q, d, device), _gamma(gamma_k, d, device), dq, lddq, dk,
+                                   lddk, _vector(dgamma_q, d, f32, device, "dgamma_q"),
                                    _vector(dgamma_k, d, f32, device, "dgamma_k"), 1 if accumulate else 0,
-                                   _ptr(workspace), nbytes, _stream(stream)))
+                                   *_scratch(workspace, device), _stream(stream)))
 
 
 def kv_blocks_workspace_bytes(blocks: KVBlocks) -> int:
     return int(lib().lrqat_kv_blocks_workspace_bytes(ctypes.byref(blocks)))
 
 
-def _blocks_arrays(blocks: KVBlocks, arrays):
-    """Addresses of (name, tensor, elements) int32 arrays on the blocks' device."""
-    i32 = (_types or _dtypes())[2]
-    for name, t, _ in arrays:
+def _blocks_arrays(blocks: KVBlocks, names, arrays, sizes):
+    """Addresses of int32 arrays of at least `sizes` elements on the blocks' device, which has to be the current one."""
+    i32, device, out = (_types or _dtypes())[2], blocks.device, []
+    for name, t, n in zip(names, arrays, sizes):
         if t is None:
             raise LrqatError(-1, f"{name} must be given")
-    device = arrays[0][1].get_device() if blocks.device is None else blocks.device
+        at = t.get_device()
+        if device is None:
+            device = at
+        if t.dtype is not i32 or t.numel() < n or not t.is_contiguous() or at != device or at < 0:
+            raise LrqatError(-1, f"{name} must be dense, int32, of at least {n} elements, on the blocks' device")
+        out.append(t.data_ptr())
     _on_current(device)
-    return [_vector(t, n, i32, device, name) for name, t, n in arrays], device
+    return out, device
 
 
 def _scratch(workspace, device):
@@ -573,9 +572,9 @@ def kv_extend(blocks: KVBlocks, lens, add, free_count, lens_out, free_out, batch
     row_start: int32 [n_seqs + 1]; pos: int32 [rows]; slot: int64 [rows] or None.  lens_out may be lens, free_out
     free_count."""
     n, rows = blocks.n_seqs, 0 if pos is None else pos.numel()
-    p, device = _blocks_arrays(blocks, [("lens", lens, n), ("add", add, n), ("free_count", free_count, 1),
-                                        ("lens_out", lens_out, n), ("free_out", free_out, 1),
-                                        ("batch_lens", batch_lens, n), ("row_start", row_start, n + 1), ("pos", pos, rows)])
+    p, device = _blocks_arrays(
+        blocks, ("lens", "add", "free_count", "lens_out", "free_out", "batch_lens", "row_start", "pos"),
+        (lens, add, free_count, lens_out, free_out, batch_lens, row_start, pos), (n, n, 1, n, 1, n, n + 1, rows))
     if slot is not None:
         import torch
         slot = _vector(slot, rows, torch.int64, device, "slot")
@@ -587,8 +586,8 @@ def kv_truncate(blocks: KVBlocks, lens, keep, free_count, lens_out, free_out, wo
     """Shortens sequence b to keep[b] tokens and appends the blocks it no longer needs to the free list.  lens, keep,
     lens_out: int32 [n_seqs]; free_count, free_out: int32 [1]; lens_out may be lens, free_out free_count."""
     n = blocks.n_seqs
-    p, device = _blocks_arrays(blocks, [("lens", lens, n), ("keep", keep, n), ("free_count", free_count, 1),
-                                        ("lens_out", lens_out, n), ("free_out", free_out, 1)])
+    p, device = _blocks_arrays(blocks, ("lens", "keep", "free_count", "lens_out", "free_out"),
+                               (lens, keep, free_count, lens_out, free_out), (n, n, 1, n, 1))
     _check(lib().lrqat_kv_truncate(ctypes.byref(blocks), *p, *_scratch(workspace, device), _stream(stream)))
 
 

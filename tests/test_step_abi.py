@@ -94,7 +94,7 @@ def _truncate(lib, b, n=OK, keep=OK, count=OK, n_out=OK, count_out=OK, ws=OK, si
 @pytest.mark.parametrize("kw,status", [
     (dict(n_seqs=0), -1), (dict(n_seqs=65536), -2), (dict(max_blocks=0), -1), (dict(max_blocks=1 << 27), -2),
     (dict(block=8), -2), (dict(block=24), -2), (dict(pinned=-1), -1), (dict(pinned=5), -1), (dict(capacity=0), -1),
-    (dict(capacity=1 << 31), -2), (dict(block_table=None), -1), (dict(free_ids=None), -1), (dict(free_ids=18), -3)])
+    (dict(capacity=(1 << 31) - 1), -2), (dict(block_table=None), -1), (dict(free_ids=None), -1), (dict(free_ids=18), -3)])
 def test_block_settings(lib, kw, status):
     assert _extend(lib, _blocks(**kw)) == status and LQ.last_error()
     assert _truncate(lib, _blocks(**kw)) == status
@@ -110,7 +110,7 @@ def test_block_arrays(lib):
         assert need > 0 and call(lib, b, ws=None) == -4 and call(lib, b, size=need - 1) == -4 and call(lib, b, ws=24) == -3
     for name in ("seen", "start", "pos"):
         assert _extend(lib, b, **{name: None}) == -1 and _extend(lib, b, **{name: 18}) == -3
-    assert _extend(lib, b, slot=20) == -3 and _extend(lib, b, rows=-1) == -1 and _extend(lib, b, rows=1 << 31) == -2
+    assert _extend(lib, b, slot=20) == -3 and _extend(lib, b, rows=-1) == -1 and _extend(lib, b, rows=(1 << 31) - 1) == -2
     assert _extend(lib, b, seen=OK) == -1                     # the batch's lengths over the sequences'
 
 
