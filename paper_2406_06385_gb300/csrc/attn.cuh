@@ -40,7 +40,9 @@ __device__ __forceinline__ float out_factor(float l, float up) {
 // The tile of `tile_rows` rows `rt` of (sequence, key/value head): row i is token
 // (tile_rows rt + i) / group of the sequence's rows and query head (tile_rows rt + i) % group of the
 // head's group.  Its keys are numbered without the gap between the sinks and the window: number x is key x before
-// sink_pad and key x + gap from there on.
+// sink_pad and key x + gap from there on.  Where there is a gap, x + gap may stand for the key in what hides keys
+// behind a row's position or before its window, whatever x: every row lies behind the gap, and a number that is
+// not below `sinks` but below sink_pad then counts as before the window, as it has to.
 struct Tile {
   SeqRows seq;
   int rows;            // rows of the sequence and head, all tiles
@@ -76,6 +78,7 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile
   if (kGeneral) {
     if (a.sinks > 0) {
       t.seen = a.window > 0 && seen > 0 ? static_cast<int>(seen) : 0;
+      t.lo = t.seen & ~15;
       if (t.lo > a.sink_pad) t.gap = t.lo - a.sink_pad;
       t.hi -= t.gap;
       t.lo = 0;
@@ -103,28 +106,74 @@ __device__ __forceinline__ int group_block(const AttnArgs& a, const Tile& t, con
   return table_entry<kGeneral>(a, table, key);
 }
 
-// The position of a row of the batch, -1 for padding, rows behind the last sequence and rows of sequences that contradict
-// the bounds.  Row starts are bisected; where the one found does not hold the row the arrays contradict
-// themselves, and the row may still belong to a sequence that does not.
-__device__ __forceinline__ int row_position(const KvArgs& a, int64_t row) {
-  int lo = 0, hi = a.n_seqs;
+// The sequence of a row of the batch and the row's position.  seq -1: a row behind the last sequence, or of a sequence that
+// contradicts the bounds; pos below 0: padding.
+struct RowPlace {
+  int seq, pos;
+};
+__device__ __forceinline__ bool row_in(const KvArgs& a, int b, int64_t row) {
+  return __ldg(a.row_start + b) <= row && row < __ldg(a.row_start + b + 1);
+}
+// The last sequence in [lo, hi) whose first row is not behind `row`, where row starts do not fall.
+__device__ __forceinline__ int last_start(const KvArgs& a, int lo, int hi, int64_t row) {
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (__ldg(a.row_start + mid) <= row) lo = mid;
     else hi = mid;
   }
-  auto holds = [&](int b) { return __ldg(a.row_start + b) <= row && row < __ldg(a.row_start + b + 1); };
-  if (!holds(lo)) {
-    const int end = __ldg(a.row_start + lo + 1);
-    if (lo == a.n_seqs - 1 && __ldg(a.row_start + lo) <= end && end <= row) return -1;
-    for (lo = 0; lo < a.n_seqs && !holds(lo); ++lo) {
+  return lo;
+}
+// The place of a row that sequence `b` should hold.  Where it does not, the arrays contradict themselves, and the row may
+// still belong to a sequence that does not.
+__device__ __forceinline__ RowPlace row_place(const KvArgs& a, int b, int64_t row) {
+  if (!row_in(a, b, row)) {
+    const int end = __ldg(a.row_start + b + 1);
+    if (b == a.n_seqs - 1 && __ldg(a.row_start + b) <= end && end <= row) return {-1, -1};
+    for (b = 0; b < a.n_seqs && !row_in(a, b, row); ++b) {
     }
-    if (lo == a.n_seqs) return -1;
+    if (b == a.n_seqs) return {-1, -1};
   }
-  const int64_t r0 = __ldg(a.row_start + lo), r1 = __ldg(a.row_start + lo + 1);
-  const int len = __ldg(a.len + lo);
-  if (r0 < 0 || r1 > a.rows || r1 - r0 > a.max_rows || len < 0 || len > a.max_len) return -1;
-  return max(static_cast<int>(len - (r1 - row)), -1);
+  const int64_t r0 = __ldg(a.row_start + b), r1 = __ldg(a.row_start + b + 1);
+  const int len = __ldg(a.len + b);
+  if (r0 < 0 || r1 > a.rows || r1 - r0 > a.max_rows || len < 0 || len > a.max_len) return {-1, -1};
+  return {b, static_cast<int>(len - (r1 - row))};
+}
+__device__ __forceinline__ RowPlace find_row(const KvArgs& a, int64_t row) {
+  return row_place(a, last_start(a, 0, a.n_seqs, row), row);
+}
+// The same for the rows of a warp's lanes, which do not fall from lane to lane: the first lane's sequence by probing 32
+// starts at a time, the others' among the 32 starts behind it.
+__device__ __forceinline__ RowPlace find_rows(const KvArgs& a, int64_t row) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row0 = __shfl_sync(0xffffffffu, row, 0);
+  int b = 0, end = a.n_seqs;
+  while (end - b > 1) {
+    const int step = (end - b + 31) >> 5, probe = b + step * lane;
+    const uint32_t hit = __ballot_sync(0xffffffffu, probe < end && __ldg(a.row_start + probe) <= row0) | 1u;
+    b += step * (31 - __clz(hit));
+    end = min(b + step, end);
+  }
+  const int start = __ldg(a.row_start + min(b + 1 + lane, a.n_seqs));
+  int behind = 0;                            // of those, how many are not behind the row
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (__shfl_sync(0xffffffffu, start, behind + o - 1) <= row) behind += o;
+  const bool more = __shfl_sync(0xffffffffu, start, 31) <= row;
+  b = min(b + behind, a.n_seqs - 1);
+  if (more) b = last_start(a, b, a.n_seqs, row);
+  return row_place(a, b, row);
+}
+
+// At the end of a launch that runs beside the one before it: its first block, and so the launch, ends behind that one, so
+// that what comes next finds the results of both.
+__device__ __forceinline__ void finish_behind() {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// Where four dimensions (number c of them) of a row of a tile lie among the floats of one of its parts.  Tiles of the
+// prompt kernel hold a thread's row beside its neighbours', so that a warp's words are neighbours.
+__device__ __forceinline__ int part_at(int tile_rows, int d, int row, int c, bool kept) {
+  return kept && tile_rows == kPromptRows ? (c * kPromptRows + row) * 4 : row * d + 4 * c;
 }
 
 // The end of the piece of a tile's keys that starts at k0.

@@ -82,7 +82,7 @@ struct SplitSmem {
 // Bound by the copies in flight (48 KB a block, four blocks an SM) and, close behind, by issue slots (58%
 // in use, half of them for turning codes into halves): 64 ragged sequences at 72% of the memory's rate.
 template <int D, int NT, bool kGeneral>
-__global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv_attn_split_kernel(AttnArgs a) {
+__device__ __forceinline__ void split_block(const AttnArgs& a) {
   using Sm = SplitSmem<D, NT>;
   constexpr int kC = D / 64;         // 64-dimension pieces of a token
   constexpr int kRows = 8 * NT;
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
       qs[nt][j] = __shfl_sync(0xffffffffu, __uint_as_float(e << 23), 4 * (2 * t4 + j));
       const int rr = t.r0 + 8 * nt + 2 * t4 + j;
       pos[nt][j] = rr < t.rows ? t.seq.first + rr / a.group : -1;
-      if (kGeneral && a.across && rr < t.rows) pos[nt][j] = row_position(a.kv, rr / a.group);
+      if (kGeneral && a.across && rr < t.rows) pos[nt][j] = max(find_row(a.kv, rr / a.group).pos, -1);
     }
   }
   if (kGeneral && a.across) {                // padding does not count: nobody reads its parts
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   for (int i = 0; i < steps; ++i) {
     copy_wait<2>();                  // in flight: this step's values and the next one's keys
     __syncwarp();                    // every lane's copies of this step's keys are here
-    const int key = key_at<kGeneral>(a, t, first_key + i * kStep * kWarps), stage = i % kStages;
+    const int number = first_key + i * kStep * kWarps, key = kGeneral ? number + t.gap : number, stage = i % kStages;
     const uint32_t src = ring + stage * kStageBytes;
     const uint32_t skip = skipped >> (2 * stage) & 3u;   // before the stage takes another step's keys
 
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
     const float coef[2] = {a.scale_log2 * __uint_as_float(sc.x), a.scale_log2 * __uint_as_float(sc.z)};
     const float lsv[2] = {lg2(__uint_as_float(sc.y)), lg2(__uint_as_float(sc.w))};
     const bool all = skip == 0 && key + kStep - 1 <= t.pos_lo &&
-                     (a.window == 0 || key > t.pos_hi - a.window || (kGeneral && key + kStep <= a.sinks));
+                     (a.window == 0 || key > t.pos_hi - a.window || (kGeneral && number + kStep <= a.sinks));
     uint32_t p[2][NT][2];
     float alpha[NT][2];
     bool moved = false;
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int k = key + 16 * u + 8 * e + g;
-              if (k > pos[nt][j] || (a.window > 0 && k <= pos[nt][j] - a.window && !(kGeneral && k < a.sinks)) || (skip >> u & 1))
+              if (k > pos[nt][j] || (a.window > 0 && k <= pos[nt][j] - a.window && !(kGeneral && k - t.gap < a.sinks)) || (skip >> u & 1))
                 z[u][e] = x[u][e] = -INFINITY;
             }
         }
@@ -429,41 +429,38 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv
   if (d0 == 0) *reinterpret_cast<float4*>(a.part_stat + slot * 4) = make_float4(mm, nn, ll, 0.0f);
 }
 
+template <int D, int NT, bool kGeneral>
+__global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv_attn_split_kernel(AttnArgs a) {
+  split_block<D, NT, kGeneral>(a);
+  if (kGeneral && a.keep_parts) finish_behind();
+}
+
 // Joins the splits of one row per thread block: the warps take interleaved splits, each relative to its own
-// maxima, and are then added in order.  kShared: the parts of the row's own keys, then those of the prefix `p`.
+// maxima, and are then added in order.
 constexpr int kJoinWarps = 8;
-template <int D, bool kGeneral, bool kShared>
-__device__ __forceinline__ void join_row(const AttnArgs& a, const AttnArgs& p, int b, int h, int rt, int row) {
+template <int D, bool kGeneral>
+__global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs a) {
   constexpr int kPer = D / 32;
+  const int h = blockIdx.y % a.kv.heads, rt = blockIdx.y / a.kv.heads, b = blockIdx.z, row = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   Tile t;
   const bool in = attn_tile<kGeneral>(a, b, rt, t);
   asm volatile("griddepcontrol.wait;" ::: "memory");         // the parts are there
-  const int own = in ? tile_splits(a, t) : 0, r = t.r0 + row;
-  if ((kShared ? !in : own <= 1) || r >= t.rows) return;
+  const int ns = in ? tile_splits(a, t) : 0, r = t.r0 + row;
+  if (ns <= 1 || r >= t.rows) return;
   const int64_t slot0 = (((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits) * a.tile_rows + row;
-  int ns = own;
-  int64_t slot1 = 0;
-  if constexpr (kShared) {
-    // rows of padding see nothing
-    if (t.seq.first + r / a.group < 0) ns = 0;
-    else ns += (p.prefix - 1) / p.chunk + 1;
-    const int64_t rr = t.seq.row0 * a.group + r, prt = rr / p.tile_rows;
-    slot1 = ((static_cast<int64_t>(h) * p.row_tiles + prt) * p.splits) * p.tile_rows + rr % p.tile_rows;
-  }
   float m = -INFINITY, n = -INFINITY, acc[kPer] = {}, l = 0.0f;
 #pragma unroll 4
   for (int s = warp; s < ns; s += warps) {
-    const bool mine = !kShared || s < own;
-    const int64_t slot = mine ? slot0 + static_cast<int64_t>(s) * a.tile_rows : slot1 + static_cast<int64_t>(s - own) * p.tile_rows;
-    const float4 v = *reinterpret_cast<const float4*>((mine ? a.part_stat : p.part_stat) + 4 * slot);
-    const float* o = (mine ? a.part : p.part) + slot * D + lane * kPer;
+    const int64_t slot = slot0 + static_cast<int64_t>(s) * a.tile_rows;
+    const float4 v = *reinterpret_cast<const float4*>(a.part_stat + 4 * slot);
+    const float* p = a.part + slot * D + lane * kPer;
     const float m1 = fmaxf(m, v.x), n1 = fmaxf(n, v.y);
     const float keep = ex2(m - finite_max(m1)), f = ex2(v.x - finite_max(m1));
     l = fmaf(l, ex2(n - finite_max(n1)), v.z * ex2(v.y - finite_max(n1)));
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) {
-      const float2 x = *reinterpret_cast<const float2*>(o + e);
+      const float2 x = *reinterpret_cast<const float2*>(p + e);
       acc[e] = fmaf(acc[e], keep, x.x * f), acc[e + 1] = fmaf(acc[e + 1], keep, x.y * f);
     }
     m = m1;
@@ -490,14 +487,86 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const AttnArgs& p, i
   uint16_t* out = a.O + (t.seq.row0 + r / a.group) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
   reinterpret_cast<uint32_t*>(out)[threadIdx.x] = pack_bf16(o0 * inv, o1 * inv);
 }
-template <int D, bool kGeneral>
-__global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs a) {
-  join_row<D, kGeneral, false>(a, a, blockIdx.z, blockIdx.y % a.kv.heads, blockIdx.y / a.kv.heads, blockIdx.x);
-}
-// One thread block per (row of a sequence and head, key/value head, sequence).
+
+// Joins the parts of the rows' own keys (`a`) with those of the prefix (`p`), in that order.  A lane has one row of the
+// batch and head, a warp four dimensions of 32 neighbouring rows, so that the prefix's parts come in whole lines;
+// kJoinShares warps take every so manyth part, each relative to its own maxima, and are then added in order.
+constexpr int kJoinShares = 4, kJoinAhead = 4;
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_shared_kernel(AttnArgs a, AttnArgs p) {
-  join_row<D, true, true>(a, p, blockIdx.z, blockIdx.y, blockIdx.x / a.tile_rows, blockIdx.x % a.tile_rows);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = warp % kJoinShares;
+  const int h = blockIdx.y, c = blockIdx.z * (kJoinWarps / kJoinShares) + warp / kJoinShares;
+  const int64_t rr = static_cast<int64_t>(blockIdx.x) * 32 + lane, rows = a.kv.rows * a.group;
+  const int64_t token = min(rr, rows - 1) / a.group;
+  const RowPlace at = find_rows(a.kv, token);
+  // the row's own keys: its tile of the sequence's rows, and the parts that tile was cut into
+  int own = 0, tile = 0, row = 0;
+  if (at.seq >= 0 && at.pos >= 0) {
+    const int r = static_cast<int>(token - __ldg(a.kv.row_start + at.seq)) * a.group + static_cast<int>(rr % a.group);
+    tile = r / a.tile_rows, row = r - tile * a.tile_rows;
+    Tile t;
+    if (attn_tile<true>(a, at.seq, tile, t)) own = tile_splits(a, t);
+  }
+  const int all = at.pos >= 0 ? own + (p.prefix - 1) / p.chunk + 1 : 0;      // rows of padding see nothing
+  const int64_t slot0 = ((static_cast<int64_t>(max(at.seq, 0)) * a.kv.heads + h) * a.row_tiles + tile) * a.splits * a.tile_rows;
+  const int64_t slot1 = (static_cast<int64_t>(h) * p.row_tiles + rr / p.tile_rows) * p.splits * p.tile_rows;
+  const int row1 = static_cast<int>(rr % p.tile_rows);
+  const float* part0 = a.part + slot0 * D + part_at(a.tile_rows, D, row, c, true);
+  const float* part1 = p.part + slot1 * D + part_at(p.tile_rows, D, row1, c, true);
+  const float* stat0 = a.part_stat + (slot0 + row) * 4;
+  const float* stat1 = p.part_stat + (slot1 + row1) * 4;
+  asm volatile("griddepcontrol.wait;" ::: "memory");         // the parts are there
+  const bool in = at.seq >= 0 && rr < rows;
+  float m = -INFINITY, n = -INFINITY, l = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = share; in && s0 < all; s0 += kJoinAhead * kJoinShares) {
+    float4 v[kJoinAhead], x[kJoinAhead];
+#pragma unroll
+    for (int u = 0; u < kJoinAhead; ++u) {
+      const int s = s0 + kJoinShares * u;
+      const bool mine = s < own;
+      const int64_t i = mine ? static_cast<int64_t>(s) * a.tile_rows : static_cast<int64_t>(s - own) * p.tile_rows;
+      v[u] = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
+      x[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (s < all) {
+        v[u] = __ldcg(reinterpret_cast<const float4*>((mine ? stat0 : stat1) + i * 4));
+        x[u] = __ldcg(reinterpret_cast<const float4*>((mine ? part0 : part1) + i * D));
+      }
+    }
+    float m1 = m, n1 = n;
+#pragma unroll
+    for (int u = 0; u < kJoinAhead; ++u) m1 = fmaxf(m1, v[u].x), n1 = fmaxf(n1, v[u].y);
+    const float base = finite_max(m1), nbase = finite_max(n1), keep = ex2(m - base);
+    l *= ex2(n - nbase);
+    acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+#pragma unroll
+    for (int u = 0; u < kJoinAhead; ++u) {
+      const float f = ex2(v[u].x - base);
+      l = fmaf(v[u].z, ex2(v[u].y - nbase), l);
+      acc = make_float4(fmaf(x[u].x, f, acc.x), fmaf(x[u].y, f, acc.y), fmaf(x[u].z, f, acc.z), fmaf(x[u].w, f, acc.w));
+    }
+    m = m1, n = n1;
+  }
+  __shared__ float4 part[kJoinWarps][32];
+  __shared__ float stat[kJoinWarps][3][32];
+  part[warp][lane] = acc;
+  stat[warp][0][lane] = m, stat[warp][1][lane] = n, stat[warp][2][lane] = l;
+  __syncthreads();
+  if (share != 0 || !in) return;
+#pragma unroll
+  for (int w = 1; w < kJoinShares; ++w) m = fmaxf(m, stat[warp + w][0][lane]), n = fmaxf(n, stat[warp + w][1][lane]);
+  const float base = finite_max(m), nbase = finite_max(n);
+  acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f), l = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kJoinShares; ++w) {
+    const float f = ex2(stat[warp + w][0][lane] - base);
+    const float4 x = part[warp + w][lane];
+    l = fmaf(stat[warp + w][2][lane], ex2(stat[warp + w][1][lane] - nbase), l);
+    acc = make_float4(fmaf(x.x, f, acc.x), fmaf(x.y, f, acc.y), fmaf(x.z, f, acc.z), fmaf(x.w, f, acc.w));
+  }
+  const float inv = out_factor(l, m - nbase);
+  uint16_t* out = a.O + token * a.ldo + static_cast<int64_t>(h * a.group + static_cast<int>(rr % a.group)) * D + 4 * c;
+  *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
 }
 
 template <int D, int NT, bool kGeneral>
@@ -507,8 +576,7 @@ cudaError_t launch_split(const AttnArgs& a, cudaStream_t stream) {
   static bool smem_set[kMaxDevices];
   const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_attn_split_kernel<D, NT, kGeneral>), Sm::kBytes, smem_set);
   if (e != cudaSuccess) return e;
-  kv_attn_split_kernel<D, NT, kGeneral><<<grid, 32 * kWarps, Sm::kBytes, stream>>>(a);
-  return cudaGetLastError();
+  return launch_lined_up(kv_attn_split_kernel<D, NT, kGeneral>, grid, 32 * kWarps, Sm::kBytes, a.behind, stream, a);
 }
 
 template <int D, bool kGeneral>
@@ -518,27 +586,13 @@ cudaError_t launch_parts(const AttnArgs& a, cudaStream_t stream) {
                                     : launch_split<D, 2, kGeneral>(a, stream);
 }
 
-// `kernel` behind the launch before it, whose last blocks it lines up behind.
-template <typename... Args>
-cudaError_t launch_join(void (*kernel)(Args...), dim3 grid, int parts, cudaStream_t stream, const Args&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(32 * (parts > 32 ? kJoinWarps : parts > 8 ? kJoinWarps / 2 : 2));   // at least D / 2 threads
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 template <int D, bool kGeneral>
 cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
   const cudaError_t e = launch_parts<D, kGeneral>(a, stream);
   if (e != cudaSuccess || a.splits <= 1) return e;
-  return launch_join(kv_attn_join_kernel<D, kGeneral>, dim3(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs), a.splits,
-                     stream, a);
+  const int threads = 32 * (a.splits > 32 ? kJoinWarps : a.splits > 8 ? kJoinWarps / 2 : 2);   // at least D / 2
+  return launch_lined_up(kv_attn_join_kernel<D, kGeneral>, dim3(a.tile_rows, a.kv.heads * a.row_tiles, a.kv.n_seqs), threads,
+                         0, 1, stream, a);
 }
 
 template <int D>
@@ -546,8 +600,9 @@ cudaError_t launch_shared(const AttnArgs& p, const AttnArgs& a, cudaStream_t str
   cudaError_t e = launch_parts<D, true>(p, stream);
   if (e == cudaSuccess) e = launch_parts<D, true>(a, stream);
   if (e != cudaSuccess) return e;
-  const int rows = a.kv.max_rows > 0 ? a.kv.max_rows * a.group : 1;
-  return launch_join(kv_attn_join_shared_kernel<D>, dim3(rows, a.kv.heads, a.kv.n_seqs), a.splits + p.splits, stream, a, p);
+  const int64_t rows = a.kv.rows * a.group;
+  const dim3 grid(static_cast<unsigned>((rows + 31) / 32), a.kv.heads, D / 4 * kJoinShares / kJoinWarps);
+  return launch_lined_up(kv_attn_join_shared_kernel<D>, grid, 32 * kJoinWarps, 0, 1, stream, a, p);
 }
 
 }  // namespace
@@ -576,9 +631,7 @@ void plan_attn(AttnArgs& a, int sms) {
   const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;
-  // the sinks' steps: of 32 keys, of 64 in the prompt kernel
-  const int step = prompt ? 64 : kKeyAlign;
-  a.sink_pad = static_cast<int>((static_cast<int64_t>(a.sinks) + step - 1) / step * step);
+  a.sink_pad = static_cast<int>((static_cast<int64_t>(a.sinks) + 15) & ~15);
   int64_t keys = a.kv.max_len > a.first ? a.kv.max_len - a.first : 0;
   if (a.window > 0) {
     const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kKeyAlign + a.sink_pad;

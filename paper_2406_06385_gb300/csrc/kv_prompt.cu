@@ -138,7 +138,7 @@ __device__ __forceinline__ void store_codes(uint32_t at0, uint32_t at1, const ui
 }
 
 template <int D, bool kGeneral>
-__global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
+__device__ __forceinline__ void prompt_block(const AttnArgs& a) {
   using Sm = PromptSmem<D>;
   constexpr uint32_t kBoxes = D / 64;
   extern __shared__ uint8_t smem_raw[];
@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
+  if (kGeneral && a.across) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the rows' own keys run beside
   // the longest rows first: the last tile of every sequence and head, then the one before, ...
   const int split = blockIdx.x % a.splits, hb = blockIdx.x / a.splits, h = hb % a.kv.heads, b = hb / a.kv.heads;
   Tile t;
@@ -199,11 +200,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       int pos = in ? t.seq.first + tok : -1;
       // rows of the two halves this one's keys are masked against
       int h_lo = t.seq.first + (t.r0 + 128 * half) / a.group;
-      if (kGeneral && a.across) {            // padding has no part
-        if (in) pos = row_position(a.kv, tok);
-        in = pos >= 0;
-        h_lo = __reduce_min_sync(0xffffffffu, in ? pos : INT32_MAX);
-      }
       const int h_hi = t.seq.first + (min(t.r0 + 128 * half + 128, t.rows) - 1) / a.group;
       float qs;
       {
@@ -212,8 +208,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
         uint4 w[D / 8];
         float top = 0.0f;
 #pragma unroll
+        for (int i = 0; i < D / 8; ++i) w[i] = in ? __ldg(q + i) : make_uint4(0u, 0u, 0u, 0u);
+        if (kGeneral && a.across) {          // while q is on its way; padding has no part
+          pos = find_rows(a.kv, in ? tok : t.seq.n - 1).pos;
+          in = in && pos >= 0;
+          if (!in) pos = -1;
+          h_lo = __reduce_min_sync(0xffffffffu, in ? pos : INT32_MAX);
+        }
+#pragma unroll
         for (int i = 0; i < D / 8; ++i) {
-          w[i] = in ? __ldg(q + i) : make_uint4(0u, 0u, 0u, 0u);
+          if (kGeneral && !in) w[i] = make_uint4(0u, 0u, 0u, 0u);
           float x[8];
           unpack8(w[i], x);
 #pragma unroll
@@ -270,12 +274,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
       for (int i = 0; i < 2 * tiles && ok; ++i) {
         const int sub = i & 1;
         const uint32_t t_p = t_s + kStepKeys * sub;      // this step's scores and, over them, its P
-        const int key = key_at<kGeneral>(a, t, k0 + i * kStepKeys);
+        const int number = k0 + i * kStepKeys, key = kGeneral ? number + t.gap : number;
         const bool all = key + kStepKeys - 1 <= h_lo &&
-                         (a.window == 0 || key > h_hi - a.window || (kGeneral && key + kStepKeys <= a.sinks));
+                         (a.window == 0 || key > h_hi - a.window || (kGeneral && number + kStepKeys <= a.sinks));
         const int c_hi = pos - key;                      // columns c_lo .. c_hi of this row are visible
         const int c_lo = a.window > 0 ? c_hi - a.window + 1 : 0;
-        const int c_sink = kGeneral ? a.sinks - key : 0;  // and those before c_sink
+        const int c_sink = kGeneral ? a.sinks - number : 0;   // and those before c_sink
         if (!all) {
 #pragma unroll
           for (int c = 0; c < kStepKeys; ++c)
@@ -394,8 +398,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
         tc_fence_after();
       }
       if (ok) {
-        const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) +
-                             128 * half + r_in;
+        const int row = 128 * half + r_in;
+        const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) + row;
         const bool whole = ns <= 1 && !(kGeneral && a.keep_parts);
         const float f = whole ? out_factor(l, m - n) : 1.0f;
         uint16_t* out = a.O + (t.seq.row0 + tok) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
@@ -421,7 +425,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
           } else {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(a.part + slot * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              *reinterpret_cast<float4*>(a.part + (slot - row) * D + part_at(kPromptRows, D, row, (c + e) / 4, kGeneral && a.keep_parts)) =
+                  make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
         if (!whole && in)
@@ -584,14 +589,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
 }
 
 template <int D, bool kGeneral>
+__global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
+  prompt_block<D, kGeneral>(a);
+  if (kGeneral && a.keep_parts) finish_behind();
+}
+
+template <int D, bool kGeneral>
 cudaError_t launch(const AttnArgs& a, cudaStream_t stream) {
   static bool smem_set[kMaxDevices];
   constexpr int bytes = PromptSmem<D>::kBytes + 1024;
   const cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kv_prompt_kernel<D, kGeneral>), bytes, smem_set);
   if (e != cudaSuccess) return e;
   const dim3 grid(static_cast<unsigned>(a.splits) * a.kv.heads * attn_grid_seqs(a), a.row_tiles);
-  kv_prompt_kernel<D, kGeneral><<<grid, kThreads, bytes, stream>>>(a);
-  return cudaGetLastError();
+  return launch_lined_up(kv_prompt_kernel<D, kGeneral>, grid, kThreads, bytes, a.behind, stream, a);
 }
 
 }  // namespace

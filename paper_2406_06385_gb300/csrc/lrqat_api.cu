@@ -724,7 +724,7 @@ int shared_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_
     return LRQAT_OK;
   AttnArgs own = a;
   own.first = prefix;
-  own.keep_parts = 1;
+  own.keep_parts = own.behind = 1;
   plan_attn(own, sm_count());
   if (attn_fits(own) != LRQAT_OK) return LRQAT_OK;
   s->a = own;

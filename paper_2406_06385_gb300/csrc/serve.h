@@ -151,13 +151,31 @@ struct AttnArgs {
   float* part_stat;         // [seq][head][tile][split][tile_rows][4] maxima m and n, denominator
   // What the kernels' general variants add; all 0 for kv_attn itself.
   int sinks;                // the first keys that a window leaves visible
-  int sink_pad;             // and the steps they come in: a multiple of a step, at most a step more
+  int sink_pad;             // and the rest of their last 16
   const int32_t* prefix_table;
   int prefix;               // keys before it lie in the prefix table's blocks, whatever the sequence
   int first;                // the first key of every tile: 0 or prefix
   int across;               // 1: the rows of all sequences are one sequence's, over the prefix alone
   int keep_parts;           // 1: outputs stay parts, even of tiles that are not cut
+  int behind;               // 1: the launch may start beside the one before it, of which it needs nothing
 };
+// Launches `kernel`; lined_up: its blocks may start while the launch before it runs (which says when), and wait for it
+// where they need it.
+template <typename... Args>
+cudaError_t launch_lined_up(void (*kernel)(Args...), dim3 grid, int threads, int smem, int lined_up, cudaStream_t stream,
+                            const Args&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = lined_up ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 inline bool attn_general(const AttnArgs& a) { return a.sinks || a.prefix; }
 inline int attn_grid_seqs(const AttnArgs& a) { return a.across ? 1 : a.kv.n_seqs; }
 // Sets chunk, splits, tile_rows, row_tiles and sink_pad for the batch's bounds.
