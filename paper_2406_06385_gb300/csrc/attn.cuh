@@ -164,17 +164,9 @@ __device__ __forceinline__ RowPlace find_rows(const KvArgs& a, int64_t row) {
   return row_place(a, b, row);
 }
 
-// At the end of a launch that runs beside the one before it: its first block, and so the launch, ends behind that one, so
-// that what comes next finds the results of both.
-__device__ __forceinline__ void finish_behind() {
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
-}
-
-// Where four dimensions (number c of them) of a row of a tile lie among the floats of one of its parts.  Tiles of the
-// prompt kernel hold a thread's row beside its neighbours', so that a warp's words are neighbours.
-__device__ __forceinline__ int part_at(int tile_rows, int d, int row, int c, bool kept) {
-  return kept && tile_rows == kPromptRows ? (c * kPromptRows + row) * 4 : row * d + 4 * c;
-}
+// At the end of one block of a launch that runs beside the one before it: the launch ends behind that one, so that what
+// comes next finds the results of both.
+__device__ __forceinline__ void finish_behind() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // The end of the piece of a tile's keys that starts at k0.
 __device__ __forceinline__ int piece_end(const AttnArgs& a, const Tile& t, int k0) {

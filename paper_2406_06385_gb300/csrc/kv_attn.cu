@@ -15,6 +15,7 @@
 // Scores, maxima, sums and outputs are 32-bit.
 #include <cuda_runtime.h>
 #include <cstdint>
+#include <type_traits>
 
 #include "attn.cuh"
 #include "kernels.h"
@@ -432,7 +433,7 @@ __device__ __forceinline__ void split_block(const AttnArgs& a) {
 template <int D, int NT, bool kGeneral>
 __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? kPerSm : kPerSm / 2) kv_attn_split_kernel(AttnArgs a) {
   split_block<D, NT, kGeneral>(a);
-  if (kGeneral && a.keep_parts) finish_behind();
+  if (kGeneral && a.keep_parts && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) finish_behind();
 }
 
 // Joins the splits of one row per thread block: the warps take interleaved splits, each relative to its own
@@ -488,85 +489,87 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
   reinterpret_cast<uint32_t*>(out)[threadIdx.x] = pack_bf16(o0 * inv, o1 * inv);
 }
 
-// Joins the parts of the rows' own keys (`a`) with those of the prefix (`p`), in that order.  A lane has one row of the
-// batch and head, a warp four dimensions of 32 neighbouring rows, so that the prefix's parts come in whole lines;
-// kJoinShares warps take every so manyth part, each relative to its own maxima, and are then added in order.
-constexpr int kJoinShares = 4, kJoinAhead = 4;
+// Joins the parts of the rows' own keys (`a`) with those of the prefix (`p`), in that order: a warp has one row of the
+// batch and head, its lanes the statistics of 32 parts at a time and the row's dimensions.
+constexpr int kJoinAhead = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_shared_kernel(AttnArgs a, AttnArgs p) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = warp % kJoinShares;
-  const int h = blockIdx.y, c = blockIdx.z * (kJoinWarps / kJoinShares) + warp / kJoinShares;
-  const int64_t rr = static_cast<int64_t>(blockIdx.x) * 32 + lane, rows = a.kv.rows * a.group;
-  const int64_t token = min(rr, rows - 1) / a.group;
+  constexpr int kPer = D / 32;
+  const int lane = threadIdx.x & 31, h = blockIdx.y;
+  const int64_t rr = static_cast<int64_t>(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
+  if (rr >= a.kv.rows * a.group) return;
+  const int64_t token = rr / a.group;
+  const int head = static_cast<int>(rr - token * a.group);
   const RowPlace at = find_rows(a.kv, token);
   // the row's own keys: its tile of the sequence's rows, and the parts that tile was cut into
   int own = 0, tile = 0, row = 0;
   if (at.seq >= 0 && at.pos >= 0) {
-    const int r = static_cast<int>(token - __ldg(a.kv.row_start + at.seq)) * a.group + static_cast<int>(rr % a.group);
+    const int r = static_cast<int>(token - __ldg(a.kv.row_start + at.seq)) * a.group + head;
     tile = r / a.tile_rows, row = r - tile * a.tile_rows;
     Tile t;
     if (attn_tile<true>(a, at.seq, tile, t)) own = tile_splits(a, t);
   }
-  const int all = at.pos >= 0 ? own + (p.prefix - 1) / p.chunk + 1 : 0;      // rows of padding see nothing
-  const int64_t slot0 = ((static_cast<int64_t>(max(at.seq, 0)) * a.kv.heads + h) * a.row_tiles + tile) * a.splits * a.tile_rows;
-  const int64_t slot1 = (static_cast<int64_t>(h) * p.row_tiles + rr / p.tile_rows) * p.splits * p.tile_rows;
-  const int row1 = static_cast<int>(rr % p.tile_rows);
-  const float* part0 = a.part + slot0 * D + part_at(a.tile_rows, D, row, c, true);
-  const float* part1 = p.part + slot1 * D + part_at(p.tile_rows, D, row1, c, true);
-  const float* stat0 = a.part_stat + (slot0 + row) * 4;
-  const float* stat1 = p.part_stat + (slot1 + row1) * 4;
+  const int all = at.seq >= 0 && at.pos >= 0 ? own + (p.prefix - 1) / p.chunk + 1 : 0;      // rows of padding see nothing
+  const int64_t slot0 = ((static_cast<int64_t>(max(at.seq, 0)) * a.kv.heads + h) * a.row_tiles + tile) * a.splits * a.tile_rows + row;
+  const int64_t slot1 = (static_cast<int64_t>(h) * p.row_tiles + rr / p.tile_rows) * p.splits * p.tile_rows + rr % p.tile_rows;
+  auto slot_of = [&](int s) {
+    return s < own ? slot0 + static_cast<int64_t>(s) * a.tile_rows : slot1 + static_cast<int64_t>(s - own) * p.tile_rows;
+  };
+  using Vec = typename std::conditional<kPer == 4, float4, float2>::type;
+  union Dims {
+    Vec v;
+    float f[kPer];
+  };
   asm volatile("griddepcontrol.wait;" ::: "memory");         // the parts are there
-  const bool in = at.seq >= 0 && rr < rows;
-  float m = -INFINITY, n = -INFINITY, l = 0.0f;
-  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s0 = share; in && s0 < all; s0 += kJoinAhead * kJoinShares) {
-    float4 v[kJoinAhead], x[kJoinAhead];
+  if (at.seq < 0) return;
+  float m = -INFINITY, n = -INFINITY, l = 0.0f, acc[kPer] = {};
+  for (int s0 = 0; s0 < all; s0 += 32) {
+    const int count = min(all - s0, 32);
+    float4 v = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
+    if (lane < count) v = __ldcg(reinterpret_cast<const float4*>((s0 + lane < own ? a : p).part_stat + slot_of(s0 + lane) * 4));
+    float f = 0.0f;
+    for (int u0 = 0; u0 < count; u0 += kJoinAhead) {
+      Dims x[kJoinAhead];
 #pragma unroll
-    for (int u = 0; u < kJoinAhead; ++u) {
-      const int s = s0 + kJoinShares * u;
-      const bool mine = s < own;
-      const int64_t i = mine ? static_cast<int64_t>(s) * a.tile_rows : static_cast<int64_t>(s - own) * p.tile_rows;
-      v[u] = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
-      x[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (s < all) {
-        v[u] = __ldcg(reinterpret_cast<const float4*>((mine ? stat0 : stat1) + i * 4));
-        x[u] = __ldcg(reinterpret_cast<const float4*>((mine ? part0 : part1) + i * D));
+      for (int u = 0; u < kJoinAhead; ++u) {
+        const int s = s0 + min(u0 + u, count - 1);
+        x[u].v = __ldcg(reinterpret_cast<const Vec*>((s < own ? a : p).part + slot_of(s) * D) + lane);
+      }
+      if (u0 == 0) {
+        float m1 = v.x, n1 = v.y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
+          n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+        }
+        m1 = fmaxf(m, m1), n1 = fmaxf(n, n1);
+        const float base = finite_max(m1), nbase = finite_max(n1), keep = ex2(m - base);
+        f = ex2(v.x - base);
+        l *= ex2(n - nbase);
+        float sum = v.z * ex2(v.y - nbase);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        l += sum;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] *= keep;
+        m = m1, n = n1;
+      }
+#pragma unroll
+      for (int u = 0; u < kJoinAhead; ++u) {
+        const float fu = __shfl_sync(0xffffffffu, f, (u0 + u) & 31);
+        if (u0 + u < count)
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) acc[e] = fmaf(x[u].f[e], fu, acc[e]);
       }
     }
-    float m1 = m, n1 = n;
-#pragma unroll
-    for (int u = 0; u < kJoinAhead; ++u) m1 = fmaxf(m1, v[u].x), n1 = fmaxf(n1, v[u].y);
-    const float base = finite_max(m1), nbase = finite_max(n1), keep = ex2(m - base);
-    l *= ex2(n - nbase);
-    acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
-#pragma unroll
-    for (int u = 0; u < kJoinAhead; ++u) {
-      const float f = ex2(v[u].x - base);
-      l = fmaf(v[u].z, ex2(v[u].y - nbase), l);
-      acc = make_float4(fmaf(x[u].x, f, acc.x), fmaf(x[u].y, f, acc.y), fmaf(x[u].z, f, acc.z), fmaf(x[u].w, f, acc.w));
-    }
-    m = m1, n = n1;
   }
-  __shared__ float4 part[kJoinWarps][32];
-  __shared__ float stat[kJoinWarps][3][32];
-  part[warp][lane] = acc;
-  stat[warp][0][lane] = m, stat[warp][1][lane] = n, stat[warp][2][lane] = l;
-  __syncthreads();
-  if (share != 0 || !in) return;
-#pragma unroll
-  for (int w = 1; w < kJoinShares; ++w) m = fmaxf(m, stat[warp + w][0][lane]), n = fmaxf(n, stat[warp + w][1][lane]);
-  const float base = finite_max(m), nbase = finite_max(n);
-  acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f), l = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kJoinShares; ++w) {
-    const float f = ex2(stat[warp + w][0][lane] - base);
-    const float4 x = part[warp + w][lane];
-    l = fmaf(stat[warp + w][2][lane], ex2(stat[warp + w][1][lane] - nbase), l);
-    acc = make_float4(fmaf(x.x, f, acc.x), fmaf(x.y, f, acc.y), fmaf(x.z, f, acc.z), fmaf(x.w, f, acc.w));
+  const float inv = out_factor(l, m - finite_max(n));
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.O + token * a.ldo + static_cast<int64_t>(h * a.group + head) * D) + lane * (kPer / 2);
+  if constexpr (kPer == 4) {
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+  } else {
+    *out = pack_bf16(acc[0] * inv, acc[1] * inv);
   }
-  const float inv = out_factor(l, m - nbase);
-  uint16_t* out = a.O + token * a.ldo + static_cast<int64_t>(h * a.group + static_cast<int>(rr % a.group)) * D + 4 * c;
-  *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
 }
 
 template <int D, int NT, bool kGeneral>
@@ -601,7 +604,7 @@ cudaError_t launch_shared(const AttnArgs& p, const AttnArgs& a, cudaStream_t str
   if (e == cudaSuccess) e = launch_parts<D, true>(a, stream);
   if (e != cudaSuccess) return e;
   const int64_t rows = a.kv.rows * a.group;
-  const dim3 grid(static_cast<unsigned>((rows + 31) / 32), a.kv.heads, D / 4 * kJoinShares / kJoinWarps);
+  const dim3 grid(static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps), a.kv.heads);
   return launch_lined_up(kv_attn_join_shared_kernel<D>, grid, 32 * kJoinWarps, 0, 1, stream, a, p);
 }
 
@@ -661,7 +664,11 @@ bool shared_together(const AttnArgs& a) {
   return a.kv.n_seqs > 1 && static_cast<int64_t>(a.kv.max_rows) * a.group <= 128;
 }
 
-// One wave of pieces: a piece costs its start and its join whatever its length.
+// At most one wave of pieces: a piece costs its start and its join whatever its length.  Blocks of the prompt kernel have
+// an SM to themselves, and the sequences' own keys, which run beside them, what is left and then all: a piece takes 9 us
+// and 2 us a tile of 128 keys, the own keys the time of three quarters of their bound's bytes at the copy rate and 0.75 us
+// of an SM a block.  64 rows of 32 heads, 8 of them for keys, behind 16000 tokens, 500 of their own: 18 pieces 50 us, 15
+// 41, 13 42, 10 48; 16 x 5 rows of 40 heads behind 2000 tokens: three pieces 35 us, two 32, one 45.
 void plan_prefix(AttnArgs& a, int sms) {
   const int64_t rows = a.kv.rows * a.group;
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
@@ -670,9 +677,22 @@ void plan_prefix(AttnArgs& a, int sms) {
   if (a.row_tiles < 1) a.row_tiles = 1;
   const int64_t tiles = static_cast<int64_t>(a.kv.heads) * a.row_tiles;
   const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
-  const int64_t pieces = tiles < at_once ? at_once / tiles : 1, unit = 128;
-  int64_t chunk = (a.prefix + pieces - 1) / pieces;
-  chunk = (chunk + unit - 1) / unit * unit;
+  const int64_t most = tiles < at_once ? at_once / tiles : 1, unit = 128;
+  auto chunk_of = [&](int64_t pieces) { return ((a.prefix + pieces - 1) / pieces + unit - 1) / unit * unit; };
+  int64_t chunk = chunk_of(most);
+  if (prompt && most > 1) {
+    const double copy_rate = 6.8e3;          // bytes a nanosecond, the machine
+    const double blocks = static_cast<double>(a.kv.n_seqs) * a.kv.heads, own = a.kv.max_len > a.prefix ? a.kv.max_len - a.prefix : 0;
+    const double own_ns = blocks * (0.75 * own * 2 * a.kv.d / copy_rate * sms + 750.0);      // of one SM
+    double best = 0.0;
+    for (int64_t pieces = most; pieces >= 1; --pieces) {
+      const int64_t c = chunk_of(pieces), used = (a.prefix + c - 1) / c;
+      const double mine = 9000.0 + 2000.0 / unit * c, left = own_ns - mine * (sms - used * tiles);
+      const double all = mine + (left > 0.0 ? left / sms : 0.0);
+      if (pieces == most || all < best) best = all, chunk = c;
+      if (mine > best) break;
+    }
+  }
   a.chunk = static_cast<int>(chunk);
   a.splits = static_cast<int>((a.prefix + chunk - 1) / chunk);
 }

@@ -43,7 +43,7 @@ constexpr int kScaleSlots = 4;
 constexpr int kSoftmaxWarps = 8, kProducerWarps = 4, kMmaWarp = kSoftmaxWarps + kProducerWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 4);                // four warpgroups; of the last, two warps work
 // Registers a thread of each role: over the warpgroups their sum is what the block is launched with.
-constexpr int kLaunchRegs = 128, kSoftmaxRegs = 184, kProducerRegs = 104, kMmaRegs = 40;
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 176, kProducerRegs = 104, kMmaRegs = 56;
 static_assert(2 * kSoftmaxRegs + kProducerRegs + kMmaRegs <= 4 * kLaunchRegs, "registers of the warpgroups");
 constexpr float kMostP = 32768.0f;           // largest sum of 16 P before m follows the maximum
 // How far log2 of the value scales may lie from the first one's for P to serve the denominator too.  Against m, which a
@@ -120,6 +120,12 @@ __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
   return one != 0;
+}
+// The lowest n bits; none where n < 0, all where n > 32.
+__device__ __forceinline__ uint32_t bits_below(int n) {
+  uint32_t r;
+  asm("bmsk.clamp.b32 %0, 0, %1;" : "=r"(r) : "r"(max(n, 0)));
+  return r;
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -203,37 +209,68 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
       const int h_hi = t.seq.first + (min(t.r0 + 128 * half + 128, t.rows) - 1) / a.group;
       float qs;
       {
-        const uint4* q = reinterpret_cast<const uint4*>(a.Q + (t.seq.row0 + tok) * a.ldq +
-                                                        static_cast<int64_t>(h * a.group + r % a.group) * D);
-        uint4 w[D / 8];
-        float top = 0.0f;
+        // A load takes whole rows, kLanes lanes each.  Every step of this is done for all of a lane's rows before the next, none
+        // behind a branch: as a chain of one row after the other it took 9000 cycles of the block, where nothing else runs.
+        constexpr int kLanes = D / 8, kTogether = 32 / kLanes;
+        const int first = 32 * (warp & 3), sub = lane / kLanes, chunk = lane % kLanes;
+        const int last = t.rows - 1 - (t.r0 + 128 * half + first);           // of the warp's rows, the last there is
+        uint4 w[kLanes];
+        {
+          const uint16_t* base = a.Q + t.seq.row0 * a.ldq + static_cast<int64_t>(h) * a.group * D + 8 * chunk;
+          int tk[kLanes];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) w[i] = in ? __ldg(q + i) : make_uint4(0u, 0u, 0u, 0u);
+          for (int i = 0; i < kLanes; ++i) tk[i] = __shfl_sync(0xffffffffu, tok, min(kTogether * i + sub, max(last, 0)));
+#pragma unroll
+          for (int i = 0; i < kLanes; ++i) {
+            const int rr = t.r0 + 128 * half + first + min(kTogether * i + sub, last);
+            w[i] = last < 0 ? make_uint4(0u, 0u, 0u, 0u)
+                            : __ldg(reinterpret_cast<const uint4*>(base + tk[i] * a.ldq + (rr - tk[i] * a.group) * D));
+          }
+        }
         if (kGeneral && a.across) {          // while q is on its way; padding has no part
           pos = find_rows(a.kv, in ? tok : t.seq.n - 1).pos;
           in = in && pos >= 0;
           if (!in) pos = -1;
           h_lo = __reduce_min_sync(0xffffffffu, in ? pos : INT32_MAX);
         }
+        const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
+        if (rows_in != 0xffffffffu) {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          if (kGeneral && !in) w[i] = make_uint4(0u, 0u, 0u, 0u);
-          float x[8];
-          unpack8(w[i], x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+          for (int i = 0; i < kLanes; ++i)
+            if (!(rows_in >> (kTogether * i + sub) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
         }
-        const uint32_t ex = min(max(__float_as_uint(top) >> 23, 1u), 253u);   // exponent of a normal power of two
-        qs = __uint_as_float(ex << 23);
-        // a negative softmax scale moves into q, so that the scores' coefficients are >= 0
-        const float inv = a.scale_log2 < 0.0f ? -__uint_as_float((254u - ex) << 23) : __uint_as_float((254u - ex) << 23);
+        float top[kLanes];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
+        for (int i = 0; i < kLanes; ++i) {
           float x[8];
           unpack8(w[i], x);
-          st_shared_v4(smem + Sm::kQ + half * Sm::kOperand + (i / 8) * Sm::kBox + swz_offset(r_in, i % 8, 128),
-                       pack_half(x[0] * inv, x[1] * inv), pack_half(x[2] * inv, x[3] * inv),
-                       pack_half(x[4] * inv, x[5] * inv), pack_half(x[6] * inv, x[7] * inv));
+          top[i] = fmaxf(max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), max3(fabsf(x[3]), fabsf(x[4]), fabsf(x[5])));
+          top[i] = max3(top[i], fabsf(x[6]), fabsf(x[7]));
+        }
+        // over a row's lanes; each exchange halves the rows a lane still has, until lane x of them is left with row x
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o /= 2)
+#pragma unroll
+          for (int i = 0; i < o; ++i) {
+            const bool up = lane & o;
+            const float other = __shfl_xor_sync(0xffffffffu, up ? top[i] : top[i + o], o);
+            top[i] = fmaxf(up ? top[i + o] : top[i], other);
+          }
+        const uint32_t ex = min(max(__float_as_uint(fmaxf(top[0], 0.0f)) >> 23, 1u), 253u);   // exponent of a normal power of two
+        qs = __uint_as_float(__shfl_sync(0xffffffffu, ex, lane % kTogether * kLanes + lane / kTogether) << 23);
+        // a negative softmax scale moves into q, so that the scores' coefficients are >= 0
+        const float scale = a.scale_log2 < 0.0f ? -__uint_as_float((254u - ex) << 23) : __uint_as_float((254u - ex) << 23);
+        float inv[kLanes];
+#pragma unroll
+        for (int i = 0; i < kLanes; ++i) inv[i] = __shfl_sync(0xffffffffu, scale, sub * kLanes + i);
+        const uint32_t dst = smem + Sm::kQ + half * Sm::kOperand + (chunk / 8) * Sm::kBox;
+#pragma unroll
+        for (int i = 0; i < kLanes; ++i) {
+          float x[8];
+          unpack8(w[i], x);
+          st_shared_v4(dst + swz_offset(first + kTogether * i + sub, chunk % 8, 128),
+                       pack_half(x[0] * inv[i], x[1] * inv[i]), pack_half(x[2] * inv[i], x[3] * inv[i]),
+                       pack_half(x[4] * inv[i], x[5] * inv[i]), pack_half(x[6] * inv[i], x[7] * inv[i]));
         }
       }
       fence_proxy_async_smem();
@@ -280,10 +317,17 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
         const int c_hi = pos - key;                      // columns c_lo .. c_hi of this row are visible
         const int c_lo = a.window > 0 ? c_hi - a.window + 1 : 0;
         const int c_sink = kGeneral ? a.sinks - number : 0;   // and those before c_sink
+        uint32_t see[2] = {};                            // bit c of word u: column 32 u + c
         if (!all) {
 #pragma unroll
-          for (int c = 0; c < kStepKeys; ++c)
-            if (c > c_hi || (c < c_lo && !(kGeneral && c < c_sink))) s[c / 32][c % 32] = -INFINITY;
+          for (int u = 0; u < 2; ++u) {
+            see[u] = ~bits_below(c_lo - 32 * u);
+            if (kGeneral) see[u] |= bits_below(c_sink - 32 * u);
+            see[u] &= bits_below(c_hi + 1 - 32 * u);
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              if (!(see[u] >> c & 1u)) s[u][c] = -INFINITY;
+          }
         }
         if (fminf(fminf(weight[0], weight[1]), fminf(weight[2], weight[3])) < 0.0f || wild) {
           const uint32_t slot = smem + Sm::kScale + ((i >> 1) % kScaleSlots) * Sm::kSlot + 16 * sub;
@@ -365,8 +409,8 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
                 for (int e = 0; e < 16; e += 2) {
                   float2 x = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(cu, cu), make_float2(du, du));
                   if (decltype(masked)::value) {         // a coefficient of 0 or NaN must not bring a hidden key back
-                    x.x = v[e] == -INFINITY ? -INFINITY : x.x;
-                    x.y = v[e + 1] == -INFINITY ? -INFINITY : x.y;
+                    x.x = see[c / 32] >> (16 * u + e) & 1u ? x.x : -INFINITY;
+                    x.y = see[c / 32] >> (16 * u + e + 1) & 1u ? x.y : -INFINITY;
                   }
                   x.x = ex2(x.x);
                   x.y = ex2(x.y);
@@ -398,14 +442,15 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
         tc_fence_after();
       }
       if (ok) {
-        const int row = 128 * half + r_in;
-        const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) + row;
+        const int64_t slot = ((((static_cast<int64_t>(b) * a.kv.heads + h) * a.row_tiles + rt) * a.splits + split) * a.tile_rows) +
+                             128 * half + r_in;
         const bool whole = ns <= 1 && !(kGeneral && a.keep_parts);
         const float f = whole ? out_factor(l, m - n) : 1.0f;
-        uint16_t* out = a.O + (t.seq.row0 + tok) * a.ldo + static_cast<int64_t>(h * a.group + r % a.group) * D;
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          float o[32];
+        const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
+        // A thread's row goes through the half's part of Q, which nothing reads any more, so that a store takes whole lines
+        // of few rows; the 16-byte pieces of a row lie in an order of its own, for distinct banks.
+        const uint32_t stage = smem + Sm::kQ + half * Sm::kOperand;
+        auto out_row = [&](int c, float (&o)[32]) {
           if (tiles > 0) {
             tmem_ld32(t_o + c, o);
             tmem_ld_wait();
@@ -413,20 +458,53 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 0.0f;
           }
-          if (!in) continue;
-          if (whole) {
+        };
+        if (whole) {
+          constexpr int kLanes = D / 8, kTogether = 32 / kLanes;
+          const int sub = lane / kLanes, chunk = lane % kLanes;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float o[32];
+            out_row(c, o);
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
               float v[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) v[i] = o[e + i] * f;
-              *reinterpret_cast<uint4*>(out + c + e) = pack8(v);
+              const uint4 x = pack8(v);
+              st_shared_v4(stage + r_in * (2 * D) + (((c + e) / 8) ^ (r_in & 7)) * 16, x.x, x.y, x.z, x.w);
             }
-          } else {
+          }
+          __syncwarp();
+#pragma unroll 4
+          for (int i = 0; i < kLanes; ++i) {
+            const int k = kTogether * i + sub, row = r_in - lane + k, rr = r - lane + k;
+            const int tk = __shfl_sync(0xffffffffu, tok, k);
+            const uint4 x = ld_shared_v4(stage + row * (2 * D) + (chunk ^ (row & 7)) * 16);
+            if (rows_in >> k & 1u)
+              reinterpret_cast<uint4*>(a.O + (t.seq.row0 + tk) * a.ldo + static_cast<int64_t>(h * a.group + rr - tk * a.group) * D)[chunk] = x;
+          }
+        } else {
+          float4* part = reinterpret_cast<float4*>(a.part + (slot - lane) * D);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            const uint32_t box = stage + c / 32 % 2 * Sm::kBox * (D / 128);
+            float o[32];
+            out_row(c, o);
+            if (D == 64) __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(a.part + (slot - row) * D + part_at(kPromptRows, D, row, (c + e) / 4, kGeneral && a.keep_parts)) =
-                  make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 8; ++e)
+              st_shared_v4(box + r_in * 128 + (e ^ (r_in & 7)) * 16, __float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                           __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int k = 4 * i + (lane >> 3), row = r_in - lane + k;
+              const uint4 x = ld_shared_v4(box + row * 128 + ((lane & 7) ^ (row & 7)) * 16);
+              if (rows_in >> k & 1u)
+                part[k * (D / 4) + c / 4 + (lane & 7)] =
+                    make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+            }
           }
         }
         if (!whole && in)
@@ -547,7 +625,7 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
         }
         mma_commit(bar(B_SFULL + 2 * half + sub));
       };
-      bool ok = tiles > 0 && wait_spin_bounded(bar(B_QFULL + half), 0, ctl, 7) && wait_spin_bounded(bar(B_KFULL), 0, ctl, 8);
+      bool ok = tiles > 0 && wait_bounded(bar(B_QFULL + half), 0, ctl, 7) && wait_bounded(bar(B_KFULL), 0, ctl, 8);
       if (ok) {
         tc_fence_after();
         scores(0, 0);
@@ -556,9 +634,9 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
       }
       for (int j = 0; j < tiles && ok; ++j) {
         const uint32_t stage = j % kStages, next = (j + 1) % kStages;
-        ok = wait_spin_bounded(bar(B_VFULL + stage), (j / kStages) & 1u, ctl, 9);
+        ok = wait_bounded(bar(B_VFULL + stage), (j / kStages) & 1u, ctl, 9);
         for (uint32_t sub = 0; sub < 2 && ok; ++sub) {
-          if (!(ok = wait_spin_bounded(bar(B_PFULL + 2 * half + sub), j & 1u, ctl, 10))) break;
+          if (!(ok = wait_bounded(bar(B_PFULL + 2 * half + sub), j & 1u, ctl, 10))) break;
           tc_fence_after();
 #pragma unroll
           for (uint32_t ks = 0; ks < kStepKeys / 16; ++ks)
@@ -567,7 +645,7 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
           mma_commit(bar(B_OFULL + half));
           if (sub == 1) mma_commit(bar(B_VEMPTY + stage));
           if (j + 1 < tiles) {
-            if (sub == 0 && !(ok = wait_spin_bounded(bar(B_KFULL + next), ((j + 1) / kStages) & 1u, ctl, 11))) break;
+            if (sub == 0 && !(ok = wait_bounded(bar(B_KFULL + next), ((j + 1) / kStages) & 1u, ctl, 11))) break;
             tc_fence_after();
             scores(next, sub);                           // in order after the product that reads P from the same columns
             if (sub == 1) mma_commit(bar(B_KEMPTY + next));
@@ -591,7 +669,7 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
 template <int D, bool kGeneral>
 __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(AttnArgs a) {
   prompt_block<D, kGeneral>(a);
-  if (kGeneral && a.keep_parts) finish_behind();
+  if (kGeneral && a.keep_parts && blockIdx.x == 0 && blockIdx.y == 0) finish_behind();
 }
 
 template <int D, bool kGeneral>
