@@ -264,13 +264,16 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
 #pragma unroll
         for (int i = 0; i < kLanes; ++i) inv[i] = __shfl_sync(0xffffffffu, scale, sub * kLanes + i);
         const uint32_t dst = smem + Sm::kQ + half * Sm::kOperand + (chunk / 8) * Sm::kBox;
+        // without keys nothing reads them, and the outputs of a warp that is ahead may lie there by now
+        if (tiles > 0) {
 #pragma unroll
-        for (int i = 0; i < kLanes; ++i) {
-          float x[8];
-          unpack8(w[i], x);
-          st_shared_v4(dst + swz_offset(first + kTogether * i + sub, chunk % 8, 128),
-                       pack_half(x[0] * inv[i], x[1] * inv[i]), pack_half(x[2] * inv[i], x[3] * inv[i]),
-                       pack_half(x[4] * inv[i], x[5] * inv[i]), pack_half(x[6] * inv[i], x[7] * inv[i]));
+          for (int i = 0; i < kLanes; ++i) {
+            float x[8];
+            unpack8(w[i], x);
+            st_shared_v4(dst + swz_offset(first + kTogether * i + sub, chunk % 8, 128),
+                         pack_half(x[0] * inv[i], x[1] * inv[i]), pack_half(x[2] * inv[i], x[3] * inv[i]),
+                         pack_half(x[4] * inv[i], x[5] * inv[i]), pack_half(x[6] * inv[i], x[7] * inv[i]));
+          }
         }
       }
       fence_proxy_async_smem();

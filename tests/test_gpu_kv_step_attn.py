@@ -373,6 +373,20 @@ def test_shared_results_do_not_depend_on_where_the_cache_lies(own, prefix):
     _check(p, p.vals[-2:], keep, q, 0.1, rows=lambda n: [n - 1])
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (8, 4)])
+def test_tiles_of_padding_alone(window, sinks):
+    """Tiles of 256 rows none of which has a position, next to some that have: rows of zeros, call after call."""
+    t = torch()
+    p = Paged([(0, 300), (40, 300), (0, 65), (70, 70)], 2, 128, 16)
+    vals = _fill(p)
+    bits, q = p.random_rows(8)
+    Q, batch = to_dev(bits), p.batch()
+    first = _sinks(p, batch, Q, 0.1, window, sinks, 8)
+    _check(p, vals, first, q, 0.1, window, sinks)
+    for _ in range(20):
+        assert t.equal(_sinks(p, batch, Q, 0.1, window, sinks, 8), first)
+
+
 @pytest.mark.parametrize("new", [1, 40])
 @pytest.mark.parametrize("call", ["sinks", "shared"])
 def test_calls_are_queued_behind_the_work_of_their_stream(call, new):
