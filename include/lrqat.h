@@ -333,8 +333,8 @@ typedef struct {
 int lrqat_rope_turns(const double* freq, int32_t n, uint64_t* turns);
 
 /* Q, Q_out: bf16 [T, n_heads, head_dim], K, K_out: bf16 [T, n_kv_heads, head_dim], rows ldq, ldqo, ldk, ldko elements
- * apart (multiples of 8), so that they may be parts of one projection's output; an output may be its input itself, but
- * not overlap it otherwise.  pos: int32 [T], or NULL for row t at position t; a row at a negative position is padding and
+ * apart (multiples of 8), so that they may be parts of one projection's output; Q_out may be Q itself and K_out K,
+ * and an output that overlaps an array of the call otherwise is refused.  pos: int32 [T], or NULL for row t at position t; a row at a negative position is padding and
  * left as it is.  gamma_q, gamma_k: bf16 [head_dim] or NULL. */
 int lrqat_qk_rope_fwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* Q, int64_t ldq,
                       const uint16_t* K, int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k,
@@ -346,7 +346,8 @@ size_t lrqat_qk_rope_bwd_workspace_bytes(const lrqat_qk_rope* rope, int64_t T);
 /* Gradient at the inputs Q, K (read only where there is a gamma; else NULL allowed): with g the gradient of an output
  * rotated back and r = 1 / sqrt(mean(x^2) + eps),
  *   dx = r (g gamma - x r^2 mean(g gamma x))   (g where gamma is NULL),  dgamma = sum over rows and heads of g x r.
- * dQ_out, dK_out, dQ, dK: bf16, laid out as the forward's arrays; dQ and dK may be one of dQ_out, dK_out, Q, K themselves.
+ * dQ_out, dK_out, dQ, dK: bf16, laid out as the forward's arrays; dQ may be dQ_out or Q itself, dK dK_out or K, and one
+ * that overlaps an array of the call otherwise is refused.
  * Rows at negative positions get a zero gradient and add nothing to dgamma.  dgamma_q, dgamma_k: fp32 [head_dim] or
  * NULL; accumulate = 1 adds to them.  Sums run in a fixed order. */
 int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* dQ_out, int64_t lddqo,

@@ -757,6 +757,34 @@ int validate_rope(const lrqat_qk_rope* r, int64_t T) {
   return LRQAT_OK;
 }
 
+// Whether T rows of `pw` elements, ldp apart, share elements with T rows of `qw`, ldq apart.  Rows of different distances
+// are taken to where what they span overlaps.
+bool rows_meet(const uint16_t* p, int64_t ldp, int64_t pw, const uint16_t* q, int64_t ldq, int64_t qw, int64_t T) {
+  if (!p || !q) return false;
+  const int64_t d = (reinterpret_cast<intptr_t>(q) - reinterpret_cast<intptr_t>(p)) / 2;
+  if (d >= (T - 1) * ldp + pw || -d >= (T - 1) * ldq + qw) return false;
+  if (T == 1 || ldp != ldq) return true;
+  const int64_t m = (d % ldp + ldp) % ldp;       // from a row of p to the next row of q
+  return m < pw || m > ldp - qw;
+}
+// An output may be an input of its own kind itself, and shares nothing with any other array of the call.
+struct RopeRows {
+  const uint16_t* p;
+  int64_t ld;
+};
+int check_apart(const RopeArgs& a, const RopeRows (&out)[2], const RopeRows (*in)[2], int n_in) {
+  auto meet = [&](const RopeRows& x, int i, const RopeRows& y, int j) {
+    return rows_meet(x.p, x.ld, static_cast<int64_t>(a.heads[i]) * a.d, y.p, y.ld, static_cast<int64_t>(a.heads[j]) * a.d, a.T);
+  };
+  bool bad = meet(out[0], 0, out[1], 1);
+  for (int k = 0; k < n_in; ++k)
+    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2; ++j)
+        if (!(i == j && out[i].p == in[k][j].p && (out[i].ld == in[k][j].ld || a.T == 1))) bad = bad || meet(out[i], i, in[k][j], j);
+  return bad ? fail(LRQAT_ERR_INVALID_ARG, "an output overlaps another array of the call (it may be its own input itself)")
+             : static_cast<int>(LRQAT_OK);
+}
+
 RopeArgs rope_args(const lrqat_qk_rope& r, int64_t T) {
   RopeArgs a{};
   a.T = T;
@@ -1556,6 +1584,8 @@ int lrqat_qk_rope_fwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, 
     if (!aligned16(gamma[i])) return fail(LRQAT_ERR_ALIGNMENT, "gamma is not 16-byte aligned");
     a.X[i] = in[i], a.ldx[i] = ld[i], a.gamma[i] = gamma[i], a.Y[i] = out[i], a.ldy[i] = ldo[i];
   }
+  const RopeRows outs[2] = {{a.Y[0], a.ldy[0]}, {a.Y[1], a.ldy[1]}}, ins[1][2] = {{{a.X[0], a.ldx[0]}, {a.X[1], a.ldx[1]}}};
+  LRQAT_TRY(check_apart(a, outs, ins, 1));
   DeviceInfo* dev = nullptr;
   LRQAT_TRY(device_info(&dev));
   LRQAT_LAUNCH("qk_rope_fwd", 1, stream, launch_rope_fwd(a, rope->neighbours != 0, dev->sms, stream), "rotation launch");
@@ -1603,6 +1633,10 @@ int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, 
     if (!aligned16(workspace)) return fail(LRQAT_ERR_ALIGNMENT, "workspace is not 16-byte aligned");
     a.part = static_cast<float*>(workspace);
   }
+  if (dgamma_q && dgamma_q == dgamma_k) return fail(LRQAT_ERR_INVALID_ARG, "dgamma_q and dgamma_k must be two arrays");
+  const RopeRows outs[2] = {{a.f.Y[0], a.f.ldy[0]}, {a.f.Y[1], a.f.ldy[1]}};
+  const RopeRows ins[2][2] = {{{a.dY[0], a.lddy[0]}, {a.dY[1], a.lddy[1]}}, {{a.f.X[0], a.f.ldx[0]}, {a.f.X[1], a.f.ldx[1]}}};
+  LRQAT_TRY(check_apart(a.f, outs, ins, 2));
   a.accumulate = accumulate;
   DeviceInfo* dev = nullptr;
   LRQAT_TRY(device_info(&dev));

@@ -64,6 +64,39 @@ def test_rope_arrays(lib):
     assert _bwd(lib, _rope(n_kv_heads=0), dgk=OK) == -1
 
 
+def test_outputs_that_overlap_other_arrays(lib):
+    """Parts of one array, 4 heads for queries, 2 for keys and 2 for values, are apart; so are an output and its own input,
+    where rows are as far apart.  Addresses are never followed: the calls that pass end at the device."""
+    try:
+        import torch
+        if torch.cuda.is_available():
+            pytest.skip("calls that pass would run")
+    except ImportError:
+        pass
+    r, at = _rope(), lambda array, element=0: 16 + (array << 20) + 2 * element
+    part = dict(ldq=1024, ldk=1024, ldqo=1024, ldko=1024)
+    fwd = lambda Q, K, Qo, Ko, **kw: _fwd(lib, r, Q=Q, K=K, Qo=Qo, Ko=Ko, **dict(part, **kw))  # noqa: E731
+    passes = -5                                                    # no device
+    q, k = at(1), at(1, 512)
+    assert fwd(q, k, q, k) == passes and fwd(q, k, at(2), at(2, 512)) == passes
+    assert fwd(q, k, at(2), at(3), ldqo=512, ldko=256) == passes
+    assert fwd(q, k, at(2), at(2, 504)) == -1 and "overlap" in LQ.last_error()     # a head's end over the keys
+    assert fwd(q, k, at(1, 8), at(2)) == -1 and fwd(q, k, at(2), q) == -1 and fwd(q, k, k, at(2)) == -1
+    assert fwd(q, k, q, at(2), ldqo=512) == -1                     # in place, rows at other distances
+    assert fwd(q, k, q, at(2), ldqo=512, T=1) == passes
+    assert fwd(q, k, at(1, 4 * 1024), at(2)) == passes and fwd(q, k, at(1, 3 * 1024), at(2)) == -1
+    assert fwd(at(1, 768), at(2), at(1), at(3)) == -1 and fwd(at(1, 512), at(2), at(1), at(3)) == passes
+    bwd = lambda dQo, dKo, Q, K, dQ, dK, **kw: _bwd(lib, r, dQo=dQo, dKo=dKo, Q=Q, K=K, dQ=dQ, dK=dK, dgk=64, **kw)  # noqa: E731
+    a = [at(i) for i in range(1, 7)]
+    assert bwd(*a) == passes and bwd(*a[:4], a[0], a[1]) == passes and bwd(*a[:4], a[2], a[3]) == passes
+    for dq, dk in ((a[1], a[5]), (a[3], a[5]), (a[4], a[0]), (a[4], a[2]), (a[4], a[4])):
+        assert bwd(*a[:4], dq, dk) == -1
+    assert bwd(*a[:4], a[0], a[5], lddq=1024) == -1
+    assert _bwd(lib, r, dQo=a[0], dKo=a[1], Q=a[2], K=a[3], dQ=a[4], dK=a[5]) == -1        # one dgamma for both
+    # the inputs of heads without a norm are not read
+    assert bwd(*a[:4], a[4], a[2], gq=None, dgq=None) == passes
+
+
 def test_turns_of_frequencies(lib):
     """Exact to half a unit of 2^-64 turns (pi to 87 digits), wrapped around, for either sign."""
     from fractions import Fraction
