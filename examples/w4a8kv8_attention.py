@@ -11,8 +11,10 @@ for the prompts and one for the single tokens, than over both at once):
     y = quantize(a) W_o^T                     act_quant, linear_fwd_quantized
     h, x = y + h, quantized norm              add_rmsnorm_fwd: what the block's MLP takes
 
-Positions: the block has none of its own.  A model with rotary positions rotates q and k between the projection and
-kv_write; the library has no operator for that.
+With rotary positions, q and k are normed by head and rotated in place between the projection and kv_write
+(qk_rope_fwd); the attention may leave a few first tokens visible behind its window (kv_attn_sinks) or read a prefix that
+all sequences share once for all of them (kv_attn_shared).  RunningSequences keeps lengths, block tables and the list of free
+blocks on the device (kv_extend, kv_truncate), so that a step copies nothing but how many tokens each sequence gets.
 
 Training, a normed projection that keeps its activations as one byte each: the codes and scales of
 add_rmsnorm_fwd, from which act_dequant rebuilds X_hat for the backward of the projection, and
@@ -64,8 +66,10 @@ class Projection:
 
 
 class AttentionBlock:
-    def __init__(self, qkv: Projection, out: Projection, gamma_in, gamma_out, heads: int, kv_heads: int, head_dim: int):
+    def __init__(self, qkv: Projection, out: Projection, gamma_in, gamma_out, heads: int, kv_heads: int, head_dim: int,
+                 rope: LQ.QKRope = None, gamma_q=None, gamma_k=None):
         self.qkv, self.out, self.gamma_in, self.gamma_out = qkv, out, gamma_in, gamma_out
+        self.rope, self.gamma_q, self.gamma_k = rope, gamma_q, gamma_k
         self.heads, self.kv_heads, self.d = heads, kv_heads, head_dim
         self.norm = LQ.Norm(qkv.k, EPS, 8)
 
@@ -74,17 +78,30 @@ class AttentionBlock:
         LQ.add_rmsnorm_fwd(self.norm, x.shape[0], x, residual, gamma, h, x_hat, None, None)
         return h, x_hat
 
-    def step(self, x, residual, cache: LQ.KVCache, batch: LQ.KVBatch, window: int = 0):
-        """x, residual: bf16 [rows, hidden], the newest tokens of the batch's sequences.  Returns the residual
+    def step(self, x, residual, cache: LQ.KVCache, batch: LQ.KVBatch, window: int = 0, sinks: int = 0, pos=None,
+             prefix_table=None):
+        """x, residual: bf16 [rows, hidden], the newest tokens of the batch's sequences; pos: their positions, for a
+        block with a rotation; prefix_table: the cache blocks that all sequences start with.  Returns the residual
         stream and the quantized input of the MLP."""
         rows = x.shape[0]
         h, x_hat = self.add_norm(x, residual, self.gamma_in)
         qkv = self.qkv.forward(x_hat).view(rows, self.heads + 2 * self.kv_heads, self.d)
         q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], 1)
+        if self.rope is not None:
+            LQ.qk_rope_fwd(self.rope, pos, q, k, self.gamma_q, self.gamma_k, q, k)
         LQ.kv_write(cache, batch, k, v)
-        a = torch.empty(rows, self.heads, self.d, dtype=torch.bfloat16, device="cuda")
-        ws = torch.empty(LQ.kv_attn_workspace_bytes(cache, batch, self.heads, window), dtype=torch.uint8, device="cuda")
-        LQ.kv_attn(cache, batch, q, 1.0 / math.sqrt(self.d), window, a, ws)
+        a, scale = torch.empty(rows, self.heads, self.d, dtype=torch.bfloat16, device="cuda"), 1.0 / math.sqrt(self.d)
+        room = lambda n: torch.empty(n, dtype=torch.uint8, device="cuda")  # noqa: E731
+        if prefix_table is not None:
+            prefix = prefix_table.numel() * cache.block
+            ws = room(LQ.kv_attn_shared_workspace_bytes(cache, batch, self.heads, prefix))
+            LQ.kv_attn_shared(cache, batch, prefix_table, prefix, q, scale, a, ws)
+        elif sinks:
+            ws = room(LQ.kv_attn_sinks_workspace_bytes(cache, batch, self.heads, window, sinks))
+            LQ.kv_attn_sinks(cache, batch, q, scale, window, sinks, a, ws)
+        else:
+            ws = room(LQ.kv_attn_workspace_bytes(cache, batch, self.heads, window))
+            LQ.kv_attn(cache, batch, q, scale, window, a, ws)
         a_hat = torch.empty_like(a)
         LQ.act_quant(self.out.layer, rows, a, None, a_hat)
         return self.add_norm(self.out.forward(a_hat.view(rows, -1)), h, self.gamma_out)
@@ -110,6 +127,38 @@ class Sequences:
             starts.append(starts[-1] + n)
         as_int = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
         return LQ.KVBatch.of(as_int(self.length), as_int(starts), self.table, starts[-1], max(new), max(self.length))
+
+
+class RunningSequences:
+    """The same with everything on the device; the first `prefix_blocks` blocks are a prefix of all sequences."""
+
+    def __init__(self, n_seqs: int, max_len: int, n_blocks: int, kv_heads: int, head_dim: int, block: int, prefix_blocks: int = 0):
+        shape, width = (n_blocks, kv_heads, block, head_dim), -(-max_len // block)
+        codes = [torch.empty(shape, dtype=torch.int8, device="cuda") for _ in range(2)]
+        scale = [torch.empty(shape[:2], device="cuda") for _ in range(2)]
+        self.cache = LQ.KVCache.of(*codes, *scale)
+        ints = lambda *n: torch.zeros(*n, dtype=torch.int32, device="cuda")  # noqa: E731
+        ids = torch.randperm(n_blocks, device="cuda").int()
+        self.prefix_table = ids[n_blocks - prefix_blocks:].clone()
+        self.free = torch.full((1,), n_blocks - prefix_blocks, dtype=torch.int32, device="cuda")
+        self.table = ints(n_seqs, width)
+        self.table[:, :prefix_blocks] = self.prefix_table
+        self.length = ints(n_seqs)
+        self.blocks = LQ.KVBlocks.of(self.table, ids, block, prefix_blocks)
+        self.batch_len, self.start, self.max_len = ints(n_seqs), ints(n_seqs + 1), max_len
+        self.room = torch.empty(LQ.kv_blocks_workspace_bytes(self.blocks), dtype=torch.uint8, device="cuda")
+
+    def append(self, new, rows: int, max_new: int):
+        """The batch that adds new[b] tokens (int32 on the device; below 0: rows of padding) to sequence b, and the positions
+        of its rows; rows, max_new: bounds on all rows and on a sequence's."""
+        pos = torch.empty(rows, dtype=torch.int32, device="cuda")
+        LQ.kv_extend(self.blocks, self.length, new, self.free, self.length, self.free, self.batch_len, self.start, pos, None,
+                     self.room)
+        return LQ.KVBatch.of(self.batch_len, self.start, self.table, rows, max_new, self.max_len), pos
+
+    def shorten(self, keep):
+        """Sequence b to keep[b] tokens (0: it is finished)."""
+        LQ.kv_truncate(self.blocks, self.length, keep, self.free, self.length, self.free, self.room)
 
 
 def train_step(proj: Projection, gamma, x, residual, dy, dh):
@@ -150,6 +199,23 @@ def main():
         LQ.get_device_status()
         print(f"new tokens {new}: residual stream rms {h.float().pow(2).mean().sqrt():.3f}, "
               f"MLP input rms {x_hat.float().pow(2).mean().sqrt():.3f}")
+    # the same with rotary positions, behind a prefix of 512 tokens that is in the cache once
+    block.rope = LQ.QKRope.of(heads, kv_heads, d, LQ.rope_turns([10000.0 ** (-2 * i / d) for i in range(d // 2)]).cuda())
+    running = RunningSequences(4, 2048, 128, kv_heads, d, 64, prefix_blocks=8)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    rows = lambda n: [torch.randn(n, hidden, device="cuda").bfloat16() for _ in range(2)]  # noqa: E731
+    alone = LQ.KVBatch.of(ints([512]), ints([0, 512]), running.prefix_table[None], 512, 512, 512)
+    block.step(*rows(512), running.cache, alone, pos=torch.arange(512, device="cuda").int())
+    running.length.fill_(512)
+    for new, keep in (([40, 7, 90, 1], None), ([4, 4, 4, -1], [1, 1, 2, 1]), ([1, 1, 1, 1], None)):
+        n = sum(abs(m) for m in new)
+        batch, pos = running.append(ints(new), n, max(new))
+        h, x_hat = block.step(*rows(n), running.cache, batch, pos=pos, prefix_table=running.prefix_table)
+        if keep:                                                     # the drafted tokens that were wrong
+            running.shorten(running.length - ints([max(m - k, 0) for m, k in zip(new, keep)]))
+        LQ.get_device_status()
+        print(f"shared prefix, new tokens {new}: MLP input rms {x_hat.float().pow(2).mean().sqrt():.3f}, "
+              f"lengths {running.length.tolist()}, free blocks {int(running.free)}")
     T = 1000
     x, residual, dh = (torch.randn(T, hidden, device="cuda").bfloat16() for _ in range(3))
     dy = torch.randn(T, hidden, device="cuda").bfloat16()
