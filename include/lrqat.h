@@ -485,7 +485,7 @@ int lrqat_kv_attn_sinks(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch
  * lies in cache block prefix_table[p / block] (int32 [prefix / block], on the device), p >= prefix in
  * block_table[b, p / block]; the first prefix / block columns of block_table are not followed.  len and positions count the
  * prefix; a row at a position inside it sees its part up to there.  Keys and values of the prefix are read once for all rows
- * of the batch, or once for each sequence where its own rows keep the machine busy.  prefix: a multiple of block, 0 for
+ * of the batch, or once for each sequence where that is faster.  prefix: a multiple of block, 0 for
  * none; the rest as for lrqat_kv_attn without a window, of which the results are, bit for bit, those with prefix = 0. */
 size_t lrqat_kv_attn_shared_workspace_bytes(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_t n_heads,
                                             int32_t prefix);

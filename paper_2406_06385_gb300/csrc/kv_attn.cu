@@ -660,8 +660,20 @@ void plan_attn(AttnArgs& a, int sms) {
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);
 }
 
+// Whether the prefix is read once for the rows of all sequences.  That takes two launches more than a call in which each
+// sequence goes over prefix and own keys, about 8 us, which the other readings of the prefix have to be worth: in bytes for
+// 8-row tiles and, at about a third of their rate, for 16-row tiles; 256-row tiles walk over 512 keys in that time.  32 / 8
+// heads of 128, together and apart: single tokens of 8 sequences behind 4000 tokens (57 MB less) 22.4 and 22.6 us, 32
+// behind 1024 (65 MB) 20.3 and 28.7, 2 behind 32000 (66 MB) 29 and 31, 16 behind 1024 (32 MB) 18.7 and 18.4, 4 behind 2000
+// (12 MB) 16.4 and 12.8; 4 tokens of 32 sequences behind 304 (19 MB) 21.4 and 14.4, 2 behind 8000 (16 MB) 23.8 and 20.5, 4
+// behind 4000 (25 MB) 23.0 and 24.5, 16 behind 1024 (32 MB) 21.8 and 32.8; 5 tokens of 16 sequences behind 320 20.8 and
+// 17.4, 20 of 4 behind 512 19.1 and 22.5, 5 of 8 behind 1024 18.7 and 37.0.  Up to 128 rows a sequence and head: with more,
+// each sequence's own tiles keep the machine busy.
 bool shared_together(const AttnArgs& a) {
-  return a.kv.n_seqs > 1 && static_cast<int64_t>(a.kv.max_rows) * a.group <= 128;
+  const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
+  if (a.kv.n_seqs < 2 || rows > 128) return false;
+  const double saved = (a.kv.n_seqs - 1.0) * a.prefix * a.kv.heads * 2.0 * a.kv.d;
+  return rows <= 8 ? saved >= 64e6 : rows <= 16 ? saved >= 20e6 : a.prefix >= 512;
 }
 
 // At most one wave of pieces: a piece costs its start and its join whatever its length.  Blocks of the prompt kernel have

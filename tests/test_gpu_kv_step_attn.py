@@ -192,6 +192,14 @@ SHARED = [
     (16, [(3000, 1), (2500, 1), (1, 1)], 4, 2, 128, 16),
     (20000, [(7, 2), (300, 1)], 2, 4, 128, 32),
     (3104, [(10, 20), (15, 18), (3, 3)], 2, 4, 64, 16),
+    # long enough to be read once for all: 8, 12 and 160 rows in all (some of padding or inside the prefix) over it
+    (12800, [(1, 1), (20, 1)], 20, 4, 128, 64),
+    (16000, [(1, 1), (20, 1), (-1 - 100, 1)], 8, 4, 128, 16),
+    (6400, [(i % 7 + 1, 1) for i in range(37)] + [(-1, 1), (-1 - 5000, 1), (-1 - 64, 1)], 2, 4, 64, 64),
+    (1600, [(5, 4), (40, 3), (9, 2), (-1 - 2, 4), (-1 - 1599, 1)] + [(5, 4)] * 15, 4, 4, 128, 32),
+    (640, [(2, 30), (-1 - 5, 30), (-1, 4), (-1 - 100, 25), (0, 0), (300, 1)], 2, 4, 128, 128),
+    (512, [(i, 17) for i in range(9)], 3, 1, 64, 16),
+    (576, [(130, 1), (7, 2)], 1, 60, 128, 64),
 ]
 
 
@@ -230,8 +238,10 @@ def test_no_prefix_is_the_plain_call(new):
     assert t.equal(out, _attn(p, batch, Q, 0.1, 0, 8))
 
 
-@pytest.mark.parametrize("own", [[(30, 1), (200, 1), (1, 1)], [(30, 6), (200, 6), (7, 6)], [(300, 100), (100, 100)]])
-def test_shared_scales_far_apart_and_zero(own):
+@pytest.mark.parametrize("own,prefix", [
+    ([(30, 1), (200, 1), (1, 1)], 160), ([(30, 6), (200, 6), (7, 6)], 160), ([(300, 100), (100, 100)], 160),
+    ([(30, 1), (200, 1), (1, 1)], 62512), ([(30, 6), (200, 6), (7, 6)], 19600), ([(300, 50), (100, 50)], 528)])
+def test_shared_scales_far_apart_and_zero(own, prefix):
     """Values of 1e20 behind negligible weights, tiny ones behind the whole weight, blocks of scale 0; on either side of the
     prefix's end.  Bound as for one table."""
     def far(kv, used, scale):
@@ -241,7 +251,7 @@ def test_shared_scales_far_apart_and_zero(own):
         return scale
 
     rng = np.random.default_rng(3)
-    p = Shared(160, own, 2, 128, 16, seed=8, kv_scale=far)
+    p = Shared(prefix, own, 2, 128, 16, seed=8, kv_scale=far)
     bits, q = p.random_rows(4)
     O = p.attend(to_dev(bits), 0.5, 4)
     LQ.get_device_status()
@@ -253,9 +263,9 @@ def test_shared_scales_far_apart_and_zero(own):
         assert (np.abs(got[at] - ref) <= bound).all()
 
 
-@pytest.mark.parametrize("new", [1, 6, 100])
-def test_nan_in_one_sequence_stays_there(new):
-    p = Shared(160, [(200, new), (150, new)], 2, 128, 16, seed=9)
+@pytest.mark.parametrize("new,prefix", [(1, 160), (6, 160), (100, 160), (1, 125008), (6, 39072), (40, 528)])
+def test_nan_in_one_sequence_stays_there(new, prefix):
+    p = Shared(prefix, [(200, new), (150, new)], 2, 128, 16, seed=9)
     bits, q = p.random_rows(4)
     ref = bits_to_f32(p.attend(to_dev(bits), 0.1, 4))
     p.scale[1][p.blocks[1][-1]] = float("nan")
@@ -270,12 +280,14 @@ def test_nan_in_one_sequence_stays_there(new):
     assert (np.abs(got[~hit] - ref[~hit]) <= 2.0 ** -7 * np.abs(ref[~hit]) + 2.0 ** -10 * np.abs(p.vals[0][1]).max()).all()
 
 
-@pytest.mark.parametrize("own", [[(30, 1), (200, 1), (1, 1)], [(300, 100), (100, 100)]])
-def test_shared_bounds_and_bad_blocks_are_reported(own):
+@pytest.mark.parametrize("own,prefix", [([(30, 1), (200, 1), (1, 1)], 160), ([(300, 100), (100, 100)], 160),
+                                        ([(30, 1), (200, 1), (1, 1)], 62512), ([(30, 5), (200, 6), (7, 4)], 19600),
+                                        ([(300, 50), (100, 50)], 528)])
+def test_shared_bounds_and_bad_blocks_are_reported(own, prefix):
     """A sequence beyond the batch's bounds, or with a block outside the pool, is reported, and the others are served; so is
     a block of the prefix outside the pool."""
     t = torch()
-    p = Shared(160, own, 2, 128, 16, seed=14)
+    p = Shared(prefix, own, 2, 128, 16, seed=14)
     bits, q = p.random_rows(4)
     Q = to_dev(bits)
     n0 = own[0][1]
@@ -312,14 +324,16 @@ def test_shared_bounds_and_bad_blocks_are_reported(own):
     assert e.value.status == -7
 
 
-@pytest.mark.parametrize("own,group", [([(31, 1)] * 3, 4), ([(31, 1)] * 9, 4), ([(31, 5)] * 9, 4), ([(90, 90)] * 2, 4)])
-def test_shared_strided_rows_other_streams_and_graphs(own, group):
+@pytest.mark.parametrize("own,group,prefix", [
+    ([(31, 1)] * 3, 4, 320), ([(31, 1)] * 9, 4, 320), ([(31, 5)] * 9, 4, 320), ([(90, 90)] * 2, 4, 320),
+    ([(31, 1)] * 9, 4, 15632), ([(31, 4)] * 9, 4, 4896), ([(31, 5)] * 9, 4, 528)])
+def test_shared_strided_rows_other_streams_and_graphs(own, group, prefix):
     """Q and O as parts of wider rows, on a side stream; a captured call replayed for other lengths, for another number of
     rows, and beside a second graph with a workspace of its own."""
     t = torch()
-    p = Shared(320, [(m + 40, n) for m, n in own], 2, 128, 16, seed=12)
+    p = Shared(prefix, [(m + 40, n) for m, n in own], 2, 128, 16, seed=12)
     vals = p.vals
-    p.seqs = [(320 + m, n) for m, n in own]
+    p.seqs = [(prefix + m, n) for m, n in own]
     heads, rows = 2 * group, sum(n for _, n in own)
     bits, q = p.random_rows(heads)
     batch = p.batch(slack=40)
@@ -336,26 +350,27 @@ def test_shared_strided_rows_other_streams_and_graphs(own, group):
     lens, Q = batch.tensors[0], to_dev(bits)
     outs, graphs = [t.zeros_like(Q) for _ in range(2)], []
     for O in outs:
-        ws = empty((LQ.kv_attn_shared_workspace_bytes(p.cache, batch, heads, 320),), t.uint8)
+        ws = empty((LQ.kv_attn_shared_workspace_bytes(p.cache, batch, heads, prefix),), t.uint8)
         graph = t.cuda.CUDAGraph()
         with t.cuda.graph(graph):
-            LQ.kv_attn_shared(p.cache, batch, p.prefix_table, 320, Q, 0.1, O, ws)
+            LQ.kv_attn_shared(p.cache, batch, p.prefix_table, prefix, Q, 0.1, O, ws)
         graphs.append((graph, ws))
     for add in (0, 37, -25, -320):
-        lens.copy_(t.tensor([320 + m + add for m, _ in own], dtype=t.int32))
+        lens.copy_(t.tensor([prefix + m + add for m, _ in own], dtype=t.int32))
         streams = [t.cuda.Stream() for _ in graphs]
         for s, (graph, _) in zip(streams, graphs):
             s.wait_stream(t.cuda.current_stream())
             with t.cuda.stream(s):
                 graph.replay()
         t.cuda.synchronize()
-        p.seqs = [(320 + m + add, n) for m, n in own]
-        cut = [[v[:320 + m + add] for v in vs] for vs, (m, _) in zip(vals, own)]
+        p.seqs = [(prefix + m + add, n) for m, n in own]
+        cut = [[v[:prefix + m + add] for v in vs] for vs, (m, _) in zip(vals, own)]
         for O in outs:
             _check(p, cut, O, q, 0.1)
 
 
-@pytest.mark.parametrize("own,prefix", [([(1, 1)] * 2, 30000), ([(60, 1)] * 64, 6000), ([(300, 1)] * 20, 640), ([(9, 5)] * 16, 2000)])
+@pytest.mark.parametrize("own,prefix", [([(1, 1)] * 2, 30000), ([(1, 1)] * 2, 32000), ([(60, 1)] * 64, 6000), ([(300, 1)] * 20, 640),
+                                        ([(300, 4)] * 20, 640), ([(9, 5)] * 16, 2000)])
 def test_shared_results_do_not_depend_on_where_the_cache_lies(own, prefix):
     t = torch()
     p = Shared(prefix, own, 8, 128, 16, seed=15)
@@ -387,12 +402,12 @@ def test_tiles_of_padding_alone(window, sinks):
         assert t.equal(_sinks(p, batch, Q, 0.1, window, sinks, 8), first)
 
 
-@pytest.mark.parametrize("new", [1, 40])
-@pytest.mark.parametrize("call", ["sinks", "shared"])
-def test_calls_are_queued_behind_the_work_of_their_stream(call, new):
+@pytest.mark.parametrize("call,new,prefix", [("sinks", 1, 160), ("sinks", 40, 160), ("shared", 1, 160), ("shared", 40, 160),
+                                             ("shared", 1, 125008), ("shared", 20, 528)])
+def test_calls_are_queued_behind_the_work_of_their_stream(call, new, prefix):
     t = torch()
-    p = Shared(160, [(90, new), (new, new)], 2, 128, 16, seed=32)
-    p.table[:, :10] = np.array(p.prefix_blocks)
+    p = Shared(prefix, [(90, new), (new, new)], 2, 128, 16, seed=32)
+    p.table[:, :prefix // 16] = np.array(p.prefix_blocks)
     src = to_dev(p.random_rows(8)[0])
     junk, side, batch = empty((1 << 28,), t.float32), t.cuda.Stream(), p.batch()
 
@@ -404,11 +419,11 @@ def test_calls_are_queued_behind_the_work_of_their_stream(call, new):
             for i in range(20):
                 junk.fill_(float(i))
             Q.copy_(src)
-        ws = empty((1 << 22,), t.uint8)
+        ws = empty((1 << 24,), t.uint8)
         if call == "sinks":
             LQ.kv_attn_sinks(p.cache, batch, Q, 0.1, 30, 5, O, ws, stream=stream)
         else:
-            LQ.kv_attn_shared(p.cache, batch, p.prefix_table, 160, Q, 0.1, O, ws, stream=stream)
+            LQ.kv_attn_shared(p.cache, batch, p.prefix_table, prefix, Q, 0.1, O, ws, stream=stream)
         t.cuda.synchronize()
         return O
 
