@@ -1,13 +1,17 @@
-"""Builds liblrqat.so in-tree for sm_103a (nvcc, one -gencode, parallel compiles).
+"""Builds liblrqat.so in-tree for sm_103a (nvcc, one -gencode, parallel compiles), and the Python binding's short way into
+it (g++, against the installed torch; without torch or Python's headers the binding does without).
 
 Usage: python -m paper_2406_06385_gb300.build [--force]
 """
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -24,6 +28,22 @@ HEADERS = ["kernels.h", "merge.h", "ptx.cuh", "quant.cuh", "serve.h", "serve.cuh
            "attn.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
+
+
+def binding_path() -> str:
+    """Where the binding's short way for the installed torch lies, "" without torch or Python's headers."""
+    if not importlib.util.find_spec("torch") or not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return ""
+    return os.path.join(LIB_DIR, f"lrqat_binding-{importlib.metadata.version('torch').split('+')[0]}-{sys.implementation.cache_tag}.so")
+
+
+def binding_command(target: str):
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    include = [sysconfig.get_paths()["include"], os.path.join(torch, "include"), cuda, INCLUDE]
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w"] + [f"-I{i}" for i in include]
+            + [os.path.join(CSRC, "binding.cpp"), "-o", target, f"-L{LIB_DIR}", "-l:liblrqat.so", "-Wl,-rpath,$ORIGIN",
+               f"-L{os.path.join(torch, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
 
 
 def nvcc() -> str:
@@ -73,6 +93,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("linking liblrqat.so failed")
         os.replace(tmp, LIB_PATH)
+    binding = binding_path()
+    source = [os.path.join(CSRC, "binding.cpp"), os.path.join(INCLUDE, "lrqat.h")]
+    if binding and (force or _stale(binding, source)):
+        r = subprocess.run(binding_command(binding + ".tmp"), capture_output=True, text=True)
+        if r.returncode != 0:
+            sys.stderr.write(r.stdout + r.stderr)
+            raise RuntimeError("compiling the binding failed")
+        os.replace(binding + ".tmp", binding)
     return LIB_PATH
 
 

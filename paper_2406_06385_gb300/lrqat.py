@@ -4,11 +4,15 @@ Argument marshalling only: every function here forwards torch tensor pointers
 and the current CUDA stream to the C entry point of the same name and raises
 ``LrqatError`` on a non-OK status.  All computation happens in the library's
 CUDA kernels; there is no fallback when the library is missing.
+
+The calls of a serving step first try a short way (csrc/binding.cpp), which looks at the same arguments in
+compiled code and returns None for whatever it does not find in order; the checks here then say what is wrong.
 """
 from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -90,6 +94,13 @@ class KVCache(ctypes.Structure):
     def of(cls, k_codes, v_codes, k_scale, v_scale) -> "KVCache":
         """`k_codes`, `v_codes`: int8 [n_blocks, n_kv_heads, block, head_dim]; `k_scale`, `v_scale`: fp32
         [n_blocks, n_kv_heads]; all dense.  The cache keeps the tensors alive."""
+        if _short is not None:
+            cache = cls()
+            device = _short.fill_cache(cache, k_codes, v_codes, k_scale, v_scale)
+            if device is not None:
+                cache.tensors = (k_codes, v_codes, k_scale, v_scale)
+                cache.device = device
+                return cache
         shape, scales = k_codes.shape, k_scale.shape
         if (len(shape) != 4 or v_codes.shape != shape or scales != shape[:2] or v_scale.shape != scales
                 or not (k_codes.is_contiguous() and v_codes.is_contiguous() and k_scale.is_contiguous()
@@ -119,6 +130,13 @@ class KVBatch(ctypes.Structure):
     def of(cls, lens, row_start, block_table, rows: int, max_rows: int, max_len: int) -> "KVBatch":
         """`lens` int32 [n_seqs], `row_start` int32 [n_seqs + 1], `block_table` int32 [n_seqs, max_blocks], all
         dense device tensors, which the batch keeps alive; `rows`, `max_rows`, `max_len`: the host's bounds."""
+        if _short is not None:
+            batch = cls()
+            device = _short.fill_batch(batch, lens, row_start, block_table, rows, max_rows, max_len)
+            if device is not None:
+                batch.tensors = (lens, row_start, block_table)
+                batch.device = device
+                return batch
         n_seqs, max_blocks = block_table.shape
         if (lens.shape != (n_seqs,) or row_start.shape != (n_seqs + 1,)
                 or not (lens.is_contiguous() and row_start.is_contiguous() and block_table.is_contiguous())):
@@ -166,6 +184,13 @@ class KVBlocks(ctypes.Structure):
     def of(cls, block_table, free_ids, block: int, pinned: int = 0) -> "KVBlocks":
         """`block_table` int32 [n_seqs, max_blocks], `free_ids` int32 [capacity], dense device tensors, which are kept
         alive."""
+        if _short is not None:
+            blocks = cls()
+            device = _short.fill_blocks(blocks, block_table, free_ids, block, pinned)
+            if device is not None:
+                blocks.tensors = (block_table, free_ids)
+                blocks.device = device
+                return blocks
         i32 = (_types or _dtypes())[2]
         if block_table.dim() != 2 or free_ids.dim() != 1 or not (block_table.is_contiguous() and free_ids.is_contiguous()):
             raise LrqatError(-1, "block_table and free_ids must be dense, of two and one dimensions")
@@ -181,11 +206,30 @@ class KVBlocks(ctypes.Structure):
 
 
 _lib = None
+_short = None                          # csrc/binding.cpp
+_short_tried = False
+
+
+def _load_short():
+    """The short way, where it has been built for the torch that is running."""
+    from importlib.machinery import ExtensionFileLoader
+    from importlib.util import module_from_spec, spec_from_file_location
+    import torch
+    path = os.path.join(os.path.dirname(LIB_PATH), f"lrqat_binding-{torch.__version__.split('+')[0]}-{sys.implementation.cache_tag}.so")
+    if not os.path.exists(path):
+        return None
+    spec = spec_from_file_location("lrqat_binding", path, loader=ExtensionFileLoader("lrqat_binding", path))
+    module = module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 def lib() -> ctypes.CDLL:
     """Loads liblrqat.so; raises if it has not been built."""
-    global _lib
+    global _lib, _short, _short_tried
+    if _lib is not None and not _short_tried and "torch" in sys.modules:
+        _short_tried = True
+        _short = _load_short()
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2406_06385_gb300.build`")
@@ -264,6 +308,7 @@ def lib() -> ctypes.CDLL:
         L.lrqat_kv_attn_shared_workspace_bytes.argtypes = [cp, bp, i32, i32]
         L.lrqat_kv_attn_shared_workspace_bytes.restype = ctypes.c_size_t
         _lib = L
+        return lib()
     return _lib
 
 
@@ -500,6 +545,10 @@ def qk_rope_fwd(rope: QKRope, pos, Q, K, gamma_q, gamma_k, Q_out, K_out, stream=
     """Norm of each head (where its gamma is not None) and rotation by position of Q, bf16 [T, n_heads, head_dim], and
     K, bf16 [T, n_kv_heads, head_dim], into Q_out and K_out (which may be Q and K).  pos: int32 [T], or None for row t at
     position t; rows at negative positions are left as they are."""
+    if stream is None and _short is not None:
+        status = _short.qk_rope_fwd(rope, pos, Q, K, gamma_q, gamma_k, Q_out, K_out)
+        if status is not None:
+            return _check(status)
     hq, hk, d = rope.n_heads, rope.n_kv_heads, rope.head_dim
     q, ldq, rows, device = _head_rows(Q, hq, d, None, None, "Q")
     k, ldk, rows, device = _head_rows(K, hk, d, rows, device, "K")
@@ -513,6 +562,10 @@ def qk_rope_fwd(rope: QKRope, pos, Q, K, gamma_q, gamma_k, Q_out, K_out, stream=
 
 
 def qk_rope_bwd_workspace_bytes(rope: QKRope, T: int) -> int:
+    if _short is not None:
+        size = _short.qk_rope_bwd_workspace_bytes(rope, T)
+        if size is not None:
+            return size
     return int(lib().lrqat_qk_rope_bwd_workspace_bytes(ctypes.byref(rope), T))
 
 
@@ -520,6 +573,11 @@ def qk_rope_bwd(rope: QKRope, pos, dQ_out, dK_out, Q, K, gamma_q, gamma_k, dQ, d
                 workspace, stream=None) -> None:
     """Gradient of qk_rope_fwd at its inputs Q and K (None where there is no gamma).  dgamma_q, dgamma_k: fp32 [head_dim] or
     None (without both the workspace may be None)."""
+    if stream is None and _short is not None:
+        status = _short.qk_rope_bwd(rope, pos, dQ_out, dK_out, Q, K, gamma_q, gamma_k, dQ, dK, dgamma_q, dgamma_k, accumulate,
+                                    workspace)
+        if status is not None:
+            return _check(status)
     hq, hk, d = rope.n_heads, rope.n_kv_heads, rope.head_dim
     _, f32, i32, _ = _types or _dtypes()
     gq, ldgq, rows, device = _head_rows(dQ_out, hq, d, None, None, "dQ_out")
@@ -538,6 +596,10 @@ def qk_rope_bwd(rope: QKRope, pos, dQ_out, dK_out, Q, K, gamma_q, gamma_k, dQ, d
 
 
 def kv_blocks_workspace_bytes(blocks: KVBlocks) -> int:
+    if _short is not None:
+        size = _short.kv_blocks_workspace_bytes(blocks)
+        if size is not None:
+            return size
     return int(lib().lrqat_kv_blocks_workspace_bytes(ctypes.byref(blocks)))
 
 
@@ -571,6 +633,10 @@ def kv_extend(blocks: KVBlocks, lens, add, free_count, lens_out, free_out, batch
     the tables, and the batch's layout.  lens, add, lens_out, batch_lens: int32 [n_seqs]; free_count, free_out: int32 [1];
     row_start: int32 [n_seqs + 1]; pos: int32 [rows]; slot: int64 [rows] or None.  lens_out may be lens, free_out
     free_count."""
+    if stream is None and _short is not None:
+        status = _short.kv_extend(blocks, lens, add, free_count, lens_out, free_out, batch_lens, row_start, pos, slot, workspace)
+        if status is not None:
+            return _check(status)
     n, rows = blocks.n_seqs, 0 if pos is None else pos.numel()
     p, device = _blocks_arrays(
         blocks, ("lens", "add", "free_count", "lens_out", "free_out", "batch_lens", "row_start", "pos"),
@@ -585,6 +651,10 @@ def kv_extend(blocks: KVBlocks, lens, add, free_count, lens_out, free_out, batch
 def kv_truncate(blocks: KVBlocks, lens, keep, free_count, lens_out, free_out, workspace, stream=None) -> None:
     """Shortens sequence b to keep[b] tokens and appends the blocks it no longer needs to the free list.  lens, keep,
     lens_out: int32 [n_seqs]; free_count, free_out: int32 [1]; lens_out may be lens, free_out free_count."""
+    if stream is None and _short is not None:
+        status = _short.kv_truncate(blocks, lens, keep, free_count, lens_out, free_out, workspace)
+        if status is not None:
+            return _check(status)
     n = blocks.n_seqs
     p, device = _blocks_arrays(blocks, ("lens", "keep", "free_count", "lens_out", "free_out"),
                                (lens, keep, free_count, lens_out, free_out), (n, n, 1, n, 1))
@@ -638,18 +708,30 @@ def _attn_rows(cache: KVCache, batch: KVBatch, Q, O, workspace):
 
 
 def kv_attn_sinks_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window: int, sinks: int) -> int:
+    if _short is not None:
+        size = _short.kv_attn_sinks_workspace_bytes(cache, batch, n_heads, window, sinks)
+        if size is not None:
+            return size
     return int(lib().lrqat_kv_attn_sinks_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, window, sinks))
 
 
 def kv_attn_sinks(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, sinks: int, O, workspace,
                   stream=None) -> None:
     """kv_attn through a window that leaves the first `sinks` tokens visible."""
+    if stream is None and _short is not None:
+        status = _short.kv_attn_sinks(cache, batch, Q, softmax_scale, window, sinks, O, workspace)
+        if status is not None:
+            return _check(status)
     heads, ldq, ldo, nbytes, _ = _attn_rows(cache, batch, Q, O, workspace)
     _check(lib().lrqat_kv_attn_sinks(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, sinks, _ptr(Q),
                                      ldq, _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
 
 
 def kv_attn_shared_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, prefix: int) -> int:
+    if _short is not None:
+        size = _short.kv_attn_shared_workspace_bytes(cache, batch, n_heads, prefix)
+        if size is not None:
+            return size
     return int(lib().lrqat_kv_attn_shared_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, prefix))
 
 
@@ -657,6 +739,10 @@ def kv_attn_shared(cache: KVCache, batch: KVBatch, prefix_table, prefix: int, Q,
                    stream=None) -> None:
     """Causal attention of a batch whose sequences start with the same `prefix` tokens (a multiple of the block), which lie
     in the cache blocks prefix_table, int32 [prefix / block]."""
+    if stream is None and _short is not None:
+        status = _short.kv_attn_shared(cache, batch, prefix_table, prefix, Q, softmax_scale, O, workspace)
+        if status is not None:
+            return _check(status)
     heads, ldq, ldo, nbytes, device = _attn_rows(cache, batch, Q, O, workspace)
     columns = -(-prefix // cache.block) if prefix > 0 and cache.block > 0 else 0
     if columns and prefix_table is None:
