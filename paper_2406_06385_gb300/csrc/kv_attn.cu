@@ -610,6 +610,30 @@ cudaError_t launch_shared(const AttnArgs& p, const AttnArgs& a, cudaStream_t str
 
 }  // namespace
 
+// Keys of a piece of 16- or 256-row tiles whose blocks come in waves of `slots`, and the call's time for it.  A block takes
+// about 6.5 us and 13.1 ns a key (16 rows, two blocks an SM) or 7 us and 14.1 ns (256 rows), a launch 3 us and the join one
+// more and its bytes; all are fitted to windows of 100 to 4000 keys and 4 sinks, 20 to 128 rows of 1, 16 and 64 sequences
+// with 8 heads.
+struct Pieces {
+  int64_t chunk;
+  double ns;
+};
+Pieces plan_pieces(const AttnArgs& a, int64_t keys, int tile_rows, int sms) {
+  const bool prompt = tile_rows == kPromptRows;
+  const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group, unit = 128, slots = prompt ? sms : sms * (kPerSm / 2);
+  const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * ((rows + tile_rows - 1) / tile_rows);
+  Pieces best{(keys + unit) / unit * unit, 0.0};
+  for (int64_t pieces = 1; pieces <= 64; ++pieces) {
+    const int64_t chunk = ((keys + pieces - 1) / pieces + unit - 1) / unit * unit, blocks = tiles * pieces;
+    double ns = 3000.0 + static_cast<double>((blocks + slots - 1) / slots) * (prompt ? 7000.0 + 14.1 * chunk : 6500.0 + 13.1 * chunk);
+    if (pieces > 1) ns += 4000.0 + 2.0 * blocks * tile_rows * a.kv.d * sizeof(float) / 6800.0;
+    if (pieces == 1) best.ns = ns;
+    else if (ns < best.ns) best = {chunk, ns};
+    if (chunk <= unit || blocks > 4 * slots) break;
+  }
+  return best;
+}
+
 // Up to 16 rows per sequence and key/value head the keys' bytes bound the call, and 8- or 16-row tiles of
 // the warp-level kernel stream them; above, the 256-row tiles of the prompt kernel convert a key once for
 // all of them.  Both sides of the limit, 32 / 8 heads, 4000 tokens: 12 and 16 rows, 16 sequences, 48 and 49
@@ -628,18 +652,35 @@ cudaError_t launch_shared(const AttnArgs& p, const AttnArgs& a, cudaStream_t str
 // in one wave: one sequence of 32001 tokens 20 us (two waves 24, 10 for its bytes), 4 drafted tokens behind
 // 32000 24 us (31), 12 windows of 1000 tokens 10.6 us (12).  The host knows bounds, not lengths: that two
 // sequences are about equally long is a guess (one of 32001 tokens beside one of 100: 25 us).
+//
+// Calls through sinks or behind a prefix (kv_attn's own calls keep their plans, and so their bits) choose between 16- and
+// 256-row tiles up to 128 rows, and the pieces of both, by plan_pieces: 32 rows of 1, 16 and 64 sequences with 500 keys
+// take 12, 18.5 and 59 us in 16-row tiles and 16, 18.5 and 67 in 256-row tiles, with 4000 keys 16, 62 and 237 and 18.5, 66
+// and 245 (kv_attn's plans: 18.5, 51 and 67, 19.5, 106 and 245); 64 rows with 500 keys 14, 33 and 107 and 16, 18.5 and 67.
 void plan_attn(AttnArgs& a, int sms) {
   const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
+  const bool general = attn_general(a);
   a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
+  a.sink_pad = static_cast<int>((static_cast<int64_t>(a.sinks) + 15) & ~15);
+  int64_t keys = a.kv.max_len > a.first ? a.kv.max_len - a.first : 0;
+  // the keys that a tile of `tile_rows` rows may see
+  auto in_window = [&](int tile_rows) {
+    const int64_t tokens = general ? (tile_rows + a.group - 2) / a.group + 1 : tile_rows;
+    const int64_t w = static_cast<int64_t>(a.window) + tokens + kKeyAlign + a.sink_pad;
+    return a.window > 0 && w < keys ? w : keys;
+  };
+  Pieces cut{0, 0.0};
+  if (general && rows > 8) {
+    cut = plan_pieces(a, in_window(a.tile_rows), a.tile_rows, sms);
+    if (rows > 16 && rows <= 128) {
+      const Pieces small = plan_pieces(a, in_window(16), 16, sms);
+      if (small.ns < cut.ns) cut = small, a.tile_rows = 16;
+    }
+  }
   const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;
-  a.sink_pad = static_cast<int>((static_cast<int64_t>(a.sinks) + 15) & ~15);
-  int64_t keys = a.kv.max_len > a.first ? a.kv.max_len - a.first : 0;
-  if (a.window > 0) {
-    const int64_t w = static_cast<int64_t>(a.window) + a.tile_rows + kKeyAlign + a.sink_pad;
-    keys = keys < w ? keys : w;
-  }
+  keys = in_window(a.tile_rows);
   const int64_t tiles = static_cast<int64_t>(a.kv.n_seqs) * a.kv.heads * a.row_tiles;
   const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
   const int64_t want = at_once * (prompt || 4 * tiles < at_once ? 2 : 4);
@@ -653,37 +694,36 @@ void plan_attn(AttnArgs& a, int sms) {
     chunk = (keys + at_once / tiles - 1) / (at_once / tiles);
   chunk = (chunk + unit - 1) / unit * unit;
   if (chunk < least) chunk = least;
+  if (cut.chunk > 0) chunk = cut.chunk;
   const int64_t whole = (keys + unit) / unit * unit;         // with many tiles keys * tiles / want passes 32 bits
-  if (chunk > whole || (prompt && tiles >= want)) chunk = whole;
+  if (chunk > whole || (prompt && cut.chunk == 0 && tiles >= want)) chunk = whole;
   a.chunk = static_cast<int>(chunk);
   const int64_t splits = (keys + chunk - 1) / chunk;
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);
 }
 
-// Whether the prefix is read once for the rows of all sequences.  That takes two launches more than a call in which each
-// sequence goes over prefix and own keys, about 8 us, which the other readings of the prefix have to be worth: in bytes for
-// 8-row tiles and, at about a third of their rate, for 16-row tiles; 256-row tiles walk over 512 keys in that time.  32 / 8
-// heads of 128, together and apart: single tokens of 8 sequences behind 4000 tokens (57 MB less) 22.4 and 22.6 us, 32
-// behind 1024 (65 MB) 20.3 and 28.7, 2 behind 32000 (66 MB) 29 and 31, 16 behind 1024 (32 MB) 18.7 and 18.4, 4 behind 2000
-// (12 MB) 16.4 and 12.8; 4 tokens of 32 sequences behind 304 (19 MB) 21.4 and 14.4, 2 behind 8000 (16 MB) 23.8 and 20.5, 4
-// behind 4000 (25 MB) 23.0 and 24.5, 16 behind 1024 (32 MB) 21.8 and 32.8; 5 tokens of 16 sequences behind 320 20.8 and
-// 17.4, 20 of 4 behind 512 19.1 and 22.5, 5 of 8 behind 1024 18.7 and 37.0.  Up to 128 rows a sequence and head: with more,
-// each sequence's own tiles keep the machine busy.
 bool shared_together(const AttnArgs& a) {
-  const int64_t rows = static_cast<int64_t>(a.kv.max_rows) * a.group;
-  if (a.kv.n_seqs < 2 || rows > 128) return false;
-  const double saved = (a.kv.n_seqs - 1.0) * a.prefix * a.kv.heads * 2.0 * a.kv.d;
-  return rows <= 8 ? saved >= 64e6 : rows <= 16 ? saved >= 20e6 : a.prefix >= 512;
+  return a.kv.n_seqs > 1 && static_cast<int64_t>(a.kv.max_rows) * a.group <= 128;
+}
+
+// A planned call in which every sequence goes over prefix and own keys: 8-row tiles take 9 us and their bytes at 5200 GB/s,
+// the others what plan_pieces says.
+double apart_ns(const AttnArgs& a, int sms) {
+  const double keys = a.kv.max_len;
+  if (a.tile_rows == 8) return 9000.0 + a.kv.n_seqs * keys * a.kv.heads * 2.0 * a.kv.d / 5200.0;
+  return plan_pieces(a, a.kv.max_len, a.tile_rows, sms).ns;
 }
 
 // At most one wave of pieces: a piece costs its start and its join whatever its length.  Blocks of the prompt kernel have
-// an SM to themselves, and the sequences' own keys, which run beside them, what is left and then all: a piece takes 9 us
-// and 2 us a tile of 128 keys, the own keys the time of three quarters of their bound's bytes at the copy rate and 0.75 us
-// of an SM a block.  64 rows of 32 heads, 8 of them for keys, behind 16000 tokens, 500 of their own: 18 pieces 50 us, 15
-// 41, 13 42, 10 48; 16 x 5 rows of 40 heads behind 2000 tokens: three pieces 35 us, two 32, one 45.
-void plan_prefix(AttnArgs& a, int sms) {
+// an SM to themselves, and the sequences' own keys (`own`, planned), which run beside them, what is left and then all: a
+// piece takes 9 us and 2 us a tile of 128 keys; own keys, of an SM, 0.75 us a block and three quarters of their bound's
+// bytes at the copy rate in 8-row tiles, 3.25 us and 6.5 ns a key in 16-row tiles, 7 us and 14.1 ns in 256-row tiles.  64 rows
+// of 32 heads, 8 of them for keys, behind 16000 tokens, 500 of their own: 18 pieces 50 us, 15 41, 13 42, 10 48; 16 x 5
+// rows of 40 heads behind 2000 tokens: three pieces 35 us, two 32, one 45.  Returns the call's time with launches and
+// join, about 8 us and the parts' bytes.
+double plan_prefix(AttnArgs& a, const AttnArgs& own, int sms) {
   const int64_t rows = a.kv.rows * a.group;
-  a.tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kPromptRows;
+  a.tile_rows = rows <= 8 ? 8 : rows <= 48 ? 16 : kPromptRows;
   const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;
@@ -691,22 +731,29 @@ void plan_prefix(AttnArgs& a, int sms) {
   const int64_t at_once = static_cast<int64_t>(sms) * (prompt ? 1 : a.tile_rows == 8 ? kPerSm : kPerSm / 2);
   const int64_t most = tiles < at_once ? at_once / tiles : 1, unit = 128;
   auto chunk_of = [&](int64_t pieces) { return ((a.prefix + pieces - 1) / pieces + unit - 1) / unit * unit; };
+  const double copy_rate = 6800.0;           // bytes a nanosecond, the machine
+  const double keys = a.kv.max_len > a.prefix ? a.kv.max_len - a.prefix : 0, key_bytes = 2.0 * a.kv.d;
+  const double own_ns = static_cast<double>(a.kv.n_seqs) * a.kv.heads * own.row_tiles *
+                        (own.tile_rows == 8 ? 750.0 + 0.75 * keys * key_bytes / copy_rate * sms
+                                            : own.tile_rows == 16 ? 3250.0 + 6.5 * keys : 7000.0 + 14.1 * keys);
   int64_t chunk = chunk_of(most);
-  if (prompt && most > 1) {
-    const double copy_rate = 6.8e3;          // bytes a nanosecond, the machine
-    const double blocks = static_cast<double>(a.kv.n_seqs) * a.kv.heads, own = a.kv.max_len > a.prefix ? a.kv.max_len - a.prefix : 0;
-    const double own_ns = blocks * (0.75 * own * 2 * a.kv.d / copy_rate * sms + 750.0);      // of one SM
-    double best = 0.0;
+  double best = 0.0;
+  if (prompt) {
     for (int64_t pieces = most; pieces >= 1; --pieces) {
-      const int64_t c = chunk_of(pieces), used = (a.prefix + c - 1) / c;
-      const double mine = 9000.0 + 2000.0 / unit * c, left = own_ns - mine * (sms - used * tiles);
+      const int64_t c = chunk_of(pieces), used = (a.prefix + c - 1) / c, waves = (used * tiles + sms - 1) / sms;
+      const double mine = waves * (9000.0 + 2000.0 / unit * c), left = own_ns - mine * (sms * waves - used * tiles) / waves;
       const double all = mine + (left > 0.0 ? left / sms : 0.0);
       if (pieces == most || all < best) best = all, chunk = c;
       if (mine > best) break;
     }
+  } else {
+    const double bytes = a.prefix * key_bytes * a.kv.heads / 5200.0;
+    best = a.tile_rows == 8 ? 4000.0 : 6500.0 + 13.1 * chunk;
+    best = (best > bytes + 4000.0 ? best : bytes + 4000.0) + own_ns / sms;
   }
   a.chunk = static_cast<int>(chunk);
   a.splits = static_cast<int>((a.prefix + chunk - 1) / chunk);
+  return best + 8000.0 + static_cast<double>(rows) * a.kv.heads * (a.splits + own.splits) * a.kv.d * sizeof(float) / copy_rate;
 }
 
 cudaError_t launch_kv_attn(const AttnArgs& a, cudaStream_t stream) {

@@ -715,18 +715,22 @@ int shared_args(const lrqat_kv_cache* cache, const lrqat_kv_batch* batch, int32_
   if (prefix > static_cast<int64_t>(a.kv.max_blocks) << a.kv.block_log2)
     return fail(LRQAT_ERR_INVALID_ARG, "prefix %d exceeds max_blocks * block", prefix);
   a.prefix = prefix;
-  if (prefix == 0 || !shared_together(a)) return LRQAT_OK;
-  AttnArgs p = a;
-  p.across = p.keep_parts = 1;
-  plan_prefix(p, sm_count());
-  if (a.kv.rows * a.group > (1 << 24) || static_cast<int64_t>(p.kv.heads) * p.row_tiles > 65535 ||
-      static_cast<int64_t>(p.splits) * p.kv.heads > INT32_MAX)
-    return LRQAT_OK;
+  if (prefix == 0) return LRQAT_OK;
+  const int sms = sm_count();
+  plan_attn(a, sms);
+  LRQAT_TRY(attn_fits(a));
+  if (!shared_together(a) || a.kv.rows * a.group > (1 << 24)) return LRQAT_OK;
   AttnArgs own = a;
   own.first = prefix;
   own.keep_parts = own.behind = 1;
-  plan_attn(own, sm_count());
-  if (attn_fits(own) != LRQAT_OK) return LRQAT_OK;
+  plan_attn(own, sms);
+  AttnArgs p = a;
+  p.across = p.keep_parts = 1;
+  // the estimates are good to a tenth; together takes another launch of the host's
+  if (plan_prefix(p, own, sms) > 0.9 * apart_ns(a, sms)) return LRQAT_OK;
+  if (attn_fits(own) != LRQAT_OK || static_cast<int64_t>(p.kv.heads) * p.row_tiles > 65535 ||
+      static_cast<int64_t>(p.splits) * p.kv.heads > INT32_MAX)
+    return LRQAT_OK;
   s->a = own;
   s->p = p;
   s->together = true;

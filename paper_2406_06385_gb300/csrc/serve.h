@@ -180,10 +180,12 @@ inline bool attn_general(const AttnArgs& a) { return a.sinks || a.prefix; }
 inline int attn_grid_seqs(const AttnArgs& a) { return a.across ? 1 : a.kv.n_seqs; }
 // Sets chunk, splits, tile_rows, row_tiles and sink_pad for the batch's bounds.
 void plan_attn(AttnArgs& a, int sms);
-// The same for the pass of all rows over the prefix.
-void plan_prefix(AttnArgs& a, int sms);
-// Whether the batch's rows go over a shared prefix together.
+// A call in which each sequence goes over a shared prefix and its own keys, and one in which the rows of all go over the
+// prefix together (planned here) and then each sequence over its own keys (`own`, planned): about how long they take.
+// shared_together: whether that is worth a comparison; sequences with many rows keep the machine busy by themselves.
 bool shared_together(const AttnArgs& a);
+double apart_ns(const AttnArgs& a, int sms);
+double plan_prefix(AttnArgs& a, const AttnArgs& own, int sms);
 inline int64_t attn_part_rows(const AttnArgs& a) {
   return a.splits > 1 || a.keep_parts
              ? static_cast<int64_t>(attn_grid_seqs(a)) * a.kv.heads * a.row_tiles * a.splits * a.tile_rows

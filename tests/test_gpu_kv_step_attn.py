@@ -161,6 +161,7 @@ class Shared(Paged):
         self.table[:, first:first + table.shape[1]] = table[1:]
         self.seqs = seqs
         self.vals = [[np.concatenate([a, b])[:length] for a, b in zip(vals[0], v)] for v, (length, _) in zip(vals[1:], seqs)]
+        self.together = None
         self.prefix_table = to_dev(np.array(self.prefix_blocks, np.int32))
 
     def attend(self, Q, scale, n_heads, batch=None, out=None, stream=None):
@@ -169,7 +170,12 @@ class Shared(Paged):
         O = t.full(Q.shape, 0x7FC0, dtype=t.int16, device="cuda") if out is None else out
         ws = empty((LQ.kv_attn_shared_workspace_bytes(self.cache, batch, n_heads, self.prefix),), t.uint8)
         ws.fill_(0xFF)
+        LQ.trace_enable(True)
         LQ.kv_attn_shared(self.cache, batch, self.prefix_table, self.prefix, Q, scale, O, ws, stream=stream)
+        LQ.trace_enable(False)
+        launches = LQ.trace_read()["kv_attn_shared"][0]
+        if self.together is not None:                        # over the prefix, over the own keys, the join
+            assert (launches == 3) == self.together
         return O
 
 
@@ -192,36 +198,53 @@ SHARED = [
     (16, [(3000, 1), (2500, 1), (1, 1)], 4, 2, 128, 16),
     (20000, [(7, 2), (300, 1)], 2, 4, 128, 32),
     (3104, [(10, 20), (15, 18), (3, 3)], 2, 4, 64, 16),
-    # long enough to be read once for all: 8, 12 and 160 rows in all (some of padding or inside the prefix) over it
-    (12800, [(1, 1), (20, 1)], 20, 4, 128, 64),
-    (16000, [(1, 1), (20, 1), (-1 - 100, 1)], 8, 4, 128, 16),
-    (6400, [(i % 7 + 1, 1) for i in range(37)] + [(-1, 1), (-1 - 5000, 1), (-1 - 64, 1)], 2, 4, 64, 64),
-    (1600, [(5, 4), (40, 3), (9, 2), (-1 - 2, 4), (-1 - 1599, 1)] + [(5, 4)] * 15, 4, 4, 128, 32),
     (640, [(2, 30), (-1 - 5, 30), (-1, 4), (-1 - 100, 25), (0, 0), (300, 1)], 2, 4, 128, 128),
     (512, [(i, 17) for i in range(9)], 3, 1, 64, 16),
     (576, [(130, 1), (7, 2)], 1, 60, 128, 64),
 ]
+# where the prefix is read once for all: in 8-row tiles, in one and three 16-row tiles, in 256-row tiles; the own keys in
+# tiles of 8, 16 and 256 rows; with padding, sequences inside the prefix and rows at both sides of its end
+TOGETHER = [
+    (16000, [(1, 1), (20, 1)], 8, 4, 128, 64),
+    (12800, [(1, 1), (20, 1)], 20, 4, 128, 16),
+    (16000, [(1, 1), (20, 1), (-1 - 100, 1), (-1, 1)], 8, 4, 128, 16),
+    (8000, [(3, 1)] * 9 + [(-1 - 7000, 1), (-1 - 64, 1), (200, 1)], 8, 4, 64, 64),
+    (4096, [(i * 13 % 70 + 1, 1) for i in range(37)] + [(-1, 1), (-1 - 4000, 1), (-1 - 64, 1)], 8, 4, 64, 64),
+    (4096, [(5, 4), (40, 3), (9, 2), (-1 - 2, 4), (-1 - 1599, 1), (1, 4), (-1 - 4096, 2), (60, 4), (5, 4), (7, 4)], 8, 4, 128, 32),
+    (4096, [(2, 8), (-1 - 5, 8), (-1, 4), (-1 - 100, 8), (0, 0), (300, 1), (8, 8)], 8, 4, 128, 128),
+    (2000, [(9, 5)] * 14 + [(1, 5), (-1 - 3, 5)], 40, 1, 128, 16),
+    (16000, [(2000, 32), (1500, 20), (3, 7)], 8, 4, 128, 64),
+    (16000, [(3, 4), (90, 1), (4, 4)], 8, 30, 64, 32),
+]
 
 
-@pytest.mark.parametrize("prefix,own,heads,group,d,block", SHARED)
-def test_shared(prefix, own, heads, group, d, block):
+@pytest.mark.parametrize("prefix,own,heads,group,d,block,together",
+                         [c + (False,) for c in SHARED] + [c + (True,) for c in TOGETHER])
+def test_shared(prefix, own, heads, group, d, block, together):
     t = torch()
     p = Shared(prefix, own, heads, d, block, seed=prefix + len(own))
+    p.together = together
     bits, q = p.random_rows(heads * group)
     scale = 1.3 / np.sqrt(d)
     O = p.attend(to_dev(bits), scale, heads * group)
     LQ.get_device_status()
-    _check(p, p.vals, O, q, scale)
+    some = (lambda n: sorted({0, n - 1}) if n else []) if together else None
+    _check(p, p.vals, O, q, scale, rows=some)
     assert t.equal(O, p.attend(to_dev(bits), scale, heads * group))
     slack = min(200, p.table.shape[1] * block - max(n for n, _ in p.seqs))
     loose = p.batch(slack=slack)
-    loose.rows += 50                                         # rows behind the last sequence: left as they were
-    wide = t.full((len(bits) + 50,) + bits.shape[1:], 7, dtype=t.int16, device="cuda")
+    if together:                                             # with bounds for which it still is
+        loose.max_rows = p.batch().max_rows
+        if len(bits) * group <= 8:
+            p.together = None                                # but for the tiles that three rows more need
+    behind = 3 if together else 50                           # rows behind the last sequence: left as they were
+    loose.rows += behind
+    wide = t.full((len(bits) + behind,) + bits.shape[1:], 7, dtype=t.int16, device="cuda")
     Q = t.zeros_like(wide)
     Q[:len(bits)] = to_dev(bits)
     p.attend(Q, scale, heads * group, loose, out=wide)
     LQ.get_device_status()
-    _check(p, p.vals, wide[:len(bits)], q, scale)
+    _check(p, p.vals, wide[:len(bits)], q, scale, rows=some)
     assert (wide[len(bits):] == 7).all()
 
 
@@ -238,10 +261,10 @@ def test_no_prefix_is_the_plain_call(new):
     assert t.equal(out, _attn(p, batch, Q, 0.1, 0, 8))
 
 
-@pytest.mark.parametrize("own,prefix", [
-    ([(30, 1), (200, 1), (1, 1)], 160), ([(30, 6), (200, 6), (7, 6)], 160), ([(300, 100), (100, 100)], 160),
-    ([(30, 1), (200, 1), (1, 1)], 62512), ([(30, 6), (200, 6), (7, 6)], 19600), ([(300, 50), (100, 50)], 528)])
-def test_shared_scales_far_apart_and_zero(own, prefix):
+@pytest.mark.parametrize("own,prefix,heads", [
+    ([(30, 1), (200, 1), (1, 1)], 160, 2), ([(30, 6), (200, 6), (7, 6)], 160, 2), ([(300, 100), (100, 100)], 160, 2),
+    ([(30, 1), (200, 1), (1, 1)], 16000, 8), ([(30, 6), (200, 6), (7, 6), (50, 6)], 16000, 8), ([(300, 20), (100, 17)], 20000, 8)])
+def test_shared_scales_far_apart_and_zero(own, prefix, heads):
     """Values of 1e20 behind negligible weights, tiny ones behind the whole weight, blocks of scale 0; on either side of the
     prefix's end.  Bound as for one table."""
     def far(kv, used, scale):
@@ -251,9 +274,10 @@ def test_shared_scales_far_apart_and_zero(own, prefix):
         return scale
 
     rng = np.random.default_rng(3)
-    p = Shared(prefix, own, 2, 128, 16, seed=8, kv_scale=far)
-    bits, q = p.random_rows(4)
-    O = p.attend(to_dev(bits), 0.5, 4)
+    p = Shared(prefix, own, heads, 128, 16, seed=8, kv_scale=far)
+    p.together = prefix > 160
+    bits, q = p.random_rows(2 * heads)
+    O = p.attend(to_dev(bits), 0.5, 2 * heads)
     LQ.get_device_status()
     got = bits_to_f32(O).astype(np.float64)
     for b, length, n, at in _seq_rows(p.seqs):
@@ -263,15 +287,16 @@ def test_shared_scales_far_apart_and_zero(own, prefix):
         assert (np.abs(got[at] - ref) <= bound).all()
 
 
-@pytest.mark.parametrize("new,prefix", [(1, 160), (6, 160), (100, 160), (1, 125008), (6, 39072), (40, 528)])
-def test_nan_in_one_sequence_stays_there(new, prefix):
-    p = Shared(prefix, [(200, new), (150, new)], 2, 128, 16, seed=9)
-    bits, q = p.random_rows(4)
-    ref = bits_to_f32(p.attend(to_dev(bits), 0.1, 4))
+@pytest.mark.parametrize("new,prefix,heads", [(1, 160, 2), (6, 160, 2), (100, 160, 2), (1, 20000, 8), (20, 20000, 8), (40, 20000, 8)])
+def test_nan_in_one_sequence_stays_there(new, prefix, heads):
+    p = Shared(prefix, [(200, new), (150, new)], heads, 128, 16, seed=9)
+    p.together = prefix > 160
+    bits, q = p.random_rows(2 * heads)
+    ref = bits_to_f32(p.attend(to_dev(bits), 0.1, 2 * heads))
     p.scale[1][p.blocks[1][-1]] = float("nan")
     bad = bits.copy()
     bad[0, 1, 5] = 0x7FC0
-    got = bits_to_f32(p.attend(to_dev(bad), 0.1, 4))
+    got = bits_to_f32(p.attend(to_dev(bad), 0.1, 2 * heads))
     assert np.isnan(got[0, 1]).all() and np.isnan(got[-1]).all()
     hit = np.zeros(got.shape[:2], bool)
     hit[0, 1] = True
@@ -280,20 +305,21 @@ def test_nan_in_one_sequence_stays_there(new, prefix):
     assert (np.abs(got[~hit] - ref[~hit]) <= 2.0 ** -7 * np.abs(ref[~hit]) + 2.0 ** -10 * np.abs(p.vals[0][1]).max()).all()
 
 
-@pytest.mark.parametrize("own,prefix", [([(30, 1), (200, 1), (1, 1)], 160), ([(300, 100), (100, 100)], 160),
-                                        ([(30, 1), (200, 1), (1, 1)], 62512), ([(30, 5), (200, 6), (7, 4)], 19600),
-                                        ([(300, 50), (100, 50)], 528)])
-def test_shared_bounds_and_bad_blocks_are_reported(own, prefix):
+@pytest.mark.parametrize("own,prefix,heads", [([(30, 1), (200, 1), (1, 1)], 160, 2), ([(300, 100), (100, 100)], 160, 2),
+                                              ([(30, 1), (200, 1), (1, 1)], 16000, 8), ([(30, 5), (200, 6), (7, 4), (9, 6)], 16000, 8),
+                                              ([(300, 20), (100, 17)], 20000, 8)])
+def test_shared_bounds_and_bad_blocks_are_reported(own, prefix, heads):
     """A sequence beyond the batch's bounds, or with a block outside the pool, is reported, and the others are served; so is
     a block of the prefix outside the pool."""
     t = torch()
-    p = Shared(prefix, own, 2, 128, 16, seed=14)
-    bits, q = p.random_rows(4)
+    p = Shared(prefix, own, heads, 128, 16, seed=14)
+    p.together = prefix > 160
+    bits, q = p.random_rows(2 * heads)
     Q = to_dev(bits)
     n0 = own[0][1]
 
     def expect(batch):
-        O = p.attend(Q, 0.1, 4, batch)
+        O = p.attend(Q, 0.1, 2 * heads, batch)
         with pytest.raises(LQ.LrqatError) as e:
             LQ.get_device_status()
         assert e.value.status == -7
@@ -301,6 +327,7 @@ def test_shared_bounds_and_bad_blocks_are_reported(own, prefix):
         got = bits_to_f32(O).astype(np.float64)
         for b, length, n, at in _seq_rows(p.seqs):
             if b:
+                at = slice(at.stop - min(n, 3 if p.together else n), at.stop)
                 ref, mass, seen = SO.attention(q[at], *p.vals[b], length, 0.1)
                 assert (np.abs(got[at] - ref) <= _bound(ref, mass, seen, np.abs(p.vals[b][1]).max())).all()
         return O
@@ -318,25 +345,28 @@ def test_shared_bounds_and_bad_blocks_are_reported(own, prefix):
     batch.tensors[1][0] = -1                                 # its rows start before the batch's
     expect(batch)
     p.prefix_table[3] = 10 ** 6
-    p.attend(Q, 0.1, 4)
+    p.attend(Q, 0.1, 2 * heads)
     with pytest.raises(LQ.LrqatError) as e:
         LQ.get_device_status()
     assert e.value.status == -7
 
 
-@pytest.mark.parametrize("own,group,prefix", [
-    ([(31, 1)] * 3, 4, 320), ([(31, 1)] * 9, 4, 320), ([(31, 5)] * 9, 4, 320), ([(90, 90)] * 2, 4, 320),
-    ([(31, 1)] * 9, 4, 15632), ([(31, 4)] * 9, 4, 4896), ([(31, 5)] * 9, 4, 528)])
-def test_shared_strided_rows_other_streams_and_graphs(own, group, prefix):
+@pytest.mark.parametrize("own,group,prefix,kv_heads", [
+    ([(31, 1)] * 3, 4, 320, 2), ([(31, 1)] * 9, 4, 320, 2), ([(31, 5)] * 9, 4, 320, 2), ([(90, 90)] * 2, 4, 320, 2),
+    ([(31, 1)] * 9, 4, 8000, 8), ([(31, 4)] * 9, 4, 4800, 8), ([(31, 8)] * 5, 4, 4800, 8)])
+def test_shared_strided_rows_other_streams_and_graphs(own, group, prefix, kv_heads):
     """Q and O as parts of wider rows, on a side stream; a captured call replayed for other lengths, for another number of
     rows, and beside a second graph with a workspace of its own."""
     t = torch()
-    p = Shared(prefix, [(m + 40, n) for m, n in own], 2, 128, 16, seed=12)
+    p = Shared(prefix, [(m + 40, n) for m, n in own], kv_heads, 128, 16, seed=12)
+    p.together = prefix > 320
     vals = p.vals
     p.seqs = [(prefix + m, n) for m, n in own]
-    heads, rows = 2 * group, sum(n for _, n in own)
+    heads, rows = kv_heads * group, sum(n for _, n in own)
     bits, q = p.random_rows(heads)
     batch = p.batch(slack=40)
+    if p.together:                                           # with bounds for which it still is
+        batch.max_rows = own[0][1]
     ref = p.attend(to_dev(bits), 0.1, heads, batch)
     wide = t.zeros((rows, heads + 8, 128), dtype=t.int16, device="cuda")
     wide[:, 4:4 + heads] = to_dev(bits)
@@ -365,11 +395,11 @@ def test_shared_strided_rows_other_streams_and_graphs(own, group, prefix):
         t.cuda.synchronize()
         p.seqs = [(prefix + m + add, n) for m, n in own]
         cut = [[v[:prefix + m + add] for v in vs] for vs, (m, _) in zip(vals, own)]
-        for O in outs:
-            _check(p, cut, O, q, 0.1)
+        assert t.equal(*outs)
+        _check(p, cut, outs[0], q, 0.1, rows=(lambda n: sorted({0, n - 1})) if p.together else None)
 
 
-@pytest.mark.parametrize("own,prefix", [([(1, 1)] * 2, 30000), ([(1, 1)] * 2, 32000), ([(60, 1)] * 64, 6000), ([(300, 1)] * 20, 640),
+@pytest.mark.parametrize("own,prefix", [([(1, 1)] * 2, 30000), ([(60, 1)] * 64, 6000), ([(300, 1)] * 20, 640),
                                         ([(300, 4)] * 20, 640), ([(9, 5)] * 16, 2000)])
 def test_shared_results_do_not_depend_on_where_the_cache_lies(own, prefix):
     t = torch()
@@ -402,13 +432,13 @@ def test_tiles_of_padding_alone(window, sinks):
         assert t.equal(_sinks(p, batch, Q, 0.1, window, sinks, 8), first)
 
 
-@pytest.mark.parametrize("call,new,prefix", [("sinks", 1, 160), ("sinks", 40, 160), ("shared", 1, 160), ("shared", 40, 160),
-                                             ("shared", 1, 125008), ("shared", 20, 528)])
-def test_calls_are_queued_behind_the_work_of_their_stream(call, new, prefix):
+@pytest.mark.parametrize("call,new,prefix,heads", [("sinks", 1, 160, 2), ("sinks", 40, 160, 2), ("shared", 1, 160, 2),
+                                                   ("shared", 40, 160, 2), ("shared", 1, 20000, 8), ("shared", 10, 20000, 8)])
+def test_calls_are_queued_behind_the_work_of_their_stream(call, new, prefix, heads):
     t = torch()
-    p = Shared(prefix, [(90, new), (new, new)], 2, 128, 16, seed=32)
+    p = Shared(prefix, [(90, new), (new, new)], heads, 128, 16, seed=32)
     p.table[:, :prefix // 16] = np.array(p.prefix_blocks)
-    src = to_dev(p.random_rows(8)[0])
+    src = to_dev(p.random_rows(4 * heads)[0])
     junk, side, batch = empty((1 << 28,), t.float32), t.cuda.Stream(), p.batch()
 
     def run(stream):
@@ -419,7 +449,7 @@ def test_calls_are_queued_behind_the_work_of_their_stream(call, new, prefix):
             for i in range(20):
                 junk.fill_(float(i))
             Q.copy_(src)
-        ws = empty((1 << 24,), t.uint8)
+        ws = empty((1 << 25,), t.uint8)
         if call == "sinks":
             LQ.kv_attn_sinks(p.cache, batch, Q, 0.1, 30, 5, O, ws, stream=stream)
         else:

@@ -105,10 +105,10 @@ def test_captured_decode_steps(shared):
     its workspaces."""
     t = torch()
     rng = np.random.default_rng(8)
-    n_seqs, hq, hk, d, P, rows, prefix = 6, 8, 2, 128, 16, 32, 528 if shared else 0
+    n_seqs, hq, hk, d, P, rows, prefix = 6, 32, 8, 128, 16, 32, 8000 if shared else 0
     freq = [500000.0 ** (-2 * i / d) for i in range(d // 2)]
     rope = LQ.QKRope.of(hq, hk, d, LQ.rope_turns(freq).cuda())
-    pool, width, pin = 120, 60, prefix // P
+    pool, width, pin = 120 + prefix // P, 24 + prefix // P, prefix // P
     codes = [t.randint(-127, 128, (pool, hk, P, d), dtype=t.int8, device="cuda") for _ in range(2)]
     scale = [t.rand(pool, hk, device="cuda") * 0.02 + 0.001 for _ in range(2)]
     cache = LQ.KVCache.of(*codes, *scale)
