@@ -265,8 +265,15 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdPerSm) rope_bwd_kernel(RopeB
             yg[e] = __fmul2_rn(y[e], gm[e]);
             gx = __ffma2_rn(yg[e], x[e], gx);
           }
-          const float r = 1.0f / sqrtf(Lane::sum(ss) * inv_d + a.f.eps);
-          const float c = -r * (r * r * (Lane::sum(gx) * inv_d));
+          // over the head's lanes, both at a time: one after the other, and with a division, 51 us where this takes 48
+          float x2 = ss.x + ss.y, xg = gx.x + gx.y;
+#pragma unroll
+          for (int o = L / 2; o > 0; o >>= 1) {
+            const float other_x2 = __shfl_xor_sync(0xffffffffu, x2, o), other_xg = __shfl_xor_sync(0xffffffffu, xg, o);
+            x2 += other_x2, xg += other_xg;
+          }
+          const float r = rsqrtf(x2 * inv_d + a.f.eps);
+          const float c = -r * (r * r * (xg * inv_d));
           if (reads) {                       // eps may be 0: nothing of a head that is not there is added
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
