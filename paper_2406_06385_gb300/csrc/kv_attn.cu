@@ -489,15 +489,20 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_kernel(AttnArgs 
   reinterpret_cast<uint32_t*>(out)[threadIdx.x] = pack_bf16(o0 * inv, o1 * inv);
 }
 
-// Joins the parts of the rows' own keys (`a`) with those of the prefix (`p`), in that order: a warp has one row of the
-// batch and head, its lanes the statistics of 32 parts at a time and the row's dimensions.
+// Joins the parts of the rows' own keys (`a`) with those of the prefix (`p`), in that order: kShares warps have one row of the
+// batch and head, each a share of its parts, a warp's lanes the statistics of 32 parts at a time and the row's dimensions.
+// Many parts, which few rows have, in four shares: 2 sequences behind 16000 tokens (64 parts and their own) 23.8 -> 20.4
+// us, behind 32000 28.9 -> 25.2, 4 x 2 tokens of 16 heads and one for keys behind 30000 28.2 -> 21.6.
 constexpr int kJoinAhead = 8;
-template <int D>
+template <int D, int kShares>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_shared_kernel(AttnArgs a, AttnArgs p) {
   constexpr int kPer = D / 32;
   const int lane = threadIdx.x & 31, h = blockIdx.y;
-  const int64_t rr = static_cast<int64_t>(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
-  if (rr >= a.kv.rows * a.group) return;
+  constexpr int kRows = kJoinWarps / kShares;
+  const int warp = threadIdx.x >> 5, share = warp % kShares;
+  const int64_t rr0 = static_cast<int64_t>(blockIdx.x) * kRows + warp / kShares, rows = a.kv.rows * a.group;
+  const bool none = rr0 >= rows;
+  const int64_t rr = none ? rows - 1 : rr0;
   const int64_t token = rr / a.group;
   const int head = static_cast<int>(rr - token * a.group);
   const RowPlace at = find_rows(a.kv, token);
@@ -521,10 +526,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_shared_kernel(At
     float f[kPer];
   };
   asm volatile("griddepcontrol.wait;" ::: "memory");         // the parts are there
-  if (at.seq < 0) return;
+  const bool skip = none || at.seq < 0;
+  if (kShares == 1 && skip) return;
+  const int per = (all + kShares - 1) / kShares, end = skip ? 0 : min(all, (share + 1) * per);
   float m = -INFINITY, n = -INFINITY, l = 0.0f, acc[kPer] = {};
-  for (int s0 = 0; s0 < all; s0 += 32) {
-    const int count = min(all - s0, 32);
+  for (int s0 = share * per; s0 < end; s0 += 32) {
+    const int count = min(end - s0, 32);
     float4 v = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
     if (lane < count) v = __ldcg(reinterpret_cast<const float4*>((s0 + lane < own ? a : p).part_stat + slot_of(s0 + lane) * 4));
     float f = 0.0f;
@@ -561,6 +568,29 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attn_join_shared_kernel(At
 #pragma unroll
           for (int e = 0; e < kPer; ++e) acc[e] = fmaf(x[u].f[e], fu, acc[e]);
       }
+    }
+  }
+  if constexpr (kShares > 1) {
+    __shared__ float4 stat[kJoinWarps];
+    __shared__ float part[kJoinWarps][D];
+    if (lane == 0) stat[warp] = make_float4(m, n, l, 0.0f);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) part[warp][lane * kPer + e] = acc[e];
+    __syncthreads();
+    if (share != 0 || skip) return;
+#pragma unroll
+    for (int w = 1; w < kShares; ++w) m = fmaxf(m, stat[warp + w].x), n = fmaxf(n, stat[warp + w].y);
+    const float base = finite_max(m), nbase = finite_max(n);
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kShares; ++w) {
+      const float4 v = stat[warp + w];
+      const float f = ex2(v.x - base);
+      l = fmaf(v.z, ex2(v.y - nbase), l);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] = fmaf(part[warp + w][lane * kPer + e], f, acc[e]);
     }
   }
   const float inv = out_factor(l, m - finite_max(n));
@@ -603,9 +633,10 @@ cudaError_t launch_shared(const AttnArgs& p, const AttnArgs& a, cudaStream_t str
   cudaError_t e = launch_parts<D, true>(p, stream);
   if (e == cudaSuccess) e = launch_parts<D, true>(a, stream);
   if (e != cudaSuccess) return e;
-  const int64_t rows = a.kv.rows * a.group;
-  const dim3 grid(static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps), a.kv.heads);
-  return launch_lined_up(kv_attn_join_shared_kernel<D>, grid, 32 * kJoinWarps, 0, 1, stream, a, p);
+  const int shares = a.splits + p.splits > 24 ? 4 : 1, per = kJoinWarps / shares;
+  const dim3 grid(static_cast<unsigned>((a.kv.rows * a.group + per - 1) / per), a.kv.heads);
+  return launch_lined_up(shares == 4 ? kv_attn_join_shared_kernel<D, 4> : kv_attn_join_shared_kernel<D, 1>, grid, 32 * kJoinWarps, 0,
+                         1, stream, a, p);
 }
 
 }  // namespace
@@ -723,7 +754,7 @@ double apart_ns(const AttnArgs& a, int sms) {
 // join, about 8 us and the parts' bytes.
 double plan_prefix(AttnArgs& a, const AttnArgs& own, int sms) {
   const int64_t rows = a.kv.rows * a.group;
-  a.tile_rows = rows <= 8 ? 8 : rows <= 48 ? 16 : kPromptRows;
+  a.tile_rows = rows <= 8 ? 8 : rows <= 32 ? 16 : kPromptRows;      // 48 rows behind 16000: 39 us in 16-row tiles, 64 in 256 34
   const bool prompt = a.tile_rows == kPromptRows;
   a.row_tiles = static_cast<int>((rows + a.tile_rows - 1) / a.tile_rows);
   if (a.row_tiles < 1) a.row_tiles = 1;

@@ -202,12 +202,13 @@ SHARED = [
     (512, [(i, 17) for i in range(9)], 3, 1, 64, 16),
     (576, [(130, 1), (7, 2)], 1, 60, 128, 64),
 ]
-# where the prefix is read once for all: in 8-row tiles, in one and three 16-row tiles, in 256-row tiles; the own keys in
+# where the prefix is read once for all: in 8-row tiles, in one and two 16-row tiles, in 256-row tiles; the own keys in
 # tiles of 8, 16 and 256 rows; with padding, sequences inside the prefix and rows at both sides of its end
 TOGETHER = [
     (16000, [(1, 1), (20, 1)], 8, 4, 128, 64),
     (12800, [(1, 1), (20, 1)], 20, 4, 128, 16),
     (16000, [(1, 1), (20, 1), (-1 - 100, 1), (-1, 1)], 8, 4, 128, 16),
+    (16000, [(3, 1)] * 5 + [(-1 - 7000, 1), (-1 - 64, 1), (200, 1)], 8, 4, 128, 64),
     (8000, [(3, 1)] * 9 + [(-1 - 7000, 1), (-1 - 64, 1), (200, 1)], 8, 4, 64, 64),
     (4096, [(i * 13 % 70 + 1, 1) for i in range(37)] + [(-1, 1), (-1 - 4000, 1), (-1 - 64, 1)], 8, 4, 64, 64),
     (4096, [(5, 4), (40, 3), (9, 2), (-1 - 2, 4), (-1 - 1599, 1), (1, 4), (-1 - 4096, 2), (60, 4), (5, 4), (7, 4)], 8, 4, 128, 32),
