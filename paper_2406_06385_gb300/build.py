@@ -31,8 +31,10 @@ NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-
 
 
 def binding_path() -> str:
-    """Where the binding's short way for the installed torch lies, "" without torch or Python's headers."""
-    if not importlib.util.find_spec("torch") or not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+    """Where the binding's short way for the installed torch lies, "" without a torch for CUDA or Python's headers."""
+    spec = importlib.util.find_spec("torch")
+    if (not spec or not os.path.exists(os.path.join(os.path.dirname(spec.origin), "lib", "libc10_cuda.so"))
+            or not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))):
         return ""
     return os.path.join(LIB_DIR, f"lrqat_binding-{importlib.metadata.version('torch').split('+')[0]}-{sys.implementation.cache_tag}.so")
 

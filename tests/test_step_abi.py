@@ -168,6 +168,32 @@ def recorded(monkeypatch):
     return torch, calls, lambda shape, dtype, device="cuda:0": _stand_in(torch, shape, dtype, device)
 
 
+def test_the_short_way_leaves_what_it_does_not_know(lib):
+    """Without CUDA tensors it says nothing and writes nothing, whatever it is given."""
+    torch = pytest.importorskip("torch")
+    LQ.lib()
+    if LQ._short is None:
+        pytest.skip("not built for this torch")
+    codes, scale, ints = torch.zeros(2, 1, 16, 64, dtype=torch.int8), torch.zeros(2, 1), torch.zeros(2, 1, dtype=torch.int32)
+    cache, batch, blocks = LQ.KVCache(), LQ.KVBatch(), LQ.KVBlocks()
+    for of, args in ((LQ._short.fill_cache, (cache, codes, codes, scale, scale)),
+                     (LQ._short.fill_batch, (batch, ints[:, 0], torch.zeros(3, dtype=torch.int32), ints, 2, 1, 16)),
+                     (LQ._short.fill_blocks, (blocks, ints, ints[:, 0], 16, 0))):
+        assert of(*args) is None and not any(bytes(args[0]))
+        for i in range(len(args)):
+            assert of(*args[:i], None, *args[i + 1:]) is None and of(*args[:i], object(), *args[i + 1:]) is None
+        assert of() is None and of(*args, 1) is None
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    assert LQ._short.kv_attn_sinks(cache, batch, q, 0.1, 0, 0, q, None) is None
+    assert LQ._short.kv_attn_shared(cache, batch, None, 0, q, 0.1, q, None) is None
+    assert LQ._short.qk_rope_fwd(_rope(head_dim=64, rot_dim=64), None, q, q[:, :2], None, None, q, q[:, :2]) is None
+    assert LQ._short.kv_extend(blocks, *[ints] * 8, None, None) is None and LQ._short.kv_truncate(blocks, *[ints] * 5, None) is None
+    # sizes need no tensors, and are the library's
+    assert LQ._short.kv_blocks_workspace_bytes(_blocks()) == lib.lrqat_kv_blocks_workspace_bytes(ctypes.byref(_blocks())) > 0
+    assert LQ._short.qk_rope_bwd_workspace_bytes(_rope(), 4) == lib.lrqat_qk_rope_bwd_workspace_bytes(ctypes.byref(_rope()), 4) > 0
+    assert LQ._short.kv_blocks_workspace_bytes(_rope()) is None and LQ._short.qk_rope_bwd_workspace_bytes(_rope(), 1.5) is None
+
+
 def test_binding_checks_rope_arrays(recorded):
     torch, calls, fake = recorded
     bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
