@@ -450,7 +450,9 @@ def test_calls_are_queued_behind_the_work_of_their_stream(call, new, prefix, hea
             for i in range(20):
                 junk.fill_(float(i))
             Q.copy_(src)
-        ws = empty((1 << 25,), t.uint8)
+        size = (LQ.kv_attn_sinks_workspace_bytes(p.cache, batch, 4 * heads, 30, 5) if call == "sinks"
+                else LQ.kv_attn_shared_workspace_bytes(p.cache, batch, 4 * heads, prefix))
+        ws = empty((size,), t.uint8)
         if call == "sinks":
             LQ.kv_attn_sinks(p.cache, batch, Q, 0.1, 30, 5, O, ws, stream=stream)
         else:
