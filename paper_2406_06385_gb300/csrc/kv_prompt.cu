@@ -24,7 +24,7 @@
 // take 407, without the producers' stores 479, without both 358, almost without matrix instructions still 505.
 // Measured against it: two threads a row 686 of 524 (the exchange of their maxima), one 128-key score buffer 834, eight
 // producer warps with 136 softmax registers 574; a row of q and of O a thread, not whole lines by the warp, 525 of 513;
-// 184, 104 and 40 registers, with spills in the issuing threads, 1% slower; blocks that stay and take over the grid
+// 184, 104 and 40 registers, with spills in the issuing threads, 330 of 322 behind the window; blocks that stay and take over the grid
 // positions of blocks not yet launched, q and keys of the next item brought in beside this one's last steps, 549 us where
 // this takes 536 (one tile of long sequences) and 317 where it takes 322 (the window).
 #include <cuda.h>
