@@ -41,6 +41,7 @@ int fail(int code, const char* fmt, ...) {
 }
 
 int cuda_fail(cudaError_t e, const char* what) {
+  cudaGetLastError();   // this call's: the next one that asks about its launch would report it too
   return fail(LRQAT_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
