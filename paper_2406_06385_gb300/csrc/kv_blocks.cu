@@ -302,7 +302,7 @@ bool extend_alone(const ExtendArgs& a) { return a.rows <= kAloneRows && a.b.n_se
 
 }  // namespace
 
-int kv_extend_launches(const ExtendArgs& a) { return extend_alone(a) ? 1 : 2; }
+int kv_extend_launches(const ExtendArgs& a) { return extend_alone(a) || a.rows == 0 ? 1 : 2; }
 int kv_truncate_launches(const TruncateArgs& a) { return a.b.n_seqs <= kAloneSeqs ? 1 : 2; }
 
 cudaError_t launch_kv_extend(const ExtendArgs& a, cudaStream_t stream) {
@@ -313,6 +313,7 @@ cudaError_t launch_kv_extend(const ExtendArgs& a, cudaStream_t stream) {
   if (a.b.n_seqs <= kScanThreads) kv_extend_scan_kernel<false, 1><<<1, kScanThreads, 0, stream>>>(a);
   else kv_extend_scan_kernel<false, 4><<<1, kScanThreads, 0, stream>>>(a);
   const cudaError_t e = cudaGetLastError();
+  if (a.rows == 0) return e;                 // nothing to expand, and no grid is empty
   return e != cudaSuccess ? e : launch_behind(kv_extend_rows_kernel, a, (a.rows + kWarpRows - 1) / kWarpRows * 32, stream);
 }
 

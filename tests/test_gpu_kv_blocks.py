@@ -148,6 +148,27 @@ def test_the_most_sequences(n_seqs):
     p.truncate(rng.integers(-1, 30, n_seqs))
 
 
+@pytest.mark.parametrize("n_seqs", [3, 1024, 1025, 65535])
+def test_steps_without_rows(n_seqs):
+    """Every sequence pauses: lengths and row starts are laid out all the same, in one launch.  What then asks for rows does
+    not fit them."""
+    length = np.random.default_rng(n_seqs).integers(0, 33, n_seqs)
+    p = Pool(n_seqs, 3, 16, 16, 16, length=length)
+    LQ.trace_enable()
+    try:
+        seen, start, _, _ = p.extend(np.zeros(n_seqs, np.int32), rows=0, in_place=False)
+        assert LQ.trace_read()["kv_extend"][0] == 1
+    finally:
+        LQ.trace_enable(False)
+    assert np.array_equal(seen.cpu().numpy(), length) and not start.any()
+    add = np.zeros(n_seqs, np.int32)
+    add[-1] = 1
+    p.extend(add, rows=0, refused=True)
+    p.extend(np.zeros(n_seqs, np.int32), rows=0)
+    p.extend(add, slots=False)
+    p.truncate(length)
+
+
 def test_long_rows_of_the_table():
     """One sequence of 2^31 - 1152 tokens takes its last blocks."""
     most = (2 ** 31 - 1 - 1024) // 128
