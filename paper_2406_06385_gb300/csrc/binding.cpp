@@ -80,18 +80,30 @@ void on(const at::Tensor& t, int& device) {
   }
   need(at == device);
 }
-// The device that a structure's tensors lie on.
-int device_of(PyObject* o) {
+// The device that a structure's tensors lie on, -1 where the binding has not seen them.
+int device_seen(PyObject* o) {
   PyObject* d = PyObject_GetAttr(o, g_device);
   if (!d) {
     PyErr_Clear();
     throw NotHere{};
   }
-  const bool known = PyLong_CheckExact(d);
-  const long at = known ? PyLong_AsLong(d) : -1;
+  const bool none = d == Py_None, known = none || PyLong_CheckExact(d);
+  int too_long = 0;                          // no error of the interpreter is left behind
+  const long at = none || !known ? -1 : PyLong_AsLongAndOverflow(d, &too_long);
   Py_DECREF(d);
-  need(known && at >= 0 && at == c10::cuda::current_device());
+  need(known && !too_long && (none || (at >= 0 && at <= INT32_MAX)));
   return static_cast<int>(at);
+}
+// The same of a structure whose tensors have been seen, on the current device.
+int device_of(PyObject* o) {
+  const int at = device_seen(o);
+  need(at >= 0 && at == c10::cuda::current_device());
+  return at;
+}
+// The turns of a rotation, where they have been seen, lie on `device`.
+void turns_on(PyObject* o, int device) {
+  const int at = device_seen(o);
+  need(at < 0 || at == device);
 }
 
 bool row_type(const at::Tensor& t) {
@@ -180,6 +192,7 @@ PyObject* qk_rope_fwd(PyObject* const* a) {
   const Rows q = head_rows(a[2], hq, d, rows, device), k = head_rows(a[3], hk, d, rows, device);
   const Rows qo = head_rows(a[6], hq, d, rows, device), ko = head_rows(a[7], hk, d, rows, device);
   need(device >= 0);
+  turns_on(a[0], device);
   const int32_t* pos = vector_or_none<int32_t>(a[1], at::kInt, rows, device);
   const uint16_t *gq = gamma_of(a[4], d, device), *gk = gamma_of(a[5], d, device);
   const cudaStream_t s = stream_of(device);
@@ -193,6 +206,7 @@ PyObject* qk_rope_bwd(PyObject* const* a) {
   int device = -1;
   const Rows gq = head_rows(a[2], hq, d, rows, device), gk = head_rows(a[3], hk, d, rows, device);
   need(device >= 0);
+  turns_on(a[0], device);
   // the inputs of heads without a norm are not read
   const Rows q = head_rows(a[4], a[6] == Py_None ? 0 : hq, d, rows, device);
   const Rows k = head_rows(a[5], a[7] == Py_None ? 0 : hk, d, rows, device);

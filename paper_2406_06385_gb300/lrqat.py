@@ -157,6 +157,7 @@ class QKRope(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("rot_dim", ctypes.c_int32), ("neighbours", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("turns", ctypes.c_void_p)]
+    device = None                      # get_device() of the turns, where `of` has seen them
 
     @classmethod
     def of(cls, n_heads: int, n_kv_heads: int, head_dim: int, turns, neighbours: bool = False,
@@ -170,6 +171,8 @@ class QKRope(ctypes.Structure):
         rope = cls(n_heads, n_kv_heads, head_dim, 0 if turns is None else 2 * turns.numel(), int(neighbours), eps,
                    _ptr(turns))
         rope.turns_tensor = turns
+        if turns is not None:
+            rope.device = turns.get_device()
         return rope
 
 
@@ -533,6 +536,13 @@ def _head_rows(t, heads: int, d: int, rows, device, name: str):
     return t.data_ptr(), _rows(t, heads, d), n, at
 
 
+def _rope_on(rope: QKRope, device) -> None:
+    """Refuses a rotation whose turns lie on another device than a call's arrays, which have to be on the current one."""
+    _on_current(device)
+    if rope.device is not None and rope.device != device:
+        raise LrqatError(-1, f"the turns lie on device {rope.device}, the call's arrays on device {device}")
+
+
 def _gamma(t, d: int, device) -> Optional[int]:
     if t is None:
         return None
@@ -554,7 +564,7 @@ def qk_rope_fwd(rope: QKRope, pos, Q, K, gamma_q, gamma_k, Q_out, K_out, stream=
     k, ldk, rows, device = _head_rows(K, hk, d, rows, device, "K")
     qo, ldqo, _, _ = _head_rows(Q_out, hq, d, rows, device, "Q_out")
     ko, ldko, _, _ = _head_rows(K_out, hk, d, rows, device, "K_out")
-    _on_current(device)
+    _rope_on(rope, device)
     if pos is not None:
         pos = _vector(pos, rows, (_types or _dtypes())[2], device, "pos")
     _check(lib().lrqat_qk_rope_fwd(ctypes.byref(rope), rows, pos, q, ldq, k, ldk, _gamma(gamma_q, d, device),
@@ -582,7 +592,7 @@ def qk_rope_bwd(rope: QKRope, pos, dQ_out, dK_out, Q, K, gamma_q, gamma_k, dQ, d
     _, f32, i32, _ = _types or _dtypes()
     gq, ldgq, rows, device = _head_rows(dQ_out, hq, d, None, None, "dQ_out")
     gk, ldgk, rows, device = _head_rows(dK_out, hk, d, rows, device, "dK_out")
-    _on_current(device)
+    _rope_on(rope, device)
     # the inputs of heads without a norm are not read
     q, ldq, _, _ = _head_rows(Q, 0 if gamma_q is None else hq, d, rows, device, "Q")
     k, ldk, _, _ = _head_rows(K, 0 if gamma_k is None else hk, d, rows, device, "K")

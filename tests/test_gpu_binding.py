@@ -147,6 +147,24 @@ def test_what_is_not_in_order(calls, name):
                 assert got is None
 
 
+@pytest.mark.parametrize("name", ["qk_rope_fwd", "qk_rope_bwd"])
+def test_turns_of_another_device(calls, name, monkeypatch):
+    """As the rotation says where they lie: the addresses are this device's."""
+    args = calls.args[name]
+    monkeypatch.setattr(args[0], "device", 1)
+    assert getattr(LQ._short, name)(*args) is None
+    with pytest.raises(LQ.LrqatError) as e:
+        getattr(LQ, name)(*args)
+    assert e.value.status == -1
+    for other in ("x", 1 << 70):
+        monkeypatch.setattr(args[0], "device", other)
+        assert getattr(LQ._short, name)(*args) is None
+    for fine in (0, None):
+        monkeypatch.setattr(args[0], "device", fine)
+        assert getattr(LQ._short, name)(*args) == 0
+    LQ.get_device_status()
+
+
 def test_structures_that_are_not_in_order(calls):
     t = torch()
     for name, (cls, good) in calls.structures.items():

@@ -240,6 +240,29 @@ def test_binding_checks_rope_arrays(recorded):
     assert len(calls) == 6
 
 
+def test_binding_checks_the_device_of_the_turns(recorded):
+    """Angles of another device than the call's arrays would be followed as an address of this one."""
+    torch, calls, fake = recorded
+    q, g, dg, ws = fake((6, 1, 16), torch.bfloat16), fake((16,), torch.bfloat16), fake((16,), torch.float32), fake((4096,), torch.uint8)
+
+    def run(rope):
+        yield lambda: LQ.qk_rope_fwd(rope, None, q, None, g, None, q, None, stream=0)
+        yield lambda: LQ.qk_rope_bwd(rope, None, q, None, q, None, g, None, q, None, dg, None, False, ws, stream=0)
+
+    here, elsewhere = (LQ.QKRope.of(1, 0, 16, fake((8,), torch.int64, device)) for device in ("cuda:0", "cuda:1"))
+    assert (here.device, elsewhere.device, LQ.QKRope.of(1, 0, 16, None).device) == (0, 1, None)
+    by_hand = LQ.QKRope(1, 0, 16, 16, 0, 0.0, OK)
+    for rope in (here, LQ.QKRope.of(1, 0, 16, None), by_hand):
+        for call in run(rope):
+            call()
+    assert len(calls) == 6
+    for call in run(elsewhere):
+        with pytest.raises(LQ.LrqatError) as e:
+            call()
+        assert e.value.status == -1
+    assert len(calls) == 6
+
+
 def test_binding_checks_block_arrays(recorded):
     torch, calls, fake = recorded
     i32 = torch.int32
