@@ -155,6 +155,7 @@ Room room_of(PyObject* o, int& device) {
   if (o == Py_None) return {};
   const at::Tensor& t = tensor(o);
   on(t, device);
+  need(t.is_contiguous());                   // or fewer bytes than its elements' are there
   return {t.data_ptr(), static_cast<size_t>(t.numel()) * t.element_size()};
 }
 cudaStream_t stream_of(int device) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream(); }

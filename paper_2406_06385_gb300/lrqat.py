@@ -499,6 +499,18 @@ def _row_array(t, heads: int, d: int, rows: int, device) -> int:
     return _rows(t, heads, d, rows)
 
 
+def _scratch(workspace, device):
+    """(address, bytes) of a workspace on the call's device (None: any); its bytes are there where it is dense."""
+    if workspace is None:
+        return None, 0
+    at = workspace.get_device()
+    if at < 0 or (device is not None and at != device):
+        raise LrqatError(-1, "the workspace must lie on the device of the call's other arrays")
+    if not workspace.is_contiguous():
+        raise LrqatError(-1, "the workspace must be dense")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def rope_turns(freq):
     """The frequencies `freq` (radians a position: base ** (-2 i / rot_dim), or a scaled variant) as the fractions of a turn
     that QKRope takes: an int64 host tensor."""
@@ -629,14 +641,6 @@ def _blocks_arrays(blocks: KVBlocks, names, arrays, sizes):
     return out, device
 
 
-def _scratch(workspace, device):
-    if workspace is None:
-        return None, 0
-    if workspace.get_device() != device:
-        raise LrqatError(-1, "the workspace must lie on the device of the call's other arrays")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
 def kv_extend(blocks: KVBlocks, lens, add, free_count, lens_out, free_out, batch_lens, row_start, pos, slot, workspace,
               stream=None) -> None:
     """Room for add[b] > 0 new tokens behind sequence b's lens[b], or -add[b] rows of padding: blocks from the free list into
@@ -691,30 +695,24 @@ def kv_attn_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window
 
 def kv_attn(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, O, workspace, stream=None) -> None:
     """Causal attention of the batch's rows Q over the cache into O, both bf16 [rows, n_heads, head_dim]."""
-    nbytes, device = 0, _device(cache, batch)
-    if workspace is not None:
-        nbytes = workspace.numel() * workspace.element_size()
-        if not workspace.is_cuda:
-            raise LrqatError(-1, "the workspace must lie on the device")
+    device = _device(cache, batch)
+    room, nbytes = _scratch(workspace, device)
     shape, d, rows = Q.shape, cache.head_dim, batch.rows
     heads = shape[1] if len(shape) == 3 else 0
     ldq, ldo = _row_array(Q, heads, d, rows, device), _row_array(O, heads, d, rows, device)
     _check(lib().lrqat_kv_attn(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, _ptr(Q), ldq,
-                               _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
+                               _ptr(O), ldo, room, nbytes, _stream(stream)))
 
 
 def _attn_rows(cache: KVCache, batch: KVBatch, Q, O, workspace):
-    """(query heads, row distances of Q and O, bytes of the workspace, device) of an attention call, checked."""
-    nbytes, device = 0, _device(cache, batch)
-    if workspace is not None:
-        nbytes = workspace.numel() * workspace.element_size()
-        if not workspace.is_cuda:
-            raise LrqatError(-1, "the workspace must lie on the device")
+    """(query heads, row distances of Q and O, workspace and its bytes, device) of an attention call, checked."""
+    device = _device(cache, batch)
+    room, nbytes = _scratch(workspace, device)
     if device is not None:
         _on_current(device)
     heads = Q.shape[1] if len(Q.shape) == 3 else 0
     return (heads, _row_array(Q, heads, cache.head_dim, batch.rows, device),
-            _row_array(O, heads, cache.head_dim, batch.rows, device), nbytes, device)
+            _row_array(O, heads, cache.head_dim, batch.rows, device), room, nbytes, device)
 
 
 def kv_attn_sinks_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window: int, sinks: int) -> int:
@@ -732,9 +730,9 @@ def kv_attn_sinks(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, windo
         status = _short.kv_attn_sinks(cache, batch, Q, softmax_scale, window, sinks, O, workspace)
         if status is not None:
             return _check(status)
-    heads, ldq, ldo, nbytes, _ = _attn_rows(cache, batch, Q, O, workspace)
+    heads, ldq, ldo, room, nbytes, _ = _attn_rows(cache, batch, Q, O, workspace)
     _check(lib().lrqat_kv_attn_sinks(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, sinks, _ptr(Q),
-                                     ldq, _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
+                                     ldq, _ptr(O), ldo, room, nbytes, _stream(stream)))
 
 
 def kv_attn_shared_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, prefix: int) -> int:
@@ -753,7 +751,7 @@ def kv_attn_shared(cache: KVCache, batch: KVBatch, prefix_table, prefix: int, Q,
         status = _short.kv_attn_shared(cache, batch, prefix_table, prefix, Q, softmax_scale, O, workspace)
         if status is not None:
             return _check(status)
-    heads, ldq, ldo, nbytes, device = _attn_rows(cache, batch, Q, O, workspace)
+    heads, ldq, ldo, room, nbytes, device = _attn_rows(cache, batch, Q, O, workspace)
     columns = -(-prefix // cache.block) if prefix > 0 and cache.block > 0 else 0
     if columns and prefix_table is None:
         raise LrqatError(-1, "prefix_table must be given")
@@ -761,7 +759,7 @@ def kv_attn_shared(cache: KVCache, batch: KVBatch, prefix_table, prefix: int, Q,
         device = prefix_table.get_device()
     table = _vector(prefix_table, columns, (_types or _dtypes())[2], device, "prefix_table")
     _check(lib().lrqat_kv_attn_shared(ctypes.byref(cache), ctypes.byref(batch), table, prefix, heads, softmax_scale,
-                                      _ptr(Q), ldq, _ptr(O), ldo, _ptr(workspace), nbytes, _stream(stream)))
+                                      _ptr(Q), ldq, _ptr(O), ldo, room, nbytes, _stream(stream)))
 
 
 def get_device_status(stream=None) -> None:

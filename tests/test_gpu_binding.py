@@ -165,6 +165,19 @@ def test_turns_of_another_device(calls, name, monkeypatch):
     LQ.get_device_status()
 
 
+@pytest.mark.parametrize("name", [n for n in NAMES if n != "qk_rope_fwd"])
+def test_workspaces_that_are_not_there(calls, name):
+    """One element, expanded: its bytes are counted, and would be written behind it."""
+    good = calls.args[name]
+    (i,) = [i for i, x in enumerate(good) if isinstance(x, torch().Tensor) and x.dtype is torch().uint8]
+    for bad in (good[i][:1].expand(good[i].numel()), good[i].repeat_interleave(2)[::2]):
+        args = good[:i] + [bad] + good[i + 1:]
+        assert getattr(LQ._short, name)(*args) is None
+        with pytest.raises(LQ.LrqatError) as e:
+            getattr(LQ, name)(*args)
+        assert e.value.status == -1
+
+
 def test_structures_that_are_not_in_order(calls):
     t = torch()
     for name, (cls, good) in calls.structures.items():

@@ -394,3 +394,37 @@ def test_binding_checks_attention_arrays(recorded, monkeypatch):
             shared(table=bad)
     LQ.kv_attn_shared(cache, batch, None, 0, q, 1.0, q, ws, stream=0)
     assert len(calls) == 5
+
+
+def test_binding_checks_workspaces(recorded, monkeypatch):
+    """One on another device, or whose elements are not all there (a single one, expanded), would be written out of range."""
+    torch, calls, fake = recorded
+    record = lambda name: lambda *a: calls.append((name, a)) or 0  # noqa: E731
+    monkeypatch.setattr(LQ, "lib", lambda: types.SimpleNamespace(**{n: record(n) for n in (
+        "lrqat_qk_rope_bwd", "lrqat_kv_extend", "lrqat_kv_truncate", "lrqat_kv_attn", "lrqat_kv_attn_sinks", "lrqat_kv_attn_shared")}))
+    i32, bf = torch.int32, torch.bfloat16
+    n = lambda k: fake((k,), i32)  # noqa: E731
+    codes, scale = fake((8, 2, 16, 128), torch.int8), fake((8, 2), torch.float32)
+    cache, batch = LQ.KVCache.of(codes, codes, scale, scale), LQ.KVBatch.of(n(2), n(3), fake((2, 4), i32), 6, 3, 64)
+    blocks, rope = LQ.KVBlocks.of(fake((2, 4), i32), n(64), 16), LQ.QKRope.of(4, 0, 128, None)
+    q, g, dg = fake((6, 4, 128), bf), fake((128,), bf), fake((128,), torch.float32)
+
+    def run(ws):
+        yield lambda: LQ.kv_attn(cache, batch, q, 1.0, 8, q, ws, stream=0)
+        yield lambda: LQ.kv_attn_sinks(cache, batch, q, 1.0, 8, 4, q, ws, stream=0)
+        yield lambda: LQ.kv_attn_shared(cache, batch, n(2), 32, q, 1.0, q, ws, stream=0)
+        yield lambda: LQ.kv_extend(blocks, n(2), n(2), n(1), n(2), n(1), n(2), n(3), n(5), None, ws, stream=0)
+        yield lambda: LQ.kv_truncate(blocks, n(2), n(2), n(1), n(2), n(1), ws, stream=0)
+        yield lambda: LQ.qk_rope_bwd(rope, None, q, None, q, None, g, None, q, None, dg, None, False, ws, stream=0)
+
+    good = fake((64,), torch.uint8)
+    expanded = types.SimpleNamespace(**{**vars(good), "is_contiguous": torch.zeros(1).expand(64).is_contiguous})
+    for call in run(good):
+        call()
+    assert len(calls) == 6 and all(OK in a and 64 in a for _, a in calls)
+    for bad in (fake((64,), torch.uint8, "cuda:1"), fake((64,), torch.uint8, "cpu"), expanded):
+        for call in run(bad):
+            with pytest.raises(LQ.LrqatError) as e:
+                call()
+            assert e.value.status == -1
+    assert len(calls) == 6
