@@ -170,7 +170,8 @@ def test_workspaces_that_are_not_there(calls, name):
     """One element, expanded: its bytes are counted, and would be written behind it."""
     good = calls.args[name]
     (i,) = [i for i, x in enumerate(good) if isinstance(x, torch().Tensor) and x.dtype is torch().uint8]
-    for bad in (good[i][:1].expand(good[i].numel()), good[i].repeat_interleave(2)[::2]):
+    room = torch().empty(1 << 21, dtype=torch().uint8, device="cuda")         # a window that is not cut needs none
+    for bad in (room[:1].expand(1 << 20), room[::2]):
         args = good[:i] + [bad] + good[i + 1:]
         assert getattr(LQ._short, name)(*args) is None
         with pytest.raises(LQ.LrqatError) as e:
