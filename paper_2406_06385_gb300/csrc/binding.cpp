@@ -24,11 +24,16 @@ inline void need(bool ok) {
 
 PyObject* g_device = nullptr;   // "device"
 
-// The C structure behind one of the binding's ctypes structures.
+// The binding's ctypes class of a C structure (see `structures`).
+template <typename T>
+PyTypeObject* g_class = nullptr;
+
+// The C structure behind one of the binding's ctypes structures; other bytes of its size are not one.
 template <typename T>
 class Struct {
  public:
   explicit Struct(PyObject* o) {
+    need(g_class<T> && PyObject_TypeCheck(o, g_class<T>));
     if (PyObject_GetBuffer(o, &b_, PyBUF_SIMPLE) != 0) {
       PyErr_Clear();
       throw NotHere{};
@@ -360,9 +365,27 @@ PyObject* fill_blocks(PyObject* const* a) {
   return PyLong_FromLong(device);
 }
 
+// Takes the binding's classes, once, before anything else.
+template <typename T>
+void set_class(PyObject* o) {
+  Py_INCREF(o);
+  g_class<T> = reinterpret_cast<PyTypeObject*>(o);
+}
+PyObject* structures(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 4) return PyErr_Format(PyExc_TypeError, "four classes expected");
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (!PyType_Check(a[i])) return PyErr_Format(PyExc_TypeError, "four classes expected");
+  set_class<lrqat_qk_rope>(a[0]);
+  set_class<lrqat_kv_cache>(a[1]);
+  set_class<lrqat_kv_batch>(a[2]);
+  set_class<lrqat_kv_blocks>(a[3]);
+  Py_RETURN_NONE;
+}
+
 #define ENTRY(name, args) \
   { #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<args, name>)), METH_FASTCALL, nullptr }
-PyMethodDef g_methods[] = {ENTRY(qk_rope_fwd, 8),
+PyMethodDef g_methods[] = {{"structures", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&structures)), METH_FASTCALL, nullptr},
+                           ENTRY(qk_rope_fwd, 8),
                            ENTRY(qk_rope_bwd, 14),
                            ENTRY(kv_extend, 11),
                            ENTRY(kv_truncate, 7),

@@ -224,6 +224,7 @@ def _load_short():
     spec = spec_from_file_location("lrqat_binding", path, loader=ExtensionFileLoader("lrqat_binding", path))
     module = module_from_spec(spec)
     spec.loader.exec_module(module)
+    module.structures(QKRope, KVCache, KVBatch, KVBlocks)
     return module
 
 

@@ -95,6 +95,14 @@ def test_sizes(calls, monkeypatch):
             assert size == getattr(LQ, name)(*args)
 
 
+@pytest.mark.parametrize("name", ["fill_cache", "fill_batch", "fill_blocks"])
+def test_bytes_are_no_structure(calls, name):
+    """Nothing is written into what only has a structure's size."""
+    cls, args = calls.structures[name]
+    room = bytearray(bytes(cls()))
+    assert getattr(LQ._short, name)(room, *args) is None and not any(room)
+
+
 def _others(t, x):
     """What is not in order where the tensor x is."""
     yield x.cpu()

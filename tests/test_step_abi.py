@@ -194,6 +194,34 @@ def test_the_short_way_leaves_what_it_does_not_know(lib):
     assert LQ._short.kv_blocks_workspace_bytes(_rope()) is None and LQ._short.qk_rope_bwd_workspace_bytes(_rope(), 1.5) is None
 
 
+def test_the_short_way_takes_the_bindings_structures_only(lib):
+    """Bytes of a structure's size are not one: the long way takes none either."""
+    pytest.importorskip("torch")
+    LQ.lib()
+    if LQ._short is None:
+        pytest.skip("not built for this torch")
+
+    class MyBlocks(LQ.KVBlocks):
+        pass
+
+    class Twin(ctypes.Structure):
+        _fields_ = LQ.KVBlocks._fields_
+
+    size, blocks, rope = LQ._short.kv_blocks_workspace_bytes, _blocks(), _rope()
+    for other in (bytes(blocks), bytearray(blocks), memoryview(bytes(blocks)), Twin.from_buffer_copy(blocks), (ctypes.c_char * 40)()):
+        assert size(other) is None
+    assert size(MyBlocks.from_buffer_copy(blocks)) == size(blocks) > 0
+    assert LQ._short.qk_rope_bwd_workspace_bytes(bytes(rope), 4) is None
+    sinks, shared = LQ._short.kv_attn_sinks_workspace_bytes, LQ._short.kv_attn_shared_workspace_bytes
+    assert sinks(_cache(), _batch(), 4, 0, 0) is not None and shared(_cache(), _batch(), 4, 16) is not None
+    for c, b in ((bytes(_cache()), _batch()), (_cache(), bytes(_batch())), (_batch(), _batch()), (_cache(), _cache())):
+        assert sinks(c, b, 4, 0, 0) is None and shared(c, b, 4, 16) is None
+    for bad in ((), (int,), (int, int, int, 5)):
+        with pytest.raises(TypeError):
+            LQ._short.structures(*bad)
+    assert size(blocks) > 0
+
+
 def test_binding_checks_rope_arrays(recorded):
     torch, calls, fake = recorded
     bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
