@@ -334,8 +334,8 @@ int lrqat_rope_turns(const double* freq, int32_t n, uint64_t* turns);
 
 /* Q, Q_out: bf16 [T, n_heads, head_dim], K, K_out: bf16 [T, n_kv_heads, head_dim], rows ldq, ldqo, ldk, ldko elements
  * apart (multiples of 8), so that they may be parts of one projection's output; Q_out may be Q itself and K_out K,
- * and an output that overlaps an array of the call otherwise is refused.  pos: int32 [T], or NULL for row t at position t; a row at a negative position is padding and
- * left as it is.  gamma_q, gamma_k: bf16 [head_dim] or NULL. */
+ * and an output that overlaps any other array of the call (or its input's other rows) is refused.  pos: int32 [T], or
+ * NULL for row t at position t; a row at a negative position is padding and left as it is.  gamma_q, gamma_k: bf16 [head_dim] or NULL. */
 int lrqat_qk_rope_fwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* Q, int64_t ldq,
                       const uint16_t* K, int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k,
                       uint16_t* Q_out, int64_t ldqo, uint16_t* K_out, int64_t ldko, lrqat_stream_t stream);
@@ -347,9 +347,10 @@ size_t lrqat_qk_rope_bwd_workspace_bytes(const lrqat_qk_rope* rope, int64_t T);
  * rotated back and r = 1 / sqrt(mean(x^2) + eps),
  *   dx = r (g gamma - x r^2 mean(g gamma x))   (g where gamma is NULL),  dgamma = sum over rows and heads of g x r.
  * dQ_out, dK_out, dQ, dK: bf16, laid out as the forward's arrays; dQ may be dQ_out or Q itself, dK dK_out or K, and one
- * that overlaps an array of the call otherwise is refused.
+ * that overlaps any other array of the call (the workspace included) is refused.
  * Rows at negative positions get a zero gradient and add nothing to dgamma.  dgamma_q, dgamma_k: fp32 [head_dim] or
- * NULL; accumulate = 1 adds to them.  Sums run in a fixed order. */
+ * NULL; accumulate = 1 adds to them.  Sums run in a fixed order.  dgamma_q, dgamma_k and the workspace overlap no row
+ * array (refused), and must not overlap each other, pos, turns or a gamma. */
 int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, const uint16_t* dQ_out, int64_t lddqo,
                       const uint16_t* dK_out, int64_t lddko, const uint16_t* Q, int64_t ldq, const uint16_t* K,
                       int64_t ldk, const uint16_t* gamma_q, const uint16_t* gamma_k, uint16_t* dQ, int64_t lddq,

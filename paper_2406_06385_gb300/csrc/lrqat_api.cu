@@ -772,20 +772,41 @@ bool rows_meet(const uint16_t* p, int64_t ldp, int64_t pw, const uint16_t* q, in
   const int64_t m = (d % ldp + ldp) % ldp;       // from a row of p to the next row of q
   return m < pw || m > ldp - qw;
 }
-// An output may be an input of its own kind itself, and shares nothing with any other array of the call.
+// Whether T rows of `width` elements, ld apart, share bytes with the `bytes` bytes at `flat` (which may lie between rows).
+bool row_meets(const uint16_t* p, int64_t ld, int64_t width, int64_t T, const void* flat, int64_t bytes) {
+  if (!p || !flat || bytes <= 0) return false;
+  const int64_t d = reinterpret_cast<intptr_t>(flat) - reinterpret_cast<intptr_t>(p), behind = d - 2 * width;
+  if (d + bytes <= 0 || behind >= (T - 1) * 2 * ld) return false;
+  const int64_t row = behind < 0 ? 0 : behind / (2 * ld) + 1;      // the first one that ends behind flat's start
+  return row * 2 * ld < d + bytes;
+}
+// An output may be an input of its own kind itself; the rows of an output share nothing with any other array of the call,
+// those of an input nothing with the flat arrays that are written.
 struct RopeRows {
   const uint16_t* p;
   int64_t ld;
 };
-int check_apart(const RopeArgs& a, const RopeRows (&out)[2], const RopeRows (*in)[2], int n_in) {
+struct RopeFlat {
+  const void* p;
+  int64_t bytes;
+  bool written;
+};
+int check_apart(const RopeArgs& a, const RopeRows (&out)[2], const RopeRows (*in)[2], int n_in, const RopeFlat* flat, int n_flat) {
+  auto width = [&](int i) { return static_cast<int64_t>(a.heads[i]) * a.d; };
   auto meet = [&](const RopeRows& x, int i, const RopeRows& y, int j) {
-    return rows_meet(x.p, x.ld, static_cast<int64_t>(a.heads[i]) * a.d, y.p, y.ld, static_cast<int64_t>(a.heads[j]) * a.d, a.T);
+    return rows_meet(x.p, x.ld, width(i), y.p, y.ld, width(j), a.T);
   };
   bool bad = meet(out[0], 0, out[1], 1);
   for (int k = 0; k < n_in; ++k)
     for (int i = 0; i < 2; ++i)
       for (int j = 0; j < 2; ++j)
         if (!(i == j && out[i].p == in[k][j].p && (out[i].ld == in[k][j].ld || a.T == 1))) bad = bad || meet(out[i], i, in[k][j], j);
+  for (int f = 0; f < n_flat; ++f)
+    for (int i = 0; i < 2; ++i) {
+      bad = bad || row_meets(out[i].p, out[i].ld, width(i), a.T, flat[f].p, flat[f].bytes);
+      for (int k = 0; k < n_in && flat[f].written; ++k)
+        bad = bad || row_meets(in[k][i].p, in[k][i].ld, width(i), a.T, flat[f].p, flat[f].bytes);
+    }
   return bad ? fail(LRQAT_ERR_INVALID_ARG, "an output overlaps another array of the call (it may be its own input itself)")
              : static_cast<int>(LRQAT_OK);
 }
@@ -1590,7 +1611,9 @@ int lrqat_qk_rope_fwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, 
     a.X[i] = in[i], a.ldx[i] = ld[i], a.gamma[i] = gamma[i], a.Y[i] = out[i], a.ldy[i] = ldo[i];
   }
   const RopeRows outs[2] = {{a.Y[0], a.ldy[0]}, {a.Y[1], a.ldy[1]}}, ins[1][2] = {{{a.X[0], a.ldx[0]}, {a.X[1], a.ldx[1]}}};
-  LRQAT_TRY(check_apart(a, outs, ins, 1));
+  const RopeFlat flat[] = {{a.turns, 4 * static_cast<int64_t>(a.rot), false}, {pos, 4 * T, false},
+                           {a.gamma[0], 2 * static_cast<int64_t>(a.d), false}, {a.gamma[1], 2 * static_cast<int64_t>(a.d), false}};
+  LRQAT_TRY(check_apart(a, outs, ins, 1, flat, 4));
   DeviceInfo* dev = nullptr;
   LRQAT_TRY(device_info(&dev));
   LRQAT_LAUNCH("qk_rope_fwd", 1, stream, launch_rope_fwd(a, rope->neighbours != 0, dev->sms, stream), "rotation launch");
@@ -1631,8 +1654,9 @@ int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, 
     a.f.X[i] = gamma[i] ? x[i] : nullptr, a.f.ldx[i] = gamma[i] ? ldx[i] : 0, a.dgamma[i] = dgamma[i];
   }
   const bool sums = dgamma_q || dgamma_k;
+  size_t need = 0;
   if (sums) {
-    const size_t need = lrqat_qk_rope_bwd_workspace_bytes(rope, T);
+    need = lrqat_qk_rope_bwd_workspace_bytes(rope, T);
     if (!workspace || workspace_bytes < need)
       return fail(LRQAT_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
     if (!aligned16(workspace)) return fail(LRQAT_ERR_ALIGNMENT, "workspace is not 16-byte aligned");
@@ -1641,7 +1665,11 @@ int lrqat_qk_rope_bwd(const lrqat_qk_rope* rope, int64_t T, const int32_t* pos, 
   if (dgamma_q && dgamma_q == dgamma_k) return fail(LRQAT_ERR_INVALID_ARG, "dgamma_q and dgamma_k must be two arrays");
   const RopeRows outs[2] = {{a.f.Y[0], a.f.ldy[0]}, {a.f.Y[1], a.f.ldy[1]}};
   const RopeRows ins[2][2] = {{{a.dY[0], a.lddy[0]}, {a.dY[1], a.lddy[1]}}, {{a.f.X[0], a.f.ldx[0]}, {a.f.X[1], a.f.ldx[1]}}};
-  LRQAT_TRY(check_apart(a.f, outs, ins, 2));
+  const int64_t d = a.f.d;
+  const RopeFlat flat[] = {{a.f.turns, 4 * static_cast<int64_t>(a.f.rot), false}, {pos, 4 * T, false},
+                           {a.f.gamma[0], 2 * d, false}, {a.f.gamma[1], 2 * d, false}, {a.dgamma[0], 4 * d, true},
+                           {a.dgamma[1], 4 * d, true}, {a.part, static_cast<int64_t>(need), true}};
+  LRQAT_TRY(check_apart(a.f, outs, ins, 2, flat, 7));
   a.accumulate = accumulate;
   DeviceInfo* dev = nullptr;
   LRQAT_TRY(device_info(&dev));

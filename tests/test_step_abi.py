@@ -97,6 +97,53 @@ def test_outputs_that_overlap_other_arrays(lib):
     assert bwd(*a[:4], a[4], a[2], gq=None, dgq=None) == passes
 
 
+def test_outputs_that_overlap_flat_arrays(lib):
+    """Positions, turns, gammas, and behind the gradient dgamma and the workspace: apart from every row of an output, but they
+    may lie between rows.  Addresses are never followed: the calls that pass end at the device."""
+    try:
+        import torch
+        if torch.cuda.is_available():
+            pytest.skip("calls that pass would run")
+    except ImportError:
+        pass
+    T, passes = 4, -5                                              # no device
+    at = lambda array, byte=0: 16 + (array << 20) + byte           # noqa: E731
+    flat = dict(pos=at(10), gq=at(11), gk=at(12))
+    rows = dict(Q=at(1), K=at(2), Qo=at(3), Ko=at(4), ldqo=1024, ldko=1024)
+
+    def fwd(turns=at(13), **kw):
+        return _fwd(lib, _rope(turns=turns), T=T, **{**rows, **flat, **kw})
+
+    bwd_rows = dict(dQo=at(1), dKo=at(2), Q=at(5), K=at(6), dQ=at(3), dK=at(4), lddq=1024, lddk=1024)
+    sums = dict(dgq=at(14), dgk=at(15), ws=at(16))
+
+    def bwd(turns=at(13), **kw):
+        return _bwd(lib, _rope(turns=turns), T=T, **{**bwd_rows, **flat, **sums, **kw})
+
+    assert fwd() == passes and bwd() == passes
+    # rows of 1024 (512) bytes, 2048 bytes apart: places at a row's start, at its end, between rows, in the last row, behind it
+    for array, width in ((3, 1024), (4, 512)):
+        for call, names in ((fwd, ("pos", "turns", "gq", "gk")), (bwd, ("pos", "turns", "gq", "gk", "dgq", "dgk", "ws"))):
+            for name in names:
+                size = dict(pos=4 * T, turns=512, gq=256, gk=256, dgq=512, dgk=512, ws=1 << 18)[name]
+                place = lambda byte: call(**{name: at(array, byte)})  # noqa: E731
+                for byte in (0, width - 16, 2048, 3 * 2048 + width - 16, -16 if size > 16 else 0):
+                    assert place(byte) == -1 and "overlap" in LQ.last_error(), (array, name, byte)
+                assert place(3 * 2048 + width) == passes
+                if name != "ws":
+                    assert place(width) == passes and place(2048 + width) == passes and place(-size) == passes
+    # what is written lies apart from the inputs' rows as well; what is read may lie anywhere among them
+    for array, width in ((1, 1024), (2, 512), (5, 1024), (6, 512)):
+        for name in ("dgq", "dgk", "ws"):
+            for byte in (0, 3 * width, 4 * width - 16):
+                assert bwd(**{name: at(array, byte)}) == -1
+            assert bwd(**{name: at(array, 4 * width)}) == passes
+        assert bwd(pos=at(array), turns=at(array), gq=at(array), gk=at(array)) == passes
+    assert fwd(gq=at(1), gk=at(1), pos=at(2)) == passes
+    # without sums there is no workspace, and inputs of heads without a norm are not read
+    assert bwd(dgq=None, dgk=None, ws=at(3)) == passes and bwd(gq=None, dgq=None, Q=at(14), dgk=at(14, 64)) == passes
+
+
 def test_turns_of_frequencies(lib):
     """Exact to half a unit of 2^-64 turns (pi to 87 digits), wrapped around, for either sign."""
     from fractions import Fraction
