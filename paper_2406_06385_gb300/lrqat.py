@@ -214,7 +214,7 @@ _short_tried = False
 
 
 def _load_short():
-    """The short way, where it has been built for the torch that is running."""
+    """The short way, where it has been built for the torch that is running and loads with it."""
     from importlib.machinery import ExtensionFileLoader
     from importlib.util import module_from_spec, spec_from_file_location
     import torch
@@ -222,8 +222,11 @@ def _load_short():
     if not os.path.exists(path):
         return None
     spec = spec_from_file_location("lrqat_binding", path, loader=ExtensionFileLoader("lrqat_binding", path))
-    module = module_from_spec(spec)
-    spec.loader.exec_module(module)
+    try:
+        module = module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:                # built for a torch of this version with libraries that this one lacks
+        return None
     module.structures(QKRope, KVCache, KVBatch, KVBlocks)
     return module
 

@@ -1,10 +1,13 @@
 """The block table and head rotation entry points reject bad arguments on the host before any CUDA work."""
 import ctypes
 import math
+import os
+import sys
 import types
 
 import pytest
 
+import paper_2406_06385_gb300.build as B
 from paper_2406_06385_gb300 import lrqat as LQ
 from paper_2406_06385_gb300.build import build
 
@@ -239,6 +242,30 @@ def test_the_short_way_leaves_what_it_does_not_know(lib):
     assert LQ._short.kv_blocks_workspace_bytes(_blocks()) == lib.lrqat_kv_blocks_workspace_bytes(ctypes.byref(_blocks())) > 0
     assert LQ._short.qk_rope_bwd_workspace_bytes(_rope(), 4) == lib.lrqat_qk_rope_bwd_workspace_bytes(ctypes.byref(_rope()), 4) > 0
     assert LQ._short.kv_blocks_workspace_bytes(_rope()) is None and LQ._short.qk_rope_bwd_workspace_bytes(_rope(), 1.5) is None
+
+
+def test_a_short_way_that_does_not_load_is_done_without(lib, monkeypatch, tmp_path):
+    """As one that was built for a torch with CUDA does not load with the same version of torch without."""
+    torch = pytest.importorskip("torch")
+    name = f"lrqat_binding-{torch.__version__.split('+')[0]}-{sys.implementation.cache_tag}.so"
+    (tmp_path / name).write_bytes(b"\x7fELF")
+    monkeypatch.setattr(LQ, "LIB_PATH", str(tmp_path / "liblrqat.so"))
+    assert LQ._load_short() is None
+    monkeypatch.setattr(LQ, "_short", LQ._short)
+    monkeypatch.setattr(LQ, "_short_tried", False)
+    assert LQ.lib() is lib and LQ._short is None
+
+
+@pytest.mark.parametrize("command", [["false"], ["no-such-compiler"]])
+def test_a_short_way_that_does_not_compile_is_done_without(lib, monkeypatch, tmp_path, capsys, command):
+    """The library is there all the same, and no short way of older sources beside it."""
+    old = tmp_path / "lrqat_binding.so"
+    old.write_bytes(b"")
+    os.utime(old, (1, 1))
+    monkeypatch.setattr(B, "binding_path", lambda: str(old))
+    monkeypatch.setattr(B, "binding_command", lambda target: command)
+    assert B.build() == B.LIB_PATH and os.path.exists(B.LIB_PATH)
+    assert not old.exists() and "does without" in capsys.readouterr().err
 
 
 def test_the_short_way_takes_the_bindings_structures_only(lib):
