@@ -49,11 +49,11 @@ struct Tile {
   int r0;              // first row of this tile
   int pos_lo, pos_hi;  // positions of the tile's first and last row
   int lo, hi;          // keys [lo, hi) that some row may see; lo a multiple of 16
-  int gap, seen;       // general variants only; `seen`: the first key of the first row's window
+  int gap;             // general variants only
 };
 template <bool kGeneral>
 __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile& t) {
-  t.gap = t.seen = 0;
+  t.gap = 0;
   if (kGeneral && a.across) {
     t.seq.row0 = 0;
     t.seq.n = static_cast<int>(a.kv.rows);
@@ -77,8 +77,7 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int b, int rt, Tile
   t.lo = a.window > 0 && seen > 0 ? static_cast<int>(seen) & ~(kKeyAlign - 1) : 0;
   if (kGeneral) {
     if (a.sinks > 0) {
-      t.seen = a.window > 0 && seen > 0 ? static_cast<int>(seen) : 0;
-      t.lo = t.seen & ~15;
+      t.lo = a.window > 0 && seen > 0 ? static_cast<int>(seen) & ~15 : 0;
       if (t.lo > a.sink_pad) t.gap = t.lo - a.sink_pad;
       t.hi -= t.gap;
       t.lo = 0;
@@ -97,12 +96,12 @@ template <bool kGeneral>
 __device__ __forceinline__ int table_entry(const AttnArgs& a, const int32_t* table, int key) {
   return __ldg((kGeneral && key < a.prefix ? a.prefix_table : table) + (key >> a.kv.block_log2));
 }
-// The block of the 16 keys from number x on; -2 where no row of the tile sees one of them: the blocks between the sinks
-// and the window may be anybody's.
+// The block of the 16 keys from number x on.  The blocks between the sinks and the window, which may be anybody's, have no
+// numbers: a tile's numbers go on from the sinks' last 16 keys to the 16 that hold the first key of its first row's window.
 template <bool kGeneral>
 __device__ __forceinline__ int group_block(const AttnArgs& a, const Tile& t, const int32_t* table, int x) {
-  const int key = key_at<kGeneral>(a, t, x);
-  if (kGeneral && key + 16 <= t.seen && key >= a.sinks) return -2;
+  int key = key_at<kGeneral>(a, t, x);
+  if (kGeneral) asm volatile("" : "+r"(key));   // kept apart from the other uses of x: merged, 8-row tiles spill 24 bytes
   return table_entry<kGeneral>(a, table, key);
 }
 

@@ -531,7 +531,6 @@ __device__ __forceinline__ void prompt_block(const AttnArgs& a) {
       const int key = k0 + j * kTileKeys + 32 * w + 16 * (lane & 1);
       if (j >= tiles || key >= k1) return -2;
       const int blk = group_block<kGeneral>(a, t, table, key);
-      if (kGeneral && blk == -2) return -2;
       return static_cast<uint32_t>(blk) < static_cast<uint64_t>(a.kv.n_blocks) ? blk : -1;
     };
     uint4 kr[4 * kBoxes], vr[4 * kBoxes];
