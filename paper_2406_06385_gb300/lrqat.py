@@ -83,6 +83,13 @@ def _dtypes():
     return _types
 
 
+def _fits(**numbers) -> None:
+    """Refuses whole numbers beyond the 32 bits of the C interface, whose lower bits ctypes would pass."""
+    for name, v in numbers.items():
+        if not -1 << 31 <= v < 1 << 31:
+            raise LrqatError(-1, f"{name} must fit 32 bits (got {v})")
+
+
 class KVCache(ctypes.Structure):
     """Mirror of lrqat_kv_cache."""
     _fields_ = [("n_blocks", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
@@ -145,6 +152,7 @@ class KVBatch(ctypes.Structure):
             raise LrqatError(-1, "lens, row_start and block_table must be int32")
         if not lens.device == row_start.device == block_table.device:
             raise LrqatError(-1, "lens, row_start and block_table must lie on one device")
+        _fits(max_rows=max_rows, max_len=max_len)
         batch = cls(n_seqs, max_blocks, lens.data_ptr(), row_start.data_ptr(), block_table.data_ptr(), rows, max_rows,
                     max_len)
         batch.tensors = (lens, row_start, block_table)
@@ -168,6 +176,7 @@ class QKRope(ctypes.Structure):
             import torch
             if turns.dtype is not torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or not turns.is_cuda:
                 raise LrqatError(-1, "turns must be a dense int64 vector on the device")
+        _fits(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim)
         rope = cls(n_heads, n_kv_heads, head_dim, 0 if turns is None else 2 * turns.numel(), int(neighbours), eps,
                    _ptr(turns))
         rope.turns_tensor = turns
@@ -201,6 +210,7 @@ class KVBlocks(ctypes.Structure):
             raise LrqatError(-1, "block_table and free_ids must be int32")
         if block_table.device != free_ids.device or not block_table.is_cuda:
             raise LrqatError(-1, "block_table and free_ids must lie on one device")
+        _fits(block=block, pinned=pinned)
         n_seqs, max_blocks = block_table.shape
         blocks = cls(n_seqs, max_blocks, block, pinned, free_ids.shape[0], block_table.data_ptr(), free_ids.data_ptr())
         blocks.tensors = (block_table, free_ids)
@@ -694,11 +704,13 @@ def kv_read(cache: KVCache, batch: KVBatch, K, V, stream=None) -> None:
 
 
 def kv_attn_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, window: int = 0) -> int:
+    _fits(n_heads=n_heads, window=window)
     return int(lib().lrqat_kv_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, window))
 
 
 def kv_attn(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, window: int, O, workspace, stream=None) -> None:
     """Causal attention of the batch's rows Q over the cache into O, both bf16 [rows, n_heads, head_dim]."""
+    _fits(window=window)
     device = _device(cache, batch)
     room, nbytes = _scratch(workspace, device)
     shape, d, rows = Q.shape, cache.head_dim, batch.rows
@@ -724,6 +736,7 @@ def kv_attn_sinks_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int, 
         size = _short.kv_attn_sinks_workspace_bytes(cache, batch, n_heads, window, sinks)
         if size is not None:
             return size
+    _fits(n_heads=n_heads, window=window, sinks=sinks)
     return int(lib().lrqat_kv_attn_sinks_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, window, sinks))
 
 
@@ -734,6 +747,7 @@ def kv_attn_sinks(cache: KVCache, batch: KVBatch, Q, softmax_scale: float, windo
         status = _short.kv_attn_sinks(cache, batch, Q, softmax_scale, window, sinks, O, workspace)
         if status is not None:
             return _check(status)
+    _fits(window=window, sinks=sinks)
     heads, ldq, ldo, room, nbytes, _ = _attn_rows(cache, batch, Q, O, workspace)
     _check(lib().lrqat_kv_attn_sinks(ctypes.byref(cache), ctypes.byref(batch), heads, softmax_scale, window, sinks, _ptr(Q),
                                      ldq, _ptr(O), ldo, room, nbytes, _stream(stream)))
@@ -744,6 +758,7 @@ def kv_attn_shared_workspace_bytes(cache: KVCache, batch: KVBatch, n_heads: int,
         size = _short.kv_attn_shared_workspace_bytes(cache, batch, n_heads, prefix)
         if size is not None:
             return size
+    _fits(n_heads=n_heads, prefix=prefix)
     return int(lib().lrqat_kv_attn_shared_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, prefix))
 
 
@@ -755,6 +770,7 @@ def kv_attn_shared(cache: KVCache, batch: KVBatch, prefix_table, prefix: int, Q,
         status = _short.kv_attn_shared(cache, batch, prefix_table, prefix, Q, softmax_scale, O, workspace)
         if status is not None:
             return _check(status)
+    _fits(prefix=prefix)
     heads, ldq, ldo, room, nbytes, device = _attn_rows(cache, batch, Q, O, workspace)
     columns = -(-prefix // cache.block) if prefix > 0 and cache.block > 0 else 0
     if columns and prefix_table is None:

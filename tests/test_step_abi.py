@@ -530,3 +530,44 @@ def test_binding_checks_workspaces(recorded, monkeypatch):
                 call()
             assert e.value.status == -1
     assert len(calls) == 6
+
+
+@pytest.mark.parametrize("beyond", [1 << 32, (1 << 32) + 5, 1 << 31, -(1 << 31) - 1, 1 << 70])
+def test_binding_refuses_numbers_beyond_32_bits(recorded, monkeypatch, beyond):
+    """Their lower 32 bits are another number: 2^32 + 5 sinks would be 5, a window of 2^32 none."""
+    torch, _, fake = recorded
+    calls = []
+    record = lambda *a: calls.append(a) or 0  # noqa: E731
+    monkeypatch.setattr(LQ, "_short", None)                        # which leaves such numbers to the long way
+    monkeypatch.setattr(LQ, "lib", lambda: types.SimpleNamespace(**{f"lrqat_kv_attn{n}": record for n in (
+        "", "_sinks", "_shared", "_workspace_bytes", "_sinks_workspace_bytes", "_shared_workspace_bytes")}))
+    i32 = torch.int32
+    n = lambda k: fake((k,), i32)  # noqa: E731
+    codes, scale, table, q = fake((8, 2, 16, 128), torch.int8), fake((8, 2), torch.float32), fake((2, 4), i32), fake((6, 4, 128), torch.bfloat16)
+    cache, batch = LQ.KVCache.of(codes, codes, scale, scale), LQ.KVBatch.of(n(2), n(3), table, 6, 3, 64)
+
+    def run(v):
+        yield lambda: LQ.kv_attn(cache, batch, q, 1.0, v, q, None, stream=0)
+        yield lambda: LQ.kv_attn_sinks(cache, batch, q, 1.0, v, 4, q, None, stream=0)
+        yield lambda: LQ.kv_attn_sinks(cache, batch, q, 1.0, 8, v, q, None, stream=0)
+        yield lambda: LQ.kv_attn_shared(cache, batch, n(2), v, q, 1.0, q, None, stream=0)
+        yield lambda: LQ.kv_attn_workspace_bytes(cache, batch, 4, v)
+        yield lambda: LQ.kv_attn_sinks_workspace_bytes(cache, batch, 4, v, 4)
+        yield lambda: LQ.kv_attn_sinks_workspace_bytes(cache, batch, 4, 8, v)
+        yield lambda: LQ.kv_attn_shared_workspace_bytes(cache, batch, 4, v)
+        yield lambda: LQ.KVBatch.of(n(2), n(3), table, 6, v, 64)
+        yield lambda: LQ.KVBatch.of(n(2), n(3), table, 6, 3, v)
+        yield lambda: LQ.KVBlocks.of(table, n(64), v, 1)
+        yield lambda: LQ.KVBlocks.of(table, n(64), 16, v)
+        yield lambda: LQ.QKRope.of(v, 1, 128, None)
+        yield lambda: LQ.QKRope.of(1, v, 128, None)
+        yield lambda: LQ.QKRope.of(1, 1, v, None)
+
+    for call in run(16):
+        call()
+    assert len(calls) == 8
+    for call in run(beyond):
+        with pytest.raises(LQ.LrqatError) as e:
+            call()
+        assert e.value.status == -1
+    assert len(calls) == 8
