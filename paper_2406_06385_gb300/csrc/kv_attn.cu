@@ -733,6 +733,8 @@ void plan_attn(AttnArgs& a, int sms) {
   a.splits = static_cast<int>(splits < 1 ? 1 : splits);
 }
 
+// Asked of the bound on one sequence's rows, whatever the others have: 63 single tokens beside one sequence of 32 rows, 4
+// heads a key head, behind 16000 tokens 79 us, beside one of 33 rows, each over the prefix alone, 918.
 bool shared_together(const AttnArgs& a) {
   return a.kv.n_seqs > 1 && static_cast<int64_t>(a.kv.max_rows) * a.group <= 128;
 }
@@ -745,6 +747,9 @@ double apart_ns(const AttnArgs& a, int sms) {
   return plan_pieces(a, a.kv.max_len, a.tile_rows, sms).ns;
 }
 
+// The bounds stand for what the sequences hold, and the constants, as plan_pieces', are of 8 heads of 128.  What own keys
+// might take makes the prefix's pieces longer: 64 single tokens behind 16000 with up to 501 of their own 38 us under their
+// own bound, 79 under 1.25 times it, 264 (one piece, a block a head) from twice it on; 16 x 5 rows behind 2000 27, 27 and 39.
 // At most one wave of pieces: a piece costs its start and its join whatever its length.  Blocks of the prompt kernel have
 // an SM to themselves, and the sequences' own keys (`own`, planned), which run beside them, what is left and then all: a
 // piece takes 9 us and 2 us a tile of 128 keys; own keys, of an SM, 0.75 us a block and three quarters of their bound's

@@ -16,17 +16,18 @@
 // Scores and O live in tensor memory: 2 x 2 x 64 and 2 x d columns.
 //
 // Four prompts of up to 4000 tokens behind 500 older ones, 32 query and 8 key/value heads of 128: 513 us,
-// 990 TFLOP/s, 53% of the rate of a plain product; behind a window of 1000 tokens and 4 sinks 322 us (floor 117: a block
-// has 8.6 tiles of keys).  A tile of 256 rows and 128 keys takes about 3700 cycles, its matrix instructions 2033, a step
+// 990 TFLOP/s, 53% of the rate of a plain product; behind a window of 1000 tokens and 4 sinks 319 us (floor 117: a block
+// has 8.6 tiles of keys; 322 when the others below were measured).  A tile of 256 rows and 128 keys takes about 3700 cycles, its matrix instructions 2033, a step
 // whose columns are masked one by one 900 more than another; the first scores come after 12600 cycles (arrays of the
 // sequence 2400, barriers 1300, table and codes 3700, q and the keys turned into halves beside each other 3000), and
 // behind the last the rows take 5000 to leave.  Of an earlier 524 us, without the softmax's arithmetic the call would
 // take 407, without the producers' stores 479, without both 358, almost without matrix instructions still 505.
 // Measured against it: two threads a row 686 of 524 (the exchange of their maxima), one 128-key score buffer 834, eight
 // producer warps with 136 softmax registers 574; a row of q and of O a thread, not whole lines by the warp, 525 of 513;
-// 184, 104 and 40 registers, with spills in the issuing threads, 330 of 322 behind the window; blocks that stay and take over the grid
-// positions of blocks not yet launched, q and keys of the next item brought in beside this one's last steps, 549 us where
-// this takes 536 (one tile of long sequences) and 317 where it takes 322 (the window).
+// 184, 104 and 40 registers, with spills in the issuing threads, 330 of 322 behind the window (176, 104 and 56 spill none);
+// blocks that stay and take over the grid positions of blocks not yet launched, q and keys of the next item brought in
+// beside this one's last steps, 549 us where this takes 536 (one tile of long sequences) and 317 where it takes 322 (the
+// window).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cstdint>

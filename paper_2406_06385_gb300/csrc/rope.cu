@@ -8,7 +8,8 @@
 //
 // An angle is kept in turns, w / (2 pi), modulo 1 as a 64-bit fraction: pos times the 64-bit fraction of
 // freq_i / (2 pi) wraps around by itself, so an angle is off by at most pos 2^-65 turns, 2^-34 at the farthest
-// position, for one multiplication of whole numbers; the sine and cosine then see the fraction rounded to 24 bits.
+// position, for one multiplication of whole numbers.  The sine and cosine see its upper 32 bits (less than 2^-32 turns
+// below it) rounded to 24 (up to 2^-26): fp32 angles could not tell more apart.
 #include <cuda_runtime.h>
 #include <cstdint>
 #include <type_traits>
@@ -178,6 +179,7 @@ __global__ void __launch_bounds__(kRopeThreads, kFwdPerSm) rope_fwd_kernel(RopeA
 // more): a lane keeps the sums of dgamma for its 16 elements in registers over all its tokens, and gamma as well; heads,
 // warps and blocks are added in a fixed order afterwards.  The words of the next kRing groups are on their way into
 // shared memory, tokens' ends or not; a lane copies, waits for and reads its own words only, so nothing guards them.
+// 128 registers a thread: heads that fill their lanes and rotate whole spill none, the others 8 to 48 bytes.
 constexpr int kRing = 3;
 template <int L, bool kNeighbours, bool kFull>
 __global__ void __launch_bounds__(kRopeThreads, kBwdPerSm) rope_bwd_kernel(RopeBwdArgs a, int per) {

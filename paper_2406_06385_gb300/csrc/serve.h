@@ -182,7 +182,7 @@ inline int attn_grid_seqs(const AttnArgs& a) { return a.across ? 1 : a.kv.n_seqs
 void plan_attn(AttnArgs& a, int sms);
 // A call in which each sequence goes over a shared prefix and its own keys, and one in which the rows of all go over the
 // prefix together (planned here) and then each sequence over its own keys (`own`, planned): about how long they take.
-// shared_together: whether that is worth a comparison; sequences with many rows keep the machine busy by themselves.
+// shared_together: whether they are compared at all, where no sequence may have many rows.
 bool shared_together(const AttnArgs& a);
 double apart_ns(const AttnArgs& a, int sms);
 double plan_prefix(AttnArgs& a, const AttnArgs& own, int sms);
