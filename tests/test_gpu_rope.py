@@ -143,6 +143,32 @@ def test_backward(T, hq, hk, d, rot, neighbours, norm):
         assert dgamma[i] is None or t.equal(dgamma2[i], dgamma[i] + dgamma[i])
 
 
+@pytest.mark.parametrize("T,hq,hk,d", [(20011, 8, 1, 128), (60001, 1, 1, 64)])
+def test_dgamma_of_many_terms(T, hq, hk, d):
+    """Sums of up to 160088 terms.  However they are ordered, one of n terms in a chain of additions per lane, with lanes,
+    warps and blocks joined by trees and short chains behind it, is off by at most 2^-24 of the terms' magnitudes for each
+    addition that a term goes through: here the lane's own (two blocks of 8 warps an SM, a warp's lanes 512 elements at a
+    time), at most 4 among a warp's heads, 8 among warps, a 32nd of the blocks, 5 in the tree, one to accumulate.  A term
+    itself is off by 2^-18, as above."""
+    rng, freq, rope, pos, g_dev, g = _setup(T, hq, hk, d, d, False, (True, True), T)
+    t = torch()
+    heads = (hq, hk)
+    x, dy = ([_bf16(rng, T, h, d) for h in heads] for _ in range(2))
+    dgamma = [t.zeros(d, device="cuda") for _ in range(2)]
+    ws = empty((LQ.qk_rope_bwd_workspace_bytes(rope, T),), t.uint8)
+    out = [t.empty((T, h, d), dtype=t.int16, device="cuda") for h in heads]
+    LQ.qk_rope_bwd(rope, to_dev(pos), *[to_dev(v[0]) for v in dy + x], *g_dev, *out, *dgamma, False, ws)
+    LQ.get_device_status()
+    blocks = 2 * t.cuda.get_device_properties(0).multi_processor_count
+    for i, h in enumerate(heads):
+        _, dg = SO.head_norm_rope_bwd(dy[i][1], x[i][1], g[i], pos, freq, EPS)
+        s, xx = _pair_sum(dy[i][1], d, False), np.abs(x[i][1])
+        terms = (s * xx / np.sqrt((xx * xx).mean(-1, keepdims=True) + EPS)).sum((0, 1))
+        lane = -(-T // (8 * blocks)) * -(-h * d // 512)
+        depth = lane + 4 + 8 + -(-blocks // 32) + 5 + 1
+        assert (np.abs(dgamma[i].cpu().numpy() - dg) <= (2.0 ** -18 + depth * 2.0 ** -24) * terms).all()
+
+
 def test_rows_without_a_position():
     """pos None is row t at position t; rows at negative positions stay as they were in the forward and have a zero gradient
     (their inputs may be anything) that adds nothing to dgamma."""
